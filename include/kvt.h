@@ -103,6 +103,64 @@ typedef struct {
 kvt_status kvt_append_kv(const kvt_pool* pool, const kvt_seqs* seqs,
                          const void* k_new, const void* v_new, void* stream);
 
+/* Rotary positions: pairs of columns (a, b) of a row turn by theta,
+ *   a' = a cos theta - b sin theta,   b' = b cos theta + a sin theta,
+ * with theta = positions[axis[j]][row] * inv_freq[j] for pair j of rot_dim/2.
+ * theta is taken as that product of exact values, reduced in fp64, so far
+ * positions lose nothing; the rotation is fp32, rounded once. */
+typedef struct {
+  const float*   inv_freq;    /* HOST [rot_dim/2], finite: radians per position */
+  const int32_t* axis;        /* HOST [rot_dim/2], each in [0,num_axes), or NULL: all on axis 0 */
+  const int32_t* positions;   /* DEVICE [num_axes][T], any int32 values; kvt_append_kv_rotary also takes NULL
+                                 with num_axes = 1: the logical positions P_b + t */
+  int32_t        num_axes;    /* 1 .. 64 (a text's or audio's place: 1; time, height, width: 3) */
+  int32_t        rot_dim;     /* R: rotated columns of each part, a positive multiple of 16, at most
+                                 head_dim / parts; the columns past them are copied */
+  int32_t        parts;       /* 1, or 2: each half of a head's columns is rotated by itself, as the two maps
+                                 of differential attention need it */
+  int32_t        interleaved; /* 0: pairs are columns (j, j + R/2) of a part; 1: (2j, 2j + 1) */
+} kvt_rotary;
+
+/* Per-token rows [T][heads][head_dim]: the heads of one token are contiguous,
+ * consecutive tokens lie `stride` elements apart (>= heads * head_dim, a
+ * multiple of 16 bytes; ignored for T = 1).  So q, K and V can be read where a
+ * fused projection left them.  data: device, 16-byte aligned. */
+typedef struct {
+  void*   data;
+  int64_t stride;
+} kvt_rows;
+
+/*
+ * kvt_rotate -- rotary positions of num_tokens rows of num_heads heads.
+ *
+ * x, out: rows of head_dim 64 or 128 in `dtype` (else KVT_ERR_UNSUPPORTED).
+ * out may be x itself (same data, same stride) and must not touch x's rows
+ * otherwise.  num_tokens = 0 is a no-op; num_tokens * num_heads at most
+ * INT32_MAX.  rotary->positions is required, [num_axes][num_tokens].
+ */
+kvt_status kvt_rotate(const kvt_rotary* rotary, const kvt_rows* x, int64_t num_tokens, int32_t num_heads,
+                      int32_t head_dim, int32_t dtype, const kvt_rows* out, void* stream);
+
+/*
+ * kvt_append_kv_rotary -- kvt_append_kv with the rotary positions applied on
+ * the way: K rows are rotated as they go into their pages, V rows are bit
+ * copies, and with q given its rows are rotated into q_out in the same launch
+ * (one launch per layer and step instead of three).
+ *
+ * For every b, t < S_b, kv-head g, with p = P_b + t:
+ *   k_pool[block_table[b][p/16]][g][p%16][:] = rotate(k_new[off_b + t][g][:])
+ *   v_pool[block_table[b][p/16]][g][p%16][:] = v_new[off_b + t][g][:]
+ *   q_out[off_b + t][h][:] = rotate(q[off_b + t][h][:])
+ * k_new, v_new: rows of Hkv heads; q, q_out: rows of num_q_heads heads (a
+ * multiple of Hkv, T * num_q_heads at most INT32_MAX), or both NULL with
+ * num_q_heads = 0.  q_out may be q itself (same data, same stride) and must
+ * not touch q, k_new or v_new otherwise; nothing may overlap a pool.  Pool,
+ * table, checked mode and ordering as for kvt_append_kv.
+ */
+kvt_status kvt_append_kv_rotary(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rotary* rotary,
+                                const kvt_rows* k_new, const kvt_rows* v_new,
+                                const kvt_rows* q, int32_t num_q_heads, const kvt_rows* q_out, void* stream);
+
 /*
  * kvt_extend_attention -- causal attention of the new tokens over prefix + suffix.
  *

@@ -198,6 +198,74 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+// The arguments of a rotation: inv_freq and axis (addresses of host arrays, axis
+// or None), positions (device address or None), num_axes, rot_dim, parts,
+// interleaved.
+constexpr Py_ssize_t kRotary = 7;
+bool rotary(PyObject* const* a, kvt_rotary* r) {
+  void *f, *x, *p;
+  if (!address(a[0], &f) || !address(a[1], &x) || !address(a[2], &p) || !int32(a[3], &r->num_axes) ||
+      !int32(a[4], &r->rot_dim) || !int32(a[5], &r->parts) || !int32(a[6], &r->interleaved))
+    return false;
+  r->inv_freq = reinterpret_cast<const float*>(f);
+  r->axis = reinterpret_cast<const int32_t*>(x);
+  r->positions = reinterpret_cast<const int32_t*>(p);
+  return true;
+}
+// Per-token rows: address, stride.
+bool rows(PyObject* const* a, kvt_rows* r) {
+  long long stride;
+  if (!address(a[0], &r->data) || !integer(a[1], &stride)) return false;
+  r->stride = stride;
+  return true;
+}
+
+// append_rotary(head..., rotary..., k_new, stride, v_new, stride, q, stride,
+// num_q_heads, q_out, stride, stream) -> status; q and q_out None: K and V only
+PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  kvt_rotary rot;
+  kvt_rows k, v, q, qo;
+  int32_t hq;
+  void* stream;
+  const Py_ssize_t at = kHead + kRotary;
+  if (!count_is(n, at + 10) || !head(a, &h) || !rotary(a + kHead, &rot) || !rows(a + at, &k) ||
+      !rows(a + at + 2, &v) || !rows(a + at + 4, &q) || !int32(a[at + 6], &hq) || !rows(a + at + 7, &qo) ||
+      !address(a[at + 9], &stream))
+    return nullptr;
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_append_kv_rotary)>(h.fn)(&h.pool, &h.seqs, &rot, &k, &v,
+                                                               q.data != nullptr ? &q : nullptr, hq,
+                                                               qo.data != nullptr ? &qo : nullptr, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// rotate(entry point, rotary..., x, stride, num_tokens, num_heads, head_dim,
+// dtype, out, stride, stream) -> status
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *fn, *stream;
+  kvt_rotary rot;
+  kvt_rows x, out;
+  long long tokens;
+  int32_t heads, d, dtype;
+  const Py_ssize_t at = 1 + kRotary;
+  if (!count_is(n, at + 9) || !address(a[0], &fn) || !rotary(a + 1, &rot) || !rows(a + at, &x) ||
+      !integer(a[at + 2], &tokens) || !int32(a[at + 3], &heads) || !int32(a[at + 4], &d) ||
+      !int32(a[at + 5], &dtype) || !rows(a + at + 6, &out) || !address(a[at + 8], &stream))
+    return nullptr;
+  if (fn == nullptr) {
+    PyErr_SetString(PyExc_TypeError, "bad entry point");
+    return nullptr;
+  }
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_rotate)>(fn)(&rot, &x, tokens, heads, d, dtype, &out, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 // workspace(head..., num_q_heads[, shared_len, mode]) -> bytes
 PyObject* workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Head h;
@@ -243,6 +311,8 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f))
 PyMethodDef methods[] = {{"pack", FAST(pack), METH_FASTCALL, nullptr},
                          {"append", FAST(append), METH_FASTCALL, nullptr},
+                         {"append_rotary", FAST(append_rotary), METH_FASTCALL, nullptr},
+                         {"rotate", FAST(rotate), METH_FASTCALL, nullptr},
                          {"workspace", FAST(workspace), METH_FASTCALL, nullptr},
                          {"attend", FAST(attend), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -13,6 +13,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <new>
 #include <numeric>
 #include <unordered_set>
 #include <vector>
@@ -96,6 +97,21 @@ kvt_status check_table_ids(const kvt_pool* pool, const kvt_seqs* seqs) {
     const int32_t* row = seqs->block_table_host + (int64_t)b * seqs->max_blocks;
     for (int64_t i = 0; i < nblk; ++i)
       if (row[i] < 0 || (int64_t)row[i] >= pool->num_blocks) return KVT_ERR_OUT_OF_RANGE;
+  }
+  return KVT_OK;
+}
+
+// Checked mode: two new tokens may not target one (block, slot).
+kvt_status check_append_targets(const kvt_seqs* seqs) {
+  if (seqs->block_table_host == nullptr) return KVT_OK;
+  std::unordered_set<int64_t> seen;
+  for (int b = 0; b < seqs->num_seqs; ++b) {
+    const int32_t* row = seqs->block_table_host + (int64_t)b * seqs->max_blocks;
+    for (int32_t t = 0; t < seqs->suffix_len[b]; ++t) {
+      const int64_t pos = (int64_t)seqs->prefix_len[b] + t;
+      const int64_t key = (int64_t)row[pos / kvt::kBlock] * kvt::kBlock + pos % kvt::kBlock;
+      if (!seen.insert(key).second) return KVT_ERR_OUT_OF_RANGE;
+    }
   }
   return KVT_OK;
 }
@@ -729,6 +745,53 @@ kvt_status combine(const kvt::ExtendArgs& a, const kvt_pool* pool, void* out, fl
   return e == hipSuccess ? KVT_OK : device_error(e);
 }
 
+// Per-token rows of `width` elements of `es` bytes: where the `T` rows lie.
+struct Rows {
+  uintptr_t first;
+  size_t width, step;   // bytes of a row, bytes from row to row
+  int64_t n;
+  size_t extent() const { return (size_t)(n - 1) * step + width; }
+};
+kvt_status check_rows(const kvt_rows* r, int64_t T, int64_t width, int es, Rows* out) {
+  if (r->data == nullptr || !aligned16(r->data)) return KVT_ERR_INVALID_ARG;
+  const int64_t stride = T == 1 ? width : r->stride;
+  if (stride < width || stride * es % 16 != 0 || stride > INT64_MAX / 8 / T) return KVT_ERR_INVALID_ARG;
+  *out = Rows{(uintptr_t)r->data, (size_t)(width * es), (size_t)(stride * es), T};
+  return KVT_OK;
+}
+// Whether two row sets share a byte.  Rows of one stride interleave without
+// touching (parts of one fused projection); of two strides only disjoint
+// extents are taken as apart.
+bool rows_touch(const Rows& x, const Rows& y) {
+  if (!overlaps((const void*)x.first, x.extent(), (const void*)y.first, y.extent())) return false;
+  if (x.step != y.step) return true;
+  const size_t ahead = y.first >= x.first ? (y.first - x.first) % x.step
+                                          : (x.step - (x.first - y.first) % x.step) % x.step;
+  return ahead < x.width || ahead + y.width > x.step;
+}
+bool rows_same(const Rows& x, const Rows& y) { return x.first == y.first && x.width == y.width && x.step == y.step; }
+
+// The rotary description; fills the launch's frequencies.
+kvt_status check_rotary(const kvt_rotary* r, int32_t head_dim, kvt::RotaryArgs* a) {
+  if (r == nullptr || r->inv_freq == nullptr) return KVT_ERR_INVALID_ARG;
+  if ((r->parts != 1 && r->parts != 2) || (r->interleaved != 0 && r->interleaved != 1)) return KVT_ERR_INVALID_ARG;
+  if (r->rot_dim < 16 || r->rot_dim % 16 != 0 || r->rot_dim > head_dim / r->parts) return KVT_ERR_INVALID_ARG;
+  if (r->num_axes < 1 || r->num_axes > 64) return KVT_ERR_INVALID_ARG;
+  if (((uintptr_t)r->positions & 3) != 0) return KVT_ERR_INVALID_ARG;
+  for (int j = 0; j < r->rot_dim / 2; ++j) {
+    if (!std::isfinite(r->inv_freq[j])) return KVT_ERR_INVALID_ARG;
+    const int32_t axis = r->axis != nullptr ? r->axis[j] : 0;
+    if (axis < 0 || axis >= r->num_axes) return KVT_ERR_INVALID_ARG;
+    a->turns[j] = (double)r->inv_freq[j] / (2.0 * 3.14159265358979323846);
+    a->axis[j] = (uint8_t)axis;
+  }
+  a->positions = r->positions;
+  a->rot_dim = r->rot_dim;
+  a->parts = r->parts;
+  a->interleaved = r->interleaved;
+  return KVT_OK;
+}
+
 // The argument checks of kvt_extend_attention (and its no-alloc variant);
 // fills the total token count.
 kvt_status check_extend(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
@@ -807,19 +870,7 @@ kvt_status kvt_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const void*
   for (const void* src : {k_new, v_new})
     for (const void* dst : {(const void*)pool->k, (const void*)pool->v})
       if (overlaps(src, new_bytes, dst, pool_bytes)) return KVT_ERR_INVALID_ARG;
-  if (seqs->block_table_host != nullptr) {
-    // two new tokens may not target one (block, slot)
-    std::unordered_set<int64_t> seen;
-    seen.reserve((size_t)T * 2);
-    for (int b = 0; b < seqs->num_seqs; ++b) {
-      const int32_t* row = seqs->block_table_host + (int64_t)b * seqs->max_blocks;
-      for (int32_t t = 0; t < seqs->suffix_len[b]; ++t) {
-        const int64_t pos = (int64_t)seqs->prefix_len[b] + t;
-        const int64_t key = (int64_t)row[pos / kvt::kBlock] * kvt::kBlock + pos % kvt::kBlock;
-        if (!seen.insert(key).second) return KVT_ERR_OUT_OF_RANGE;
-      }
-    }
-  }
+  if ((st = check_append_targets(seqs)) != KVT_OK) return st;
 
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   kvt::AppendArgs a;
@@ -847,6 +898,102 @@ kvt_status kvt_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const void*
     if (e != hipSuccess) return device_error(e);
   }
   return KVT_OK;
+}
+
+kvt_status kvt_rotate(const kvt_rotary* rotary, const kvt_rows* x, int64_t num_tokens, int32_t num_heads,
+                      int32_t head_dim, int32_t dtype, const kvt_rows* out, void* stream) {
+  if (head_dim != 64 && head_dim != 128) return KVT_ERR_UNSUPPORTED;
+  if (dtype != KVT_DTYPE_BF16 && dtype != KVT_DTYPE_F32) return KVT_ERR_UNSUPPORTED;
+  kvt::RotaryArgs a;
+  std::memset(&a, 0, sizeof(a));
+  kvt_status st = check_rotary(rotary, head_dim, &a);
+  if (st != KVT_OK) return st;
+  if (x == nullptr || out == nullptr || num_tokens < 0 || num_heads < 1) return KVT_ERR_INVALID_ARG;
+  if (num_tokens == 0) return KVT_OK;
+  if (num_tokens > INT32_MAX / num_heads || rotary->positions == nullptr) return KVT_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)num_heads * head_dim;
+  Rows from, to;
+  if ((st = check_rows(x, num_tokens, width, elem_bytes(dtype), &from)) != KVT_OK) return st;
+  if ((st = check_rows(out, num_tokens, width, elem_bytes(dtype), &to)) != KVT_OK) return st;
+  if (!rows_same(from, to) && rows_touch(from, to)) return KVT_ERR_INVALID_ARG;
+  a.q = x->data;
+  a.q_out = out->data;
+  a.q_stride = x->stride;
+  a.q_out_stride = out->stride;
+  a.num_q_heads = num_heads;
+  a.rows = a.total_rows = num_tokens;
+  const hipError_t e = kvt::launch_rotary(a, dtype, head_dim, device_cus(), reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? KVT_OK : device_error(e);
+}
+
+kvt_status kvt_append_kv_rotary(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rotary* rotary,
+                                const kvt_rows* k_new, const kvt_rows* v_new, const kvt_rows* q, int32_t num_q_heads,
+                                const kvt_rows* q_out, void* stream) try {
+  kvt_status st = check_pool(pool);
+  if (st != KVT_OK) return st;
+  int64_t T = 0;
+  if ((st = check_seqs(seqs, &T)) != KVT_OK) return st;
+  kvt::RotaryArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if ((st = check_rotary(rotary, pool->head_dim, &a)) != KVT_OK) return st;
+  if (rotary->positions == nullptr && rotary->num_axes != 1) return KVT_ERR_INVALID_ARG;
+  if (k_new == nullptr || v_new == nullptr || (q == nullptr) != (q_out == nullptr)) return KVT_ERR_INVALID_ARG;
+  if (q == nullptr ? num_q_heads != 0 : !heads_ok(pool, num_q_heads, T)) return KVT_ERR_INVALID_ARG;
+  const int es = elem_bytes(pool->dtype);
+  const int64_t kv_width = (int64_t)pool->num_kv_heads * pool->head_dim;
+  Rows k, v, qi, qo;
+  if ((st = check_rows(k_new, T, kv_width, es, &k)) != KVT_OK) return st;
+  if ((st = check_rows(v_new, T, kv_width, es, &v)) != KVT_OK) return st;
+  const size_t pool_bytes = (size_t)pool->num_blocks * kvt::kBlock * kv_width * es;
+  auto in_pool = [&](const Rows& r) {
+    return overlaps((const void*)r.first, r.extent(), pool->k, pool_bytes) ||
+           overlaps((const void*)r.first, r.extent(), pool->v, pool_bytes);
+  };
+  if (in_pool(k) || in_pool(v)) return KVT_ERR_INVALID_ARG;
+  if (q != nullptr) {
+    const int64_t q_width = (int64_t)num_q_heads * pool->head_dim;
+    if ((st = check_rows(q, T, q_width, es, &qi)) != KVT_OK) return st;
+    if ((st = check_rows(q_out, T, q_width, es, &qo)) != KVT_OK) return st;
+    if (in_pool(qi) || in_pool(qo) || rows_touch(qo, k) || rows_touch(qo, v)) return KVT_ERR_INVALID_ARG;
+    if (!rows_same(qi, qo) && rows_touch(qi, qo)) return KVT_ERR_INVALID_ARG;
+    a.q = q->data;
+    a.q_out = q_out->data;
+    a.q_stride = q->stride;
+    a.q_out_stride = q_out->stride;
+    a.num_q_heads = num_q_heads;
+  }
+  if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
+  if ((st = check_append_targets(seqs)) != KVT_OK) return st;
+
+  a.k_new = k_new->data;
+  a.v_new = v_new->data;
+  a.k_stride = k_new->stride;
+  a.v_stride = v_new->stride;
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.block_table = seqs->block_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.total_rows = T;
+  int32_t row = 0;
+  for (int b0 = 0; b0 < seqs->num_seqs; b0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - b0);
+    a.nseq = n;
+    a.row_begin = row;
+    for (int i = 0; i < n; ++i) {
+      const int b = b0 + i;
+      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row};
+      row += seqs->suffix_len[b];
+    }
+    a.rows = row - a.row_begin;
+    const hipError_t e =
+        kvt::launch_rotary(a, pool->dtype, pool->head_dim, device_cus(), reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
 }
 
 size_t kvt_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {

@@ -1,0 +1,212 @@
+// Rotary positions, by themselves and on the way into the cache pages.
+//
+// Column pairs (a, b) of a query or key row turn by an angle that grows with
+// the row's position: with theta = position * inv_freq,
+//   a' = a cos(theta) - b sin(theta),   b' = b cos(theta) + a sin(theta).
+// The pairs are columns (j, j + R/2) of each rotated run of R columns, or the
+// neighbours (2j, 2j + 1); each frequency reads the position of its own axis
+// (time, height, width of an image patch); columns past R and V rows are
+// copied bit for bit.
+//
+// Angles.  theta is needed modulo one turn, and far positions make it large:
+// 131071 * 1 rad in fp32 is off by up to 2^-8 rad.  The host turns each
+// frequency into turns per position in fp64, the kernel multiplies by the
+// position, takes off the whole turns in fp64 (off by at most 2^-53 of the
+// turns, 2^-22 turns at the largest position there is) and only the rest
+// becomes fp32; sine and cosine of it are those of sincospif.  The rotation is
+// fp32, rounded once to the storage type.
+//
+// One launch moves q, K and V of a token: a workgroup holds a few tokens by
+// eight heads; a lane keeps the sines and cosines of eight frequencies in
+// registers and goes through the heads in steps of eight, so they are formed
+// once per token and lane, not once per row.  Bound by HBM (by the launch for a
+// decoding step).
+#include <algorithm>
+
+#include "kvt_device.h"
+#include "kvt_internal.h"
+
+namespace kvt {
+namespace {
+
+using namespace dev;
+
+constexpr int kThreads = 256;
+constexpr int kHeadLanes = 8;   // heads that a workgroup holds at a time
+constexpr int kAhead = 2;       // heads per lane whose loads are in flight together
+
+// Eight consecutive elements of a row, as stored.
+template <typename T>
+struct Piece {
+  u32x4 w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Piece<T> load_piece(const T* p) {
+  Piece<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+    r.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, const Piece<T>& x) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(p)[i] = x.w[i];
+}
+__device__ __forceinline__ void widen(const Piece<__bf16>& x, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __builtin_bit_cast(float, x.w[0][i] << 16);
+    f[2 * i + 1] = __builtin_bit_cast(float, x.w[0][i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen(const Piece<float>& x, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const unsigned u = x.w[i / 4][i % 4];
+    f[i] = __builtin_bit_cast(float, u);
+  }
+}
+__device__ __forceinline__ void narrow(const float (&f)[8], Piece<__bf16>& x) {
+  x.w[0] = round8((f32x4){f[0], f[1], f[2], f[3]}, (f32x4){f[4], f[5], f[6], f[7]});
+}
+__device__ __forceinline__ void narrow(const float (&f)[8], Piece<float>& x) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x.w[i / 4][i % 4] = __builtin_bit_cast(unsigned, f[i]);
+}
+
+// A lane's pieces of a row: two runs of eight columns, first and second.  In a
+// rotated run of R columns they are R/2 apart, so that eight columns of the one
+// are the partners of eight of the other (split pairs) or both hold whole pairs
+// (neighbours); either way consecutive lanes read consecutive bytes.
+template <typename T, int D, bool PAIRS>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
+  constexpr int SLOTS = D / 16;                            // lanes per row
+  constexpr int TOKENS = kThreads / (SLOTS * kHeadLanes);  // tokens per workgroup
+  const int slot = threadIdx.x % SLOTS;
+  const int hl = threadIdx.x / SLOTS % kHeadLanes;
+  const int64_t r = (int64_t)blockIdx.x * TOKENS + threadIdx.x / (SLOTS * kHeadLanes);   // launch-local row
+  if (r >= a.rows) return;
+  const int64_t row = a.row_begin + r;                     // packed row of the call
+  const int hq = a.num_q_heads, hkv = a.num_kv_heads;
+  const int jobs = hq + 2 * hkv;                           // q rows, K rows, V rows of one token
+
+  // ---- where the token's K/V go, and its position
+  int64_t page_row = -1;    // row of (page, head 0, slot) in the pools, -1: nowhere
+  int32_t logical = 0;
+  if (hkv > 0) {
+    int lo = 0, hi = a.nseq - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.seq[mid].row_off <= row) lo = mid;
+      else hi = mid - 1;
+    }
+    const SeqDesc sd = a.seq[lo];
+    logical = sd.prefix + (int32_t)(row - sd.row_off);
+    const int32_t bid = a.block_table[(int64_t)sd.seq * a.max_blocks + logical / kBlock];
+    if (bid >= 0 && (int64_t)bid < a.num_blocks) page_row = (int64_t)bid * hkv * kBlock + logical % kBlock;
+  }
+
+  // ---- the lane's columns of a rotated row, and its sines and cosines
+  const int width = D / a.parts, rot = a.rot_dim;
+  const int part = slot / (width / 16), u = slot % (width / 16);
+  const bool turns = u < rot / 16;
+  const int col0 = part * width + (turns ? 8 * u : rot + 8 * (u - rot / 16));
+  const int col1 = col0 + (turns ? rot : width - rot) / 2;
+  float cs[8], sn[8];
+  if (turns) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // split pairs: frequencies 8u .. 8u+7 turn both runs; neighbours: four each
+      const int f = PAIRS ? (i < 4 ? 4 * u + i : rot / 4 + 4 * u + i - 4) : 8 * u + i;
+      const int32_t pos = a.positions ? a.positions[(int64_t)a.axis[f] * a.total_rows + row] : logical;
+      double t = (double)pos * a.turns[f];
+      t -= __builtin_rint(t);
+      sincospif(2.0f * (float)t, &sn[i], &cs[i]);
+    }
+  }
+
+  // ---- the token's rows, kAhead of this lane's at a time
+  const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_stride;
+  const T* k = reinterpret_cast<const T*>(a.k_new) + row * a.k_stride;
+  const T* v = reinterpret_cast<const T*>(a.v_new) + row * a.v_stride;
+  T* qo = reinterpret_cast<T*>(a.q_out) + row * a.q_out_stride;
+  const int step = kHeadLanes * gridDim.y;
+  for (int j0 = hl + kHeadLanes * blockIdx.y; j0 < jobs; j0 += step * kAhead) {
+    Piece<T> p0[kAhead], p1[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int j = j0 + i * step;
+      if (j >= jobs) break;
+      const bool is_v = j >= hq + hkv;
+      const T* src = j < hq ? q + (int64_t)j * D : is_v ? v + (int64_t)(j - hq - hkv) * D : k + (int64_t)(j - hq) * D;
+      p0[i] = load_piece(src + (is_v ? 8 * slot : col0));
+      p1[i] = load_piece(src + (is_v ? 8 * slot + D / 2 : col1));
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int j = j0 + i * step;
+      if (j >= jobs) break;
+      const bool is_v = j >= hq + hkv;
+      if (turns && !is_v) {
+        float x[8], y[8];
+        widen(p0[i], x);
+        widen(p1[i], y);
+        if constexpr (PAIRS) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float c0 = cs[e / 2], s0 = sn[e / 2], c1 = cs[4 + e / 2], s1 = sn[4 + e / 2];
+            const float x0 = x[e], x1 = x[e + 1], y0 = y[e], y1 = y[e + 1];
+            x[e] = x0 * c0 - x1 * s0;
+            x[e + 1] = x1 * c0 + x0 * s0;
+            y[e] = y0 * c1 - y1 * s1;
+            y[e + 1] = y1 * c1 + y0 * s1;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x0 = x[e], y0 = y[e];
+            x[e] = x0 * cs[e] - y0 * sn[e];
+            y[e] = y0 * cs[e] + x0 * sn[e];
+          }
+        }
+        narrow(x, p0[i]);
+        narrow(y, p1[i]);
+      }
+      T* dst;
+      if (j < hq) {
+        dst = qo + (int64_t)j * D;
+      } else {
+        if (page_row < 0) continue;   // an id outside the pool is never dereferenced
+        const int64_t at = (page_row + (int64_t)(is_v ? j - hq - hkv : j - hq) * kBlock) * D;
+        dst = reinterpret_cast<T*>(is_v ? a.v_pool : a.k_pool) + at;
+      }
+      store_piece(dst + (is_v ? 8 * slot : col0), p0[i]);
+      store_piece(dst + (is_v ? 8 * slot + D / 2 : col1), p1[i]);
+    }
+  }
+}
+
+template <typename T, int D>
+void launch_as(const RotaryArgs& a, int cus, hipStream_t stream) {
+  constexpr int TOKENS = kThreads / (D / 16 * kHeadLanes);
+  const int64_t tiles = ((int64_t)a.rows + TOKENS - 1) / TOKENS;
+  const int64_t steps = (a.num_q_heads + 2 * (int64_t)a.num_kv_heads + kHeadLanes - 1) / kHeadLanes;
+  // few tokens: the heads are spread over workgroups until there are four per CU
+  const int64_t gy = std::max<int64_t>(1, std::min<int64_t>({steps, (4 * (int64_t)cus + tiles - 1) / tiles, 65535}));
+  const dim3 grid((unsigned)tiles, (unsigned)gy), block(kThreads);
+  if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, D, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((rotary_kernel<T, D, false>), grid, block, 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream) {
+  if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, cus, stream);
+  else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, cus, stream);
+  else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, cus, stream);
+  else launch_as<float, 64>(a, cus, stream);
+  return hipGetLastError();
+}
+
+}  // namespace kvt

@@ -10,6 +10,7 @@ raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -38,11 +39,11 @@ MGR_EXPORTED = ("kvt_mgr_append", "kvt_mgr_begin_request", "kvt_mgr_create", "kv
                 "kvt_mgr_start_prefill", "kvt_mgr_terminate", "kvt_mgr_unpin")
 MGR_OPS = ("spawn", "fork", "append", "one_off", "pin", "unpin", "replace", "remove", "terminate", "begin_request",
            "start_prefill", "prefill_done", "end_request")   # KVT_MGR_OP_* in this order
-EXPORTED = ("kvt_append_kv", "kvt_cascade_extend_attention", "kvt_cascade_extend_attention_ex",
+EXPORTED = ("kvt_append_kv", "kvt_append_kv_rotary", "kvt_cascade_extend_attention", "kvt_cascade_extend_attention_ex",
             "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
             "kvt_copy_blocks",
             "kvt_decode_attention", "kvt_decode_workspace_bytes", "kvt_extend_attention",
-            "kvt_extend_attention_noalloc", "kvt_extend_workspace_bytes", "kvt_last_hip_error",
+            "kvt_extend_attention_noalloc", "kvt_extend_workspace_bytes", "kvt_last_hip_error", "kvt_rotate",
             "kvt_status_str") + MGR_EXPORTED
 CASCADE_AUTO, CASCADE_SHARED_PASS, CASCADE_PLAIN = 0, 1, 2    # kvt_cascade_mode
 KVT_COPY_TO_HOST = 0
@@ -60,6 +61,16 @@ class KvtSeqs(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("prefix_len", ctypes.POINTER(ctypes.c_int32)),
                 ("suffix_len", ctypes.POINTER(ctypes.c_int32)), ("block_table", ctypes.c_void_p),
                 ("block_table_host", ctypes.POINTER(ctypes.c_int32)), ("max_blocks", ctypes.c_int32)]
+
+
+class KvtRotary(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("num_axes", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("parts", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class KvtRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
 
 
 class KvtMgrReport(ctypes.Structure):
@@ -92,6 +103,12 @@ def lib():
         P = ctypes.POINTER
         L.kvt_append_kv.argtypes = [P(KvtPool), P(KvtSeqs), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
         L.kvt_append_kv.restype = ctypes.c_int
+        L.kvt_append_kv_rotary.argtypes = [P(KvtPool), P(KvtSeqs), P(KvtRotary), P(KvtRows), P(KvtRows), P(KvtRows),
+                                           ctypes.c_int32, P(KvtRows), ctypes.c_void_p]
+        L.kvt_append_kv_rotary.restype = ctypes.c_int
+        L.kvt_rotate.argtypes = [P(KvtRotary), P(KvtRows), ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                 ctypes.c_int32, P(KvtRows), ctypes.c_void_p]
+        L.kvt_rotate.restype = ctypes.c_int
         L.kvt_extend_attention.argtypes = [P(KvtPool), P(KvtSeqs), ctypes.c_void_p, ctypes.c_int32, ctypes.c_float,
                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                                            ctypes.c_void_p]
@@ -287,6 +304,155 @@ def append_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len
     st = _native().append(*head, k_new.data_ptr(), v_new.data_ptr(), _stream_handle(k_pool, stream))
     if st != KVT_OK:
         raise KvtError(st, "kvt_append_kv")
+
+
+def _host_values(x, name: str, dtype: str) -> np.ndarray:
+    """A host array of 32-bit values: a torch CPU tensor's or numpy array's own
+    memory where it has the type, a copy of anything else."""
+    if not isinstance(x, np.ndarray) and hasattr(x, "data_ptr"):
+        if x.device.type != "cpu":
+            raise ValueError(f"{name} is read on the host: pass a CPU tensor, an array or a list")
+        x = x.detach().numpy()
+    x = np.asarray(x)
+    if dtype == "int32":
+        if x.dtype.kind not in "iu":
+            raise TypeError(f"{name} must hold integers")
+        if x.size and (int(x.min()) < _I32_MIN or int(x.max()) > _I32_MAX):
+            raise OverflowError(f"{name} outside the int32 range")
+    if x.ndim != 1:
+        raise ValueError(f"{name} must have one dimension")
+    return np.ascontiguousarray(x, dtype=dtype)
+
+
+def _rotary_args(inv_freq, axis, positions, tokens: int, parts: int, interleaved: bool, device) -> tuple:
+    """The arguments of a rotation as ``_kvt_call`` takes them, and the host
+    arrays that they point into."""
+    import torch
+    freq = _host_values(inv_freq, "inv_freq", "float32")
+    ax = None if axis is None else _host_values(axis, "axis", "int32")
+    if ax is not None and ax.size != freq.size:
+        raise ValueError("axis must name one axis for each frequency")
+    axes = 1
+    if positions is not None:
+        if positions.dim() == 1:
+            positions = positions[None]
+        if (positions.dtype != torch.int32 or positions.dim() != 2 or positions.shape[1] != tokens
+                or not positions.is_contiguous() or positions.device != device):
+            raise ValueError(f"positions must be a contiguous int32 [axes][{tokens}] tensor on {device}")
+        axes = positions.shape[0]
+    return (freq.ctypes.data, None if ax is None else ax.ctypes.data,
+            None if positions is None else positions.data_ptr(), axes, 2 * freq.size, int(parts),
+            int(bool(interleaved))), (freq, ax)
+
+
+def _rows_of(t, name: str, tokens: int, heads: Optional[int], d: int, dtype, device) -> tuple:
+    """(address, token stride) of a [tokens][heads][d] tensor whose tokens may lie apart."""
+    shape = t.shape
+    if (t.dtype != dtype or len(shape) != 3 or shape[0] != tokens or (heads is not None and shape[1] != heads)
+            or shape[2] != d):
+        raise ValueError(f"{name} must be a [{tokens}][{'heads' if heads is None else heads}][{d}] {dtype} tensor, "
+                         f"got {tuple(shape)} {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    packed = shape[1] * d
+    strides = t.stride()
+    if strides[2] != 1 or (shape[1] > 1 and strides[1] != d) or (tokens > 1 and strides[0] < packed):
+        raise ValueError(f"the heads of one token of {name} must be contiguous and its tokens must not overlap")
+    return t.data_ptr(), strides[0] if tokens > 1 else packed
+
+
+def _check_table(block_table, sequences: int, device, *others):
+    """A table row for every sequence, everything on one device."""
+    if block_table.shape[0] < sequences:
+        raise ValueError(f"block_table has {block_table.shape[0]} rows for {sequences} sequences")
+    if any(t.device != device for t in (block_table, *others)):
+        raise ValueError(f"every tensor of the call must be on {device}")
+
+
+def _on_device(t):
+    """Makes a tensor's GPU the current one for a launch where it is not."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError("expected GPU tensors")
+    if t.get_device() == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(t.device)
+
+
+def rotate(x, positions, inv_freq, *, axis=None, interleaved: bool = False, parts: int = 1, out=None, stream=None):
+    """Rotary positions of the rows of ``x`` [T][H][D] (``kvt_rotate``).
+
+    ``positions``: int32 [T], or [axes][T] with ``axis`` naming the axis of
+    each frequency; ``inv_freq``: R/2 host values, radians per position.  The
+    first R columns of each of ``parts`` equal parts of a head are rotated, in
+    pairs (j, j + R/2), or (2j, 2j + 1) if ``interleaved``.  The tokens of ``x``
+    and ``out`` may lie apart (views of a fused projection); ``out`` may be ``x``.
+    Returns ``out``.
+    """
+    import torch
+    if stream is not None:   # out is allocated for the stream that it is written on
+        with torch.cuda.stream(stream):
+            return rotate(x, positions, inv_freq, axis=axis, interleaved=interleaved, parts=parts, out=out)
+    if x.dim() != 3:
+        raise ValueError("x must be [T][H][D]")
+    T, H, d = x.shape
+    if positions is None:
+        raise ValueError("rotate needs positions")
+    rotary, keep = _rotary_args(inv_freq, axis, positions, T, parts, interleaved, x.device)
+    rows = _rows_of(x, "x", T, H, d, x.dtype, x.device)
+    code = _dtype_code(x)
+    with _on_device(x):
+        if out is None:
+            out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
+        to = _rows_of(out, "out", T, H, d, x.dtype, x.device)
+        st = _native().rotate(lib().address["kvt_rotate"], *rotary, *rows, T, H, d, code, *to, _stream_handle(x))
+    del keep
+    if st != KVT_OK:
+        raise KvtError(st, "kvt_rotate")
+    return out
+
+
+def append_kv_rotary(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], k_new, v_new,
+                     inv_freq, *, axis=None, interleaved: bool = False, parts: int = 1, positions=None, q=None,
+                     q_out=None, stream=None, checked: bool = False):
+    """``append_kv`` with rotary positions applied to K on the way, and to ``q``
+    in the same launch (``kvt_append_kv_rotary``).
+
+    The rotation's arguments are those of ``rotate``; without ``positions`` the
+    logical ones (``prefix_len[b]`` + t) are used.  The tokens of ``k_new``,
+    ``v_new``, ``q`` and ``q_out`` may lie apart (views of a fused projection);
+    ``q_out`` may be ``q``.  Returns the rotated q (None without ``q``).
+    """
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return append_kv_rotary(k_pool, v_pool, block_table, prefix_len, suffix_len, k_new, v_new, inv_freq,
+                                    axis=axis, interleaved=interleaved, parts=parts, positions=positions, q=q,
+                                    q_out=q_out, checked=checked)
+    pool = _pool_args(k_pool, v_pool)
+    hkv, d, dtype, device = pool[3], pool[4], k_pool.dtype, k_pool.device
+    head, T = _head("kvt_append_kv_rotary", pool, prefix_len, suffix_len, block_table, checked)
+    _check_table(block_table, head[8], device, v_pool)
+    rotary, keep = _rotary_args(inv_freq, axis, positions, T, parts, interleaved, device)
+    k_rows = _rows_of(k_new, "k_new", T, hkv, d, dtype, device)
+    v_rows = _rows_of(v_new, "v_new", T, hkv, d, dtype, device)
+    q_rows = to = (None, 0)
+    hq = 0
+    if q is not None:
+        q_rows = _rows_of(q, "q", T, None, d, dtype, device)
+        hq = q.shape[1]
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    with _on_device(k_pool):
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty((T, hq, d), dtype=dtype, device=device)
+            to = _rows_of(q_out, "q_out", T, hq, d, dtype, device)
+        st = _native().append_rotary(*head, *rotary, *k_rows, *v_rows, *q_rows, hq, *to, _stream_handle(k_pool))
+    del keep
+    if st != KVT_OK:
+        raise KvtError(st, "kvt_append_kv_rotary")
+    return q_out
 
 
 def extend_workspace_bytes(k_pool, v_pool, block_table, prefix_len, suffix_len, num_q_heads: int) -> int:
