@@ -316,6 +316,73 @@ kvt_status kvt_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
  * arguments are invalid.  Host-only; enqueues nothing. */
 size_t kvt_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
 
+/* What differential attention adds to an attention call.  lambda: device
+ * floats, the weight of the second map of head h of packed token row t at
+ * lambda[t * lambda_stride + h]; lambda_stride 0 gives every token the same
+ * Hq weights, otherwise it is at least num_q_heads.  norm_weight: device float
+ * [head_dim], 16-byte aligned, or NULL for no norm; eps: finite and > 0 (read
+ * with a norm only); out_scale: finite. */
+typedef struct {
+  const float* lambda;
+  int64_t      lambda_stride;
+  const float* norm_weight;
+  float        eps;
+  float        out_scale;
+} kvt_diff;
+
+/*
+ * kvt_diff_extend_attention -- differential attention of the new tokens over
+ * prefix + suffix.
+ *
+ * Every head's columns hold two maps of d = head_dim/2: with q_m, K_m the
+ * columns m*d .. m*d + d - 1, for every b, new token i < S_b, query head h
+ * (g = h / (Hq/Hkv)), j = 0 .. P_b + i:
+ *   A_m = softmax_j(scale * <q_m[off_b+i][h], K_b,m[j]>),   m = 0, 1
+ *   y   = sum_j (A_0[j] - lambda A_1[j]) V_b[j]
+ *   out[off_b+i][h] = out_scale * norm_weight * y / sqrt(mean(y^2) + eps)
+ * or out_scale * y without norm_weight.  K_b/V_b are read through the block
+ * table from pools that kvt_append_kv or kvt_append_kv_rotary (parts = 2)
+ * filled; scale is usually 1/sqrt(d).  Each row's own position is visible, so
+ * no row is empty.
+ *
+ * bf16 inputs feed bf16 MFMA, the probabilities rounded to bf16 for the value
+ * product; fp32 inputs run fp32 MFMA (unlike the other attention calls, which
+ * round them to bf16: here the difference of two maps would keep that error).
+ * Softmax statistics, accumulation and the norm are fp32.
+ *
+ * Other arguments, alignments and errors as for kvt_extend_attention (there
+ * is no lse: the maps' difference cannot be merged by one).  lambda and
+ * norm_weight may not overlap out, nor the workspace q or out.  workspace:
+ * NULL/0 runs without splitting, otherwise at least
+ * kvt_diff_extend_workspace_bytes() for the same arguments, 16-byte aligned
+ * (else KVT_ERR_WORKSPACE, KVT_ERR_INVALID_ARG; any workspace will do where
+ * that is 0).  Results are bit-reproducible for given arguments.
+ */
+kvt_status kvt_diff_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs,
+                                     const void* q, int32_t num_q_heads, float scale, const kvt_diff* diff,
+                                     void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace that lets kvt_diff_extend_attention split long key ranges over
+ * more workgroups.  0 when no split is planned or the arguments are invalid.
+ * Host-only; enqueues nothing. */
+size_t kvt_diff_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
+
+/*
+ * kvt_diff_decode_attention -- one decoding step of differential attention.
+ *
+ * The same operation with S_b = 1 for every b (else KVT_ERR_INVALID_ARG), built
+ * for batches whose cost is streaming every sequence's K/V once from HBM.  Row
+ * b of q, out and (with a stride) lambda is sequence b.  Any Hq/Hkv.
+ */
+kvt_status kvt_diff_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
+                                     const void* q, int32_t num_q_heads, float scale, const kvt_diff* diff,
+                                     void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace that lets kvt_diff_decode_attention split each sequence's keys
+ * over several workgroups.  0 when no split is planned or the arguments are
+ * invalid.  Host-only; enqueues nothing. */
+size_t kvt_diff_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
+
 /* Direction of kvt_copy_blocks. */
 typedef enum {
   KVT_COPY_TO_HOST = 0,     /* pool pages -> host buffer (offload)  */

@@ -308,6 +308,35 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+// diff_attend(head..., q, num_q_heads, scale, lambda, lambda_stride,
+// norm_weight, eps, out_scale, out, workspace, workspace_bytes, stream) -> status
+PyObject* diff_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  kvt_diff d;
+  void *q, *lambda, *norm, *out, *ws, *stream;
+  int32_t hq;
+  long long stride, ws_bytes;
+  if (!count_is(n, kHead + 12) || !head(a, &h) || !address(a[kHead], &q) || !int32(a[kHead + 1], &hq) ||
+      !address(a[kHead + 3], &lambda) || !integer(a[kHead + 4], &stride) || !address(a[kHead + 5], &norm) ||
+      !address(a[kHead + 8], &out) || !address(a[kHead + 9], &ws) || !integer(a[kHead + 10], &ws_bytes) ||
+      !address(a[kHead + 11], &stream))
+    return nullptr;
+  const double scale = PyFloat_AsDouble(a[kHead + 2]), eps = PyFloat_AsDouble(a[kHead + 6]),
+               out_scale = PyFloat_AsDouble(a[kHead + 7]);
+  if (PyErr_Occurred()) return nullptr;
+  d.lambda = reinterpret_cast<const float*>(lambda);
+  d.lambda_stride = stride;
+  d.norm_weight = reinterpret_cast<const float*>(norm);
+  d.eps = (float)eps;
+  d.out_scale = (float)out_scale;
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_diff_extend_attention)>(h.fn)(&h.pool, &h.seqs, q, hq, (float)scale, &d, out, ws,
+                                                                    (size_t)ws_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f))
 PyMethodDef methods[] = {{"pack", FAST(pack), METH_FASTCALL, nullptr},
                          {"append", FAST(append), METH_FASTCALL, nullptr},
@@ -315,6 +344,7 @@ PyMethodDef methods[] = {{"pack", FAST(pack), METH_FASTCALL, nullptr},
                          {"rotate", FAST(rotate), METH_FASTCALL, nullptr},
                          {"workspace", FAST(workspace), METH_FASTCALL, nullptr},
                          {"attend", FAST(attend), METH_FASTCALL, nullptr},
+                         {"diff_attend", FAST(diff_attend), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvt_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

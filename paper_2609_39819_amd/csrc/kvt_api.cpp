@@ -837,6 +837,218 @@ kvt_status launch_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, const 
   return plan.nsplit > 1 ? combine(a, pool, out, lse, T, num_q_heads, plan.nsplit, plan.heaviest > 0.0, s) : KVT_OK;
 }
 
+// Key splits of a differential attention call: every sequence has its own
+// count, so that long contexts split beside short ones that do not, and the
+// partial rows of the split ones lie one after the other.
+struct DiffPlan {
+  std::vector<int> order;          // sequences, longest key range first
+  std::vector<int32_t> nsplit;     // by sequence
+  std::vector<int32_t> part_row;   // by sequence: first partial row (0 where it is not split)
+  int64_t part_rows = 0;
+  size_t ws_bytes = 0;
+};
+
+size_t diff_o_bytes(const kvt_pool* pool, int64_t part_rows) {
+  return ((size_t)part_rows * 2 * pool->head_dim * sizeof(float) + 255) / 256 * 256;
+}
+
+// Lays out the partial rows of the plan's splits; more than 32-bit row indices
+// hold (terabytes of them) runs unsplit.
+void diff_layout(DiffPlan* p, const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
+  const int B = seqs->num_seqs;
+  p->part_row.assign(B, 0);
+  p->part_rows = 0;
+  for (int b = 0; b < B; ++b) {
+    if (p->nsplit[b] == 1) continue;
+    p->part_row[b] = (int32_t)p->part_rows;
+    p->part_rows += (int64_t)p->nsplit[b] * seqs->suffix_len[b] * num_q_heads;
+    if (p->part_rows > INT32_MAX) {
+      p->nsplit.assign(B, 1);
+      p->part_row.assign(B, 0);
+      p->part_rows = 0;
+      break;
+    }
+  }
+  p->ws_bytes = p->part_rows > 0 ? diff_o_bytes(pool, p->part_rows) + (size_t)p->part_rows * 4 * sizeof(float) : 0;
+}
+
+// The splits of a differential extend call.  Every sequence's keys are cut into
+// chunks of about equal length, the longest one's range divided by k, for a
+// range of k; each k is charged the finish of its units (list scheduling, longest
+// first, one XCD's eighth of the units on its CUs; with many sequences the work
+// spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and a launch.
+// The best k is taken if it beats no split by more than 5 %.
+int diff_row_tiles(int32_t suffix, int group) {
+  return (int)(((int64_t)suffix * group + kvt::kDiffTileRows - 1) / kvt::kDiffTileRows);
+}
+DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
+  DiffPlan p;
+  const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
+  const int cus = device_cus(), KT = 64;
+  p.order = longest_first(seqs);
+  p.nsplit.assign(B, 1);
+  const double tile_us = (pool->dtype == KVT_DTYPE_BF16 ? 1.0 : 11.0) * pool->head_dim / 128;
+  std::vector<int64_t> jobs(B), kt(B);
+  for (int i = 0; i < B; ++i) {
+    const int b = p.order[i];
+    jobs[i] = (int64_t)diff_row_tiles(seqs->suffix_len[b], G) * H;
+    kt[i] = ((int64_t)seqs->prefix_len[b] + seqs->suffix_len[b] + KT - 1) / KT;
+  }
+  constexpr int kXcds = 8, kListed = 32;
+  const int xcd_cus = std::max(1, cus / kXcds);
+  auto splits = [&](int i, int64_t chunk) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kvt::kMaxPartials, (kt[i] + chunk - 1) / chunk));
+  };
+  auto cost = [&](int64_t chunk) {
+    double span = 0.0, work = 0.0, longest = 0.0, rows = 0.0;
+    FreeTimes free_at(0.0, xcd_cus, 0.0, 0);
+    for (int i = 0; i < B; ++i) {
+      const int ns = splits(i, chunk);
+      const double len = std::ceil((double)kt[i] / ns) + kUnitTiles;
+      if (B <= kListed) span = std::max(span, free_at.run((jobs[i] * ns + kXcds - 1) / kXcds, len));
+      work += (double)jobs[i] * ns * len;
+      longest = std::max(longest, len);
+      if (ns > 1) rows += (double)ns * seqs->suffix_len[p.order[i]] * num_q_heads;
+    }
+    if (B > kListed) span = std::max(longest, work / cus + 0.5 * longest);
+    return span + (rows > 0 ? (4.0 + 2.0 * rows * 2 * pool->head_dim * 4 / 4.5e6) / tile_us : 0.0);
+  };
+  int64_t best = kt[0];
+  double best_cost = 0.95 * cost(kt[0]);
+  for (int k : {2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64}) {
+    if (k > kt[0]) break;
+    const int64_t chunk = (kt[0] + k - 1) / k;
+    const double c = cost(chunk);
+    if (c < best_cost - 1e-9) best = chunk, best_cost = c;
+  }
+  for (int i = 0; i < B; ++i) p.nsplit[p.order[i]] = best == kt[0] ? 1 : splits(i, best);
+  diff_layout(&p, pool, seqs, num_q_heads);
+  return p;
+}
+
+// The splits of a differential decoding step: chunks that give every CU four
+// units in all, at least 256 keys each.
+DiffPlan diff_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
+  DiffPlan p;
+  const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
+  const int64_t heads = (int64_t)pool->num_kv_heads * ((G + kvt::kDiffDecHeads - 1) / kvt::kDiffDecHeads);
+  p.order = longest_first(seqs);
+  p.nsplit.assign(B, 1);
+  const int64_t units = 4 * (int64_t)device_cus();
+  const int64_t chunk = std::max<int64_t>(256, (total_keys(seqs) * heads + units - 1) / units);
+  for (int b = 0; b < B; ++b)
+    p.nsplit[b] = (int)std::max<int64_t>(
+        1, std::min<int64_t>(kvt::kMaxPartials, ((int64_t)seqs->prefix_len[b] + 1 + chunk / 2) / chunk));
+  diff_layout(&p, pool, seqs, num_q_heads);
+  return p;
+}
+
+// The checks of both differential attention calls; fills the total token count.
+kvt_status check_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
+                      const kvt_diff* diff, const void* out, int64_t* T) {
+  kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, nullptr, T);
+  if (st != KVT_OK) return st;
+  if (diff == nullptr || diff->lambda == nullptr || ((uintptr_t)diff->lambda & 3) != 0) return KVT_ERR_INVALID_ARG;
+  if (diff->lambda_stride != 0 &&
+      (diff->lambda_stride < num_q_heads || diff->lambda_stride > INT64_MAX / 8 / *T))
+    return KVT_ERR_INVALID_ARG;
+  if (!std::isfinite(diff->out_scale)) return KVT_ERR_INVALID_ARG;
+  const size_t out_bytes = (size_t)*T * num_q_heads * pool->head_dim * elem_bytes(pool->dtype);
+  const size_t lambda_bytes = ((size_t)(*T - 1) * diff->lambda_stride + num_q_heads) * sizeof(float);
+  if (overlaps(out, out_bytes, diff->lambda, lambda_bytes)) return KVT_ERR_INVALID_ARG;
+  if (diff->norm_weight != nullptr) {
+    if (!aligned16(diff->norm_weight) || !(diff->eps > 0.f) || !std::isfinite(diff->eps)) return KVT_ERR_INVALID_ARG;
+    if (overlaps(out, out_bytes, diff->norm_weight, pool->head_dim * sizeof(float))) return KVT_ERR_INVALID_ARG;
+  }
+  return KVT_OK;
+}
+
+// Launches of one differential attention call: the units of every sequence,
+// then the join of those that are split.
+kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
+                       const kvt_diff* diff, void* out, int64_t T, DiffPlan& plan, bool decode, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
+  if (plan.ws_bytes > 0) {
+    if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
+      plan.nsplit.assign(B, 1);
+      plan.ws_bytes = 0;
+    } else {
+      if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
+      if (!aligned16(workspace)) return KVT_ERR_INVALID_ARG;
+      const size_t io = (size_t)T * num_q_heads * pool->head_dim * elem_bytes(pool->dtype);
+      if (overlaps(workspace, plan.ws_bytes, q, io) || overlaps(workspace, plan.ws_bytes, out, io))
+        return KVT_ERR_INVALID_ARG;
+    }
+  }
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  std::vector<int32_t> row_off(B + 1, 0);
+  for (int b = 0; b < B; ++b) row_off[b + 1] = row_off[b] + seqs->suffix_len[b];
+  kvt::DiffArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.out = out;
+  a.lambda = diff->lambda;
+  a.lambda_stride = diff->lambda_stride;
+  a.norm_weight = diff->norm_weight;
+  a.eps = diff->eps;
+  a.out_scale = diff->out_scale;
+  a.block_table = seqs->block_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.group = G;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  if (plan.ws_bytes > 0) {
+    a.part_o = reinterpret_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + diff_o_bytes(pool, plan.part_rows));
+  }
+  auto describe = [&](int i, int b) {
+    a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
+    a.nsplit[i] = (uint8_t)plan.nsplit[b];
+    a.part_row[i] = plan.part_row[b];
+  };
+  const int64_t per_unit = (int64_t)pool->num_kv_heads *
+                           (decode ? (G + kvt::kDiffDecHeads - 1) / kvt::kDiffDecHeads : 1);   // workgroups
+  for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
+    int64_t units = 0;
+    for (int i = 0; i < n; ++i) {
+      const int b = plan.order[c0 + i];
+      describe(i, b);
+      a.unit_begin[i] = (int32_t)units;
+      units += (int64_t)(decode ? 1 : diff_row_tiles(seqs->suffix_len[b], G)) * plan.nsplit[b];
+      if (units * per_unit > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    }
+    a.nseq = n;
+    a.unit_begin[n] = (int32_t)units;
+    const int grid = (int)(units * per_unit);
+    const hipError_t e = decode ? kvt::launch_diff_decode(a, pool->dtype, pool->head_dim, grid, s)
+                                : kvt::launch_diff_extend(a, pool->dtype, pool->head_dim, grid, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  for (int c0 = 0; c0 < B && plan.ws_bytes > 0;) {
+    int n = 0;
+    int64_t rows = 0;
+    for (; c0 < B && n < kvt::kSeqsPerLaunch; ++c0) {
+      const int b = plan.order[c0];
+      if (plan.nsplit[b] == 1) continue;
+      describe(n, b);
+      a.unit_begin[n++] = (int32_t)rows;
+      rows += (int64_t)seqs->suffix_len[b] * num_q_heads;
+    }
+    if (n == 0) break;
+    a.nseq = n;
+    a.unit_begin[n] = (int32_t)rows;
+    const hipError_t e = kvt::launch_diff_combine(a, pool->dtype, pool->head_dim, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1238,6 +1450,49 @@ kvt_status kvt_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, cons
     if (e != hipSuccess) return device_error(e);
   }
   return plan.nsplit > 1 ? combine(a, pool, out, lse, T, num_q_heads, plan.nsplit, false, s) : KVT_OK;
+}
+
+size_t kvt_diff_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) try {
+  if (check_pool(pool) != KVT_OK) return 0;
+  int64_t T = 0;
+  if (check_seqs(seqs, &T) != KVT_OK || !heads_ok(pool, num_q_heads, T)) return 0;
+  return diff_extend_plan(pool, seqs, num_q_heads).ws_bytes;
+} catch (const std::bad_alloc&) {
+  return 0;
+}
+
+kvt_status kvt_diff_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                     float scale, const kvt_diff* diff, void* out, void* workspace,
+                                     size_t workspace_bytes, void* stream) try {
+  int64_t T = 0;
+  const kvt_status st = check_diff(pool, seqs, q, num_q_heads, scale, diff, out, &T);
+  if (st != KVT_OK) return st;
+  DiffPlan plan = diff_extend_plan(pool, seqs, num_q_heads);
+  return launch_diff(pool, seqs, q, num_q_heads, scale, diff, out, T, plan, false, workspace, workspace_bytes, stream);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+size_t kvt_diff_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) try {
+  if (check_pool(pool) != KVT_OK) return 0;
+  int64_t T = 0;
+  if (check_seqs(seqs, &T) != KVT_OK || T != seqs->num_seqs || !heads_ok(pool, num_q_heads, T)) return 0;
+  return diff_decode_plan(pool, seqs, num_q_heads).ws_bytes;
+} catch (const std::bad_alloc&) {
+  return 0;
+}
+
+kvt_status kvt_diff_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                     float scale, const kvt_diff* diff, void* out, void* workspace,
+                                     size_t workspace_bytes, void* stream) try {
+  int64_t T = 0;
+  const kvt_status st = check_diff(pool, seqs, q, num_q_heads, scale, diff, out, &T);
+  if (st != KVT_OK) return st;
+  if (T != seqs->num_seqs) return KVT_ERR_INVALID_ARG;   // one new token per sequence
+  DiffPlan plan = diff_decode_plan(pool, seqs, num_q_heads);
+  return launch_diff(pool, seqs, q, num_q_heads, scale, diff, out, T, plan, true, workspace, workspace_bytes, stream);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
 }
 
 }  // extern "C"

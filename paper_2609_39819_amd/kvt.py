@@ -42,7 +42,9 @@ MGR_OPS = ("spawn", "fork", "append", "one_off", "pin", "unpin", "replace", "rem
 EXPORTED = ("kvt_append_kv", "kvt_append_kv_rotary", "kvt_cascade_extend_attention", "kvt_cascade_extend_attention_ex",
             "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
             "kvt_copy_blocks",
-            "kvt_decode_attention", "kvt_decode_workspace_bytes", "kvt_extend_attention",
+            "kvt_decode_attention", "kvt_decode_workspace_bytes", "kvt_diff_decode_attention",
+            "kvt_diff_decode_workspace_bytes", "kvt_diff_extend_attention", "kvt_diff_extend_workspace_bytes",
+            "kvt_extend_attention",
             "kvt_extend_attention_noalloc", "kvt_extend_workspace_bytes", "kvt_last_hip_error", "kvt_rotate",
             "kvt_status_str") + MGR_EXPORTED
 CASCADE_AUTO, CASCADE_SHARED_PASS, CASCADE_PLAIN = 0, 1, 2    # kvt_cascade_mode
@@ -71,6 +73,11 @@ class KvtRotary(ctypes.Structure):
 
 class KvtRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class KvtDiff(ctypes.Structure):
+    _fields_ = [("lambda_", ctypes.c_void_p), ("lambda_stride", ctypes.c_int64), ("norm_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("out_scale", ctypes.c_float)]
 
 
 class KvtMgrReport(ctypes.Structure):
@@ -141,6 +148,16 @@ def lib():
         L.kvt_decode_attention.restype = ctypes.c_int
         L.kvt_decode_workspace_bytes.argtypes = L.kvt_extend_workspace_bytes.argtypes
         L.kvt_decode_workspace_bytes.restype = ctypes.c_size_t
+        L.kvt_diff_extend_attention.argtypes = [P(KvtPool), P(KvtSeqs), ctypes.c_void_p, ctypes.c_int32, ctypes.c_float,
+                                                P(KvtDiff), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                                ctypes.c_void_p]
+        L.kvt_diff_extend_attention.restype = ctypes.c_int
+        L.kvt_diff_extend_workspace_bytes.argtypes = L.kvt_extend_workspace_bytes.argtypes
+        L.kvt_diff_extend_workspace_bytes.restype = ctypes.c_size_t
+        L.kvt_diff_decode_attention.argtypes = L.kvt_diff_extend_attention.argtypes
+        L.kvt_diff_decode_attention.restype = ctypes.c_int
+        L.kvt_diff_decode_workspace_bytes.argtypes = L.kvt_extend_workspace_bytes.argtypes
+        L.kvt_diff_decode_workspace_bytes.restype = ctypes.c_size_t
         M, I64, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
         L.kvt_mgr_create.argtypes, L.kvt_mgr_create.restype = [I64], M
         L.kvt_mgr_destroy.argtypes, L.kvt_mgr_destroy.restype = [M], None
@@ -615,6 +632,100 @@ def _attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, prefix
     if st != KVT_OK:
         raise KvtError(st, entry)
     return (out, lse) if want_lse else out
+
+
+def diff_extend_workspace_bytes(k_pool, v_pool, block_table, prefix_len, suffix_len, num_q_heads: int) -> int:
+    head, _ = _head("kvt_diff_extend_workspace_bytes", _pool_args(k_pool, v_pool), prefix_len, suffix_len,
+                    block_table, False)
+    return _native().workspace(*head, int(num_q_heads))
+
+
+def diff_extend_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], lam,
+                          scale: Optional[float] = None, *, norm_weight=None, eps: float = 1e-5,
+                          out_scale: float = 1.0, out=None, workspace=None, use_workspace: bool = True, stream=None,
+                          checked: bool = False):
+    """Differential attention of the new tokens over prefix + suffix
+    (``kvt_diff_extend_attention``).
+
+    A head's columns hold two maps; with their softmax maps A_0, A_1 the result
+    is (A_0 - lam A_1) V, normalised per head by ``norm_weight`` ([D] float32,
+    RMS with ``eps``; None: not), times ``out_scale``.  ``lam``: float32 [Hq], or
+    [T][Hq] for a weight of its own per token (its tokens may lie apart).
+    ``scale`` defaults to 1/sqrt(D/2).  Returns ``out`` ([T][Hq][D], pool dtype).
+    ``workspace``: a byte tensor of at least ``diff_extend_workspace_bytes``
+    (allocated here when ``use_workspace`` and none is given).
+    """
+    return _diff_attention("kvt_diff_extend_attention", "kvt_diff_extend_workspace_bytes", q, k_pool, v_pool,
+                           block_table, prefix_len, suffix_len, lam, scale, norm_weight, eps, out_scale, out,
+                           workspace, use_workspace, stream, checked)
+
+
+def diff_decode_workspace_bytes(k_pool, v_pool, block_table, prefix_len, num_q_heads: int) -> int:
+    head, _ = _head("kvt_diff_decode_workspace_bytes", _pool_args(k_pool, v_pool), prefix_len, None, block_table,
+                    False)
+    return _native().workspace(*head, int(num_q_heads))
+
+
+def diff_decode_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], lam,
+                          scale: Optional[float] = None, *, norm_weight=None, eps: float = 1e-5,
+                          out_scale: float = 1.0, out=None, workspace=None, use_workspace: bool = True, stream=None,
+                          checked: bool = False):
+    """One decoding step of differential attention (``kvt_diff_decode_attention``):
+    row b of ``q`` ([B][Hq][D]) is the new token of sequence b at position
+    ``prefix_len[b]``, whose K/V was appended first.  Other arguments as for
+    ``diff_extend_attention``."""
+    return _diff_attention("kvt_diff_decode_attention", "kvt_diff_decode_workspace_bytes", q, k_pool, v_pool,
+                           block_table, prefix_len, None, lam, scale, norm_weight, eps, out_scale, out, workspace,
+                           use_workspace, stream, checked)
+
+
+def _diff_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, prefix_len, suffix_len, lam, scale,
+                    norm_weight, eps, out_scale, out, workspace, use_workspace, stream, checked):
+    import torch
+    if stream is not None:   # what is allocated here belongs to the stream that the kernels run on
+        with torch.cuda.stream(stream):
+            return _diff_attention(entry, ws_entry, q, k_pool, v_pool, block_table, prefix_len, suffix_len, lam, scale,
+                                   norm_weight, eps, out_scale, out, workspace, use_workspace, None, checked)
+    native = _native()
+    pool = _pool_args(k_pool, v_pool)
+    head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
+    Hq, d, device = int(q.shape[1]), pool[4], k_pool.device
+    _check_tokens(q, "q", T, Hq, d, k_pool.dtype)
+    if lam.dtype != torch.float32 or lam.shape not in ((Hq,), (T, Hq)) or (Hq > 1 and lam.stride(-1) != 1):
+        raise ValueError(f"lam must be a float32 [{Hq}] or [{T}][{Hq}] tensor, its heads contiguous")
+    stride = lam.stride(0) if lam.dim() == 2 and T > 1 else 0
+    given = [v_pool, q, lam]
+    if norm_weight is not None:
+        if norm_weight.dtype != torch.float32 or norm_weight.shape != (d,) or not norm_weight.is_contiguous():
+            raise ValueError(f"norm_weight must be a contiguous float32 [{d}] tensor")
+        given.append(norm_weight)
+    if out is not None:
+        _check_tokens(out, "out", T, Hq, d, k_pool.dtype)
+        given.append(out)
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        given.append(workspace)
+    _check_table(block_table, head[8], device, *given)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d // 2)
+    with _on_device(k_pool):
+        if out is None:
+            out = torch.empty_like(q)
+        ws_ptr, ws_bytes = None, 0
+        if workspace is not None:
+            ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        elif use_workspace:
+            ws_bytes = native.workspace(lib().address[ws_entry], *head[1:], Hq)
+            if ws_bytes:
+                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+                ws_ptr = workspace.data_ptr()
+        st = native.diff_attend(*head, q.data_ptr(), Hq, float(scale), lam.data_ptr(), stride,
+                                None if norm_weight is None else norm_weight.data_ptr(), float(eps), float(out_scale),
+                                out.data_ptr(), ws_ptr, ws_bytes, _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, entry)
+    return out
 
 
 # ---------------------------------------------------------------------------
