@@ -11,17 +11,29 @@
 //
 // Work decomposition: one workgroup per (sequence, kv-head, 128 packed query
 // rows, key split), as the extend kernel's (row r = token r/G, head g*G + r%G);
-// 4 waves of 32 rows.  A wave computes both maps of its rows, so each V fragment
-// read from LDS feeds the products of both, and one map's products run beside
-// the other's exponentials.  S^T = K Q^T (keys on the MFMA rows, queries on the
-// columns), so a query's scores sit in one lane pair (l, l+32) and leave the
-// accumulators in the layout that the value product takes them in.
+// 8 waves, two per SIMD: waves 0..3 take the first map of 32 rows each, waves
+// 4..7 the second map of the same rows, on the K/V tiles that all of them share
+// in LDS.  (A wave with both maps reads each V fragment once for two products,
+// but its two outputs leave no registers to read operands ahead: 96/8 heads of
+// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.27 this way; one output
+// of 512 registers' worth per SIMD, both maps, 4.0 ms.)  S^T = K Q^T (keys on the
+// MFMA rows, queries on the columns), so a query's scores sit in one lane pair
+// (l, l+32) and leave the accumulators in the layout that the value product
+// takes them in.  At the end the second map's waves hand their rows over through
+// LDS and the first map's form the difference and the norm; a key split writes
+// both maps' rows as they are, for the joining launch.
 //
 // bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys, probabilities
-// rounded to bf16 for the value product (their sum adds the rounded ones).
-// fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded: the
-// difference of two maps has the error of the larger one, so what bf16 inputs
-// lose anyway fp32 ones would lose here.
+// rounded to bf16 for the value product (their sum adds the rounded ones): the
+// result is off by 2.6e-3 of itself (2-norm), of which its own rounding is 1.7e-3.
+// fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded (the
+// difference of two maps keeps the error of the larger one).
+//
+// What bounds it: the matrix cores and the softmax beside them.  A tile of 64 keys
+// takes 2 x 24 MFMAs of 32 cycles per SIMD (1536) and 2 x 115 other vector
+// instructions (about 1200); with 8 workgroups on the chip it takes 3040 cycles
+// (1.27 us), with all CUs busy 1.45 us at the clock that the board then holds.
+// 2048 new tokens over 131072, 32/8 heads of 128: see the figures at the launch.
 //
 // Masked positions.  Their scores are replaced by -inf, so their weight is
 // exactly 0 whatever K holds; positions past the end of the sequence and unused
@@ -53,11 +65,16 @@ struct Shape {
   static constexpr int CHUNKS = ROWB / 16;
   static constexpr int RPR = 1024 / ROWB;               // key rows per 1 KiB wave load
   static constexpr int DT = D / 32;                     // 32-wide output column tiles
-  // bf16: swz (kvt_device.h).  fp32: a row is a whole number of 256-byte bank
-  // cycles, and 16 keys read the same chunk column at once.
-  static __device__ __forceinline__ int swizzle(int key) {
+  // Chunk swizzles of K and V rows.  bf16: swz (kvt_device.h).  fp32: a row is a
+  // whole number of 256-byte bank cycles; a K read takes one chunk of 16 keys at
+  // once, a V read half a bank cycle of one key and of the fourth after it.
+  static __device__ __forceinline__ int swizzle_k(int key) {
     if constexpr (kBf16) return swz<D>(key);
     else return key & 15;
+  }
+  static __device__ __forceinline__ int swizzle_v(int key) {
+    if constexpr (kBf16) return swz<D>(key);
+    else return (key & 4) << 1;
   }
 };
 
@@ -74,57 +91,61 @@ __device__ __forceinline__ unsigned finite_part(unsigned w) {
   else return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
 }
 
-// One K or V tile; a ring slot is one object holding K then V.
+// One K or V tile.
 template <typename T, int D>
 struct HalfTile {
   T e[Shape<T, D>::KT * D];
 };
-template <typename T, int D>
-struct Slot {
-  HalfTile<T, D>& k;
-  HalfTile<T, D>& v;
-};
 
-// A wave's query rows as the B operand of the score product, a map's half of
-// the columns after the other's.  bf16: fragment kk holds columns 16 kk + 8 hh
-// .. + 7.  fp32: element i of chunk pair kk is column 8 kk + 4 hh + i.
+// A wave's query rows, its map's half of the columns, as the B operand of the
+// score product.  bf16: fragment k holds columns 16 k + 8 hh .. + 7.  fp32:
+// element i of fragment k is column 8 k + 4 hh + i.
 template <typename T, int D>
 struct Queries;
 template <int D>
 struct Queries<__bf16, D> {
-  bf16x8 f[D / 16];
+  bf16x8 f[D / 32];
   __device__ __forceinline__ void load(const __bf16* p, int hh) {
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) f[kk] = __builtin_bit_cast(bf16x8, load8(p + kk * 16 + hh * 8));
+    for (int k = 0; k < D / 32; ++k) f[k] = __builtin_bit_cast(bf16x8, load8(p + k * 16 + hh * 8));
   }
 };
 template <int D>
 struct Queries<float, D> {
-  f32x4 f[D / 8];
+  f32x4 f[D / 16];
   __device__ __forceinline__ void load(const float* p, int hh) {
 #pragma unroll
-    for (int kk = 0; kk < D / 8; ++kk) f[kk] = *reinterpret_cast<const f32x4*>(p + kk * 8 + hh * 4);
+    for (int k = 0; k < D / 16; ++k) f[k] = load4(p + k * 8 + hh * 4);
   }
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 1) void diff_extend_kernel(const DiffArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs a) {
   using S = Shape<T, D>;
   constexpr int KT = S::KT, HALVES = S::HALVES, DT = S::DT, RPR = S::RPR;
   constexpr int PAGES = KT / kBlock;                              // pages per tile
   constexpr int NREG = KT * S::ROWB / 1024 / kDiffWaves;          // 1 KiB loads per wave per tensor
+  constexpr int QK = S::kBf16 ? D / 32 : D / 16;                  // query fragments
+  constexpr int KG = S::kBf16 ? 2 : 16;                           // key groups of the value product over 32 keys
   constexpr float kRescaleSlack = 8.0f;                           // log2 headroom before O is rescaled
-  typedef typename std::conditional<S::kBf16, bf16x8, f32x16>::type Probs;
-  constexpr int NP = S::kBf16 ? KT / 16 : HALVES;                 // probability operands per map
-  __shared__ __attribute__((aligned(1024))) HalfTile<T, D> slot0[2];   // K, V
-  __shared__ __attribute__((aligned(1024))) HalfTile<T, D> slot1[2];
-  const Slot<T, D> tile0{slot0[0], slot0[1]}, tile1{slot1[0], slot1[1]};
+  constexpr float kSumLimit = 65536.0f;                           // a lane's sum of probabilities over 32 keys
+  struct Probs {   // B operands of the value product over 32 keys
+    typename std::conditional<S::kBf16, u32x4, float>::type w[KG];
+  };
+  typedef typename std::conditional<S::kBf16, bf16x8, float>::type VFrag;
+  // rings of two K and two V tiles; distinct objects, so that the compiler can
+  // tell the page gather into one from the operand reads of another
+  __shared__ __attribute__((aligned(1024))) HalfTile<T, D> k0, k1, k2, k3, v0, v1, v2, v3;
+  __shared__ float row_sum[kDiffTileRows];   // of the second map, for the epilogue
+  __shared__ int odd_seen;                   // a non-finite value was found in a tile with masked positions
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int map = wave >> 2, rg = wave & 3;   // this wave's map and 32-row block
   const int hh = lane >> 5;     // lane half
   const int l32 = lane & 31;
+  if (tid == 0) odd_seen = 0;
 
   // ---- which (sequence, kv-head, row tile, key split) this workgroup owns
   const int hkv = a.num_kv_heads;
@@ -150,18 +171,19 @@ __global__ __launch_bounds__(kThreads, 1) void diff_extend_kernel(const DiffArgs
   const int per_split = (ntiles_kv + nsplit - 1) / nsplit;
   const int j0 = split * per_split;
   const int j1 = min(ntiles_kv, j0 + per_split);
-  const int lim_min = P + r0 / G;              // smallest last-visible key of the tile
+  const int n = j1 - j0;                       // tiles (none: a split past the keys)
+  const int masked = max(0, (P + r0 / G + 1) / KT - j0);   // first one with positions that some row does not see
 
   // ---- this lane's query row
-  int r = r0 + wave * 32 + l32;
-  const bool row_valid = r < rows_seq;
-  if (!row_valid) r = rows_seq - 1;
+  const bool idle = r0 + rg * 32 >= rows_seq;  // a wave past the last row only takes part in the gather
+  const int r = min(r0 + rg * 32 + l32, rows_seq - 1);
+  const bool row_valid = r0 + rg * 32 + l32 < rows_seq;
   const int t_row = r / G;
   const int h_row = g * G + (r - t_row * G);
   const int lim = P + t_row;                   // last visible position
   const int64_t qrow = (int64_t)(sd.row_off + t_row) * a.num_q_heads + h_row;
   Queries<T, D> q;
-  q.load(reinterpret_cast<const T*>(a.q) + qrow * D, hh);
+  q.load(reinterpret_cast<const T*>(a.q) + qrow * D + map * (D / 2), hh);
 
   const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const char* vpool = reinterpret_cast<const char*>(a.v_pool);
@@ -171,316 +193,350 @@ __global__ __launch_bounds__(kThreads, 1) void diff_extend_kernel(const DiffArgs
       (const __attribute__((address_space(4))) int32_t*)(a.block_table + (int64_t)sd.seq * a.max_blocks);
   const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
 
-  // ---- gather geometry: wave w, load i covers key rows RPR*(w + 4i) ..
-  // +RPR-1 of the tile, all inside one page.  Lane l lands at LDS byte 16*l of
-  // that 1 KiB run, i.e. row RPR*(w + 4i) + l/CHUNKS, physical chunk l%CHUNKS,
-  // so it fetches logical chunk (l%CHUNKS) ^ swizzle(row).
-  constexpr uint32_t ROWM = S::ROWB - 1;
-  int lds_off[NREG], page_in_tile[NREG];
-  uint32_t lane_off[NREG];                     // this lane's byte offset within its page run
+  // ---- gather geometry: a wave's NREG loads of a tile lie in one page, so it
+  // looks up one page id per tile.  Load i covers key rows RPR*(NREG*w + i) ..
+  // +RPR-1; lane l lands at LDS byte 16*l of that 1 KiB run, i.e. row l/CHUNKS,
+  // physical chunk l%CHUNKS, so it fetches logical chunk (l%CHUNKS) ^ swizzle(row).
+  const int page_in_tile = wave * PAGES / kDiffWaves;
+  uint32_t k_off[NREG], v_off[NREG];           // this lane's byte offset within its page run
 #pragma unroll
   for (int i = 0; i < NREG; ++i) {
-    const int run = wave + kDiffWaves * i;
-    const int keyrow = RPR * run + lane / S::CHUNKS;
-    page_in_tile[i] = (RPR * run) / kBlock;
-    lds_off[i] = run * 1024;                   // bytes
-    lane_off[i] = (uint32_t)((keyrow & (kBlock - 1)) * S::ROWB + (((lane % S::CHUNKS) ^ S::swizzle(keyrow)) << 4));
+    const int key = RPR * (wave * NREG + i) + lane / S::CHUNKS;
+    const int row = (key & (kBlock - 1)) * S::ROWB, chunk = lane % S::CHUNKS;
+    k_off[i] = (uint32_t)(row + ((chunk ^ S::swizzle_k(key)) << 4));
+    v_off[i] = (uint32_t)(row + ((chunk ^ S::swizzle_v(key)) << 4));
   }
-  // page ids as the block table has them, clamped into the pool where they are used
-  auto page_ids = [&](int jn, uint32_t (&ids)[NREG]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NREG; ++i) {
-      const int page = __builtin_amdgcn_readfirstlane(min(jn * PAGES + page_in_tile[i], nblk - 1));
-      ids[i] = (uint32_t)bt[page];
-    }
+  // page id as the block table has it, clamped into the pool where it is used
+  auto page_id = [&](int jn) __attribute__((always_inline)) {
+    return (uint32_t)bt[__builtin_amdgcn_readfirstlane(min(jn * PAGES + page_in_tile, nblk - 1))];
   };
   // positions past the end of the sequence take the last real position's offset
-  const uint32_t tail = (uint32_t)((L - 1) & (kBlock - 1)) * (ROWM + 1);
-  auto gather = [&](int jn, const uint32_t (&ids)[NREG], const Slot<T, D>& dst) __attribute__((always_inline)) {
+  const uint32_t tail = (uint32_t)((L - 1) & (kBlock - 1)) * S::ROWB;
+  auto gather = [&](const char* pool, const uint32_t (&lane_off)[NREG], int jn, uint32_t id, HalfTile<T, D>& dst)
+      __attribute__((always_inline)) {
+    const uint32_t last = jn * PAGES + page_in_tile >= nblk - 1 ? tail : (kBlock - 1) * S::ROWB;
+    const char* base = pool + (((int64_t)min(id, nb_max) * hkv + g) << 4) * S::ROWB;
 #pragma unroll
-    for (int i = 0; i < NREG; ++i) {
-      const uint32_t last = jn * PAGES + page_in_tile[i] >= nblk - 1 ? tail : (kBlock - 1) * (ROWM + 1);
-      const uint32_t lb = min(lane_off[i], last | (lane_off[i] & ROWM));
-      const int64_t base = (((int64_t)min(ids[i], nb_max) * hkv + g) << 4) * S::ROWB;
-      __builtin_amdgcn_global_load_lds((const void*)(kpool + base + lb),
-                                       (__attribute__((address_space(3))) void*)((lds_char*)dst.k.e + lds_off[i]), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((const void*)(vpool + base + lb),
-                                       (__attribute__((address_space(3))) void*)((lds_char*)dst.v.e + lds_off[i]), 16, 0, 0);
-    }
+    for (int i = 0; i < NREG; ++i)
+      __builtin_amdgcn_global_load_lds((const void*)(base + min(lane_off[i], last | (lane_off[i] & (S::ROWB - 1)))),
+                                       (lds_void*)((lds_char*)dst.e + (wave * NREG + i) * 1024), 16, 0, 0);
   };
 
-  f32x16 o[2][DT];
-  float m_ref[2], l_run[2];   // reference max of scale*log2e*score; this lane's share of sum 2^(s*c - m_ref)
+  f32x16 o[DT];
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    m_ref[m] = -INFINITY, l_run[m] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[m][dt] = (f32x16){};
-  }
+  for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16){};
+  float m_ref = -INFINITY, l_run = 0.f;   // reference max of scale*log2e*score; this lane's share of sum 2^(s*c - m_ref)
   const float c = a.scale_log2;
 
-  // ---- S^T = K Q^T of one tile and map
-  auto scores = [&](const Slot<T, D>& tl, int m, f32x16 (&s)[HALVES]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int half = 0; half < HALVES; ++half) s[half] = (f32x16){};
+  // ---- S^T = K Q^T: product k of a 32-key block takes 16 of the map's columns (fp32: 8)
+  auto read_k = [&](const HalfTile<T, D>& tl, int k, int half) __attribute__((always_inline)) {
+    const int chunk = 2 * (map * QK + k) + hh;
+    return reinterpret_cast<const u32x4*>(tl.e)[(half * 32 + l32) * S::CHUNKS + (chunk ^ S::swizzle_k(l32))];
+  };
+  auto score_product = [&](u32x4 kf, int k, f32x16 acc) __attribute__((always_inline)) {
     if constexpr (S::kBf16) {
-#pragma unroll
-      for (int k0 = 0; k0 < D / 32; ++k0) {
-        const int kk = m * (D / 32) + k0;
-        const int off = l32 * D + (((2 * kk + hh) ^ S::swizzle(l32)) << 3);
-#pragma unroll
-        for (int half = 0; half < HALVES; ++half) {
-          const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tl.k.e + off + half * 32 * D));
-          s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q.f[kk], s[half], 0, 0, 0);
-        }
-      }
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), q.f[k], acc, 0, 0, 0);
     } else {
+      const f32x4 k4 = __builtin_bit_cast(f32x4, kf);
 #pragma unroll
-      for (int k0 = 0; k0 < D / 16; ++k0) {
-        const int kk = m * (D / 16) + k0;
-        const int off = l32 * D + (((2 * kk + hh) ^ S::swizzle(l32)) << 2);
-        const f32x4 kf = *reinterpret_cast<const f32x4*>(tl.k.e + off);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], q.f[kk][i], s[0], 0, 0, 0);
-      }
+      for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[i], q.f[k][i], acc, 0, 0, 0);
+      return acc;
     }
   };
-  // ---- causal mask, row max and the reference-max update of one map.  Element
-  // e of block `half` is key j*KT + 32 half + 8 (e/4) + 4 hh + e%4.  The reference
-  // only moves when a tile max passes it by more than the slack; O and l are then
-  // rescaled (rare after the first tiles).
-  auto settle = [&](int j, int m, f32x16 (&s)[HALVES]) __attribute__((always_inline)) {
-    if (j * KT + KT - 1 > lim_min) {
-      const int thr = lim - j * KT - 4 * hh;
+  // ---- causal mask of 32 keys from `first` on.  Element e is key first + 8 (e/4) + 4 hh + e%4.
+  auto mask = [&](int first, f32x16& s) __attribute__((always_inline)) {
+    const int thr = lim - first - 4 * hh;
 #pragma unroll
-      for (int half = 0; half < HALVES; ++half)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (half * 32 + 8 * (e >> 2) + (e & 3) > thr) s[half][e] = -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e)
+      if (8 * (e >> 2) + (e & 3) > thr) s[e] = -INFINITY;
+  };
+  // ---- moves the reference to the row maxima of these scores where they pass it
+  // by more than the slack; returns the factor for what was summed before
+  auto settle = [&](const f32x16& s) __attribute__((always_inline)) {
     float mx = -INFINITY;
 #pragma unroll
-    for (int half = 0; half < HALVES; ++half)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[half][e]);
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
     const float mxc = pair_max(mx) * c;
-    const float m_new = (mxc > m_ref[m] + kRescaleSlack) ? mxc : m_ref[m];
+    const float m_new = (mxc > m_ref + kRescaleSlack) ? mxc : m_ref;
     // 1 when unchanged, 0 when leaving -inf; kept at 1 while the row has seen no visible key
-    const float alpha = (m_new == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(m_ref[m] - m_new);
-    m_ref[m] = m_new;
-    l_run[m] *= alpha;
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[m][dt] *= alpha;
-    }
+    const float alpha = (m_new == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
+    m_ref = m_new;
+    return alpha;
   };
-  // ---- probabilities of a settled tile as the B operands of the value product
-  auto probs = [&](int m, const f32x16 (&s)[HALVES], Probs (&pb)[NP]) __attribute__((always_inline)) {
-    const float m_use = (m_ref[m] == -INFINITY) ? 0.f : m_ref[m];
+  // ---- probabilities of 32 keys as B operands of the value product; returns their sum
+  auto probs = [&](const f32x16& s, Probs& p) __attribute__((always_inline)) {
+    const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
     float rs = 0.f;
-    if constexpr (S::kBf16) {
-      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-      for (int kg = 0; kg < NP; ++kg) {
-        const int half = kg >> 1, b0 = (kg & 1) * 8;
-        u32x4 wv;
-#pragma unroll
-        for (int q2 = 0; q2 < 4; ++q2) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[half][b0 + 2 * q2], c, -m_use));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[half][b0 + 2 * q2 + 1], c, -m_use));
-          const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-          rs = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, rs, false);
-          wv[q2] = __builtin_bit_cast(unsigned, pp);
-        }
-        pb[kg] = __builtin_bit_cast(bf16x8, wv);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        pb[0][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][e], c, -m_use));
-        rs += pb[0][e];
+    for (int i = 0; i < 16; i += 2) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m_use));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, -m_use));
+      if constexpr (S::kBf16) {
+        const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+        rs = __builtin_amdgcn_fdot2_f32_bf16(pp, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, rs, false);
+        p.w[i / 8][i % 8 / 2] = __builtin_bit_cast(unsigned, pp);
+      } else {
+        p.w[i] = p0;
+        p.w[i + 1] = p1;
+        rs += p0 + p1;
       }
     }
-    l_run[m] += rs;
+    return rs;
   };
-  // ---- O^T += V^T P^T of both maps, each V fragment feeding two products
+  // ---- O^T += V^T P^T: product kg takes 16 keys (fp32: keys 8 (kg/4) + kg%4 and the
+  // fourth after it, one per lane half) of 32 columns
   const int g16 = (lane >> 4) & 1, rsel = (lane & 15) >> 2;
-  auto values = [&](const Slot<T, D>& tl, const Probs (&pb)[2][NP]) __attribute__((always_inline)) {
+  auto read_v = [&](const HalfTile<T, D>& tl, int half, int kg, int dt) __attribute__((always_inline)) {
     if constexpr (S::kBf16) {
-      const lds_bf16* vl = (const lds_bf16*)tl.v.e;
+      bf16x4 v[2];
 #pragma unroll
-      for (int kg = 0; kg < NP; ++kg)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          bf16x4 v[2];
-#pragma unroll
-          for (int r2 = 0; r2 < 2; ++r2) {
-            const int key = 8 * r2 + 4 * hh + rsel;          // key within a 16-key group
-            const int dcol = dt * 32 + g16 * 16 + 4 * (lane & 3);
-            const int off = key * D + (((dcol >> 3) ^ S::swizzle(key)) << 3) + (dcol & 7);
-            v[r2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vl + off + kg * 16 * D));
-          }
-          const bf16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-          for (int m = 0; m < 2; ++m) o[m][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[m][kg], o[m][dt], 0, 0, 0);
-        }
-    } else {
-      // product e takes keys 8 (e/4) + e%4 and the fourth after it, one per lane half
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = 8 * (e >> 2) + 4 * hh + (e & 3);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const int col = dt * 32 + l32;
-          const float vf = tl.v.e[key * D + (((col >> 2) ^ S::swizzle(key)) << 2) + (col & 3)];
-#pragma unroll
-          for (int m = 0; m < 2; ++m) o[m][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, pb[m][0][e], o[m][dt], 0, 0, 0);
-        }
+      for (int r2 = 0; r2 < 2; ++r2) {
+        const int key = 8 * r2 + 4 * hh + rsel;          // key within a 16-key group
+        const int dcol = dt * 32 + g16 * 16 + 4 * (lane & 3);
+        const int off = key * D + (((dcol >> 3) ^ S::swizzle_v(key)) << 3) + (dcol & 7);
+        v[r2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)((const lds_bf16*)tl.e + off + (half * 32 + kg * 16) * D));
       }
+      return (VFrag)__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int key = 8 * (kg >> 2) + 4 * hh + (kg & 3), col = dt * 32 + l32;
+      return (VFrag)tl.e[key * D + (((col >> 2) ^ S::swizzle_v(key)) << 2) + (col & 3)];
     }
+  };
+  auto value_product = [&](VFrag vf, const Probs& p, int kg, f32x16 acc) __attribute__((always_inline)) {
+    if constexpr (S::kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p.w[kg]), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p.w[kg], acc, 0, 0, 0);
   };
 
-  // ---- non-finite values in a tile with masked positions (see the top): whether
-  // there is one (workgroup-uniform), ...
-  constexpr int VCHUNKS = KT * S::ROWB / 16 / kThreads;   // 16-byte pieces of a V tile per thread
-  auto odd_values = [&](int j, const Slot<T, D>& tl) __attribute__((always_inline)) {
-    if (j * KT + KT - 1 <= lim_min) return false;
-    const u32x4* p = reinterpret_cast<const u32x4*>(tl.v.e);
+  // ---- non-finite values in a V tile with masked positions (see the top) become
+  // 0 there; any_odd (workgroup-uniform) remembers it
+  bool any_odd = false;
+  constexpr int VPIECES = KT * S::ROWB / 16 / kThreads;   // 16-byte pieces of a tile per thread
+  auto drop_odd = [&](HalfTile<T, D>& tl) __attribute__((always_inline)) {
+    u32x4* p = reinterpret_cast<u32x4*>(tl.e) + tid;
     bool odd = false;
 #pragma unroll
-    for (int i = 0; i < VCHUNKS; ++i) {
-      const u32x4 w = p[tid + kThreads * i];
+    for (int i = 0; i < VPIECES; ++i) {
+      const u32x4 w = p[kThreads * i];
 #pragma unroll
       for (int x = 0; x < 4; ++x) odd = odd || non_finite<T>(w[x]);
     }
-    return __syncthreads_or(odd) != 0;
+    if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) odd_seen = 1;
+    __syncthreads();
+    if (odd_seen == 0) return;
+    any_odd = true;
+#pragma unroll
+    for (int i = 0; i < VPIECES; ++i) {
+      u32x4 w = p[kThreads * i];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[x] = finite_part<T>(w[x]);
+      p[kThreads * i] = w;
+    }
+    __syncthreads();
   };
-  // ... its part in the rows that see it, ...
-  auto add_odd = [&](int j, const Slot<T, D>& tl) __attribute__((always_inline)) {
-    const unsigned* words = reinterpret_cast<const unsigned*>(tl.v.e);
-    constexpr int WORDS = S::ROWB / 4;
-    for (int key = 0; key < KT; ++key) {
+
+  auto score_block = [&](const HalfTile<T, D>& tl, int half, f32x16& s) __attribute__((always_inline)) {
+    s = (f32x16){};
+#pragma unroll
+    for (int k = 0; k < QK; ++k) s = score_product(read_k(tl, k, half), k, s);
+  };
+  auto value_block = [&](const HalfTile<T, D>& tl, int half, const Probs& p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kg = 0; kg < KG; ++kg)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] = value_product(read_v(tl, half, kg, dt), p, kg, o[dt]);
+  };
+  // whether the probabilities p of the scores s hold; rs: their sum.  Where the
+  // reference is not set yet, or some score passed it by far, or is a NaN, they
+  // are done again from the row maxima.
+  auto check = [&](const f32x16& s, Probs& p, float rs) __attribute__((always_inline)) {
+    if (__builtin_amdgcn_ballot_w64(!(rs < kSumLimit) || m_ref == -INFINITY) != 0) {
+      const float alpha = settle(s);
+      rs = probs(s, p);
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+    }
+    l_run += rs;
+  };
+  // bf16, 32 keys: probabilities of `cur` while the matrix cores form the scores of
+  // the next 32 keys and the value product of the 32 before, three streams that
+  // do not depend on each other
+  auto turn = [&](const HalfTile<T, D>& kt, int khalf, const f32x16& cur, f32x16& next, const HalfTile<T, D>& vt, int vhalf,
+                  const Probs& prev, Probs& out) __attribute__((always_inline)) {
+    score_block(kt, khalf, next);
+    value_block(vt, vhalf, prev);
+    const float rs = probs(cur, out);
+    if constexpr (D == 128) {   // operands read ahead, softmax between the products (with heads of 64 the compiler's order is faster)
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+      for (int i = 0; i < QK + KG * DT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+    }
+    check(cur, out, rs);
+  };
+
+  // ---- main loop: step t takes tile t.  K of tile t+3 and V of tile t+2 start to
+  // stream in, each into the slot that the step before was done with (past the
+  // last tile the gather reads clamped, in-bounds pages into slots no one reads);
+  // the wait at the end leaves them in flight and is for those of the step before.
+  // bf16: the scores of a tile's first half come from the step before, and the
+  // value product of its second half is left to the step after.
+  uint32_t id2 = page_id(j0 + 2), id3 = page_id(j0 + 3);   // pages of tiles t+2, t+3
+  f32x16 s0, s1;
+  Probs p0, p1;
+  if (n > 0) {
+    const uint32_t id0 = page_id(j0), id1 = page_id(j0 + 1);
+    gather(kpool, k_off, j0, id0, k0);
+    gather(vpool, v_off, j0, id0, v0);
+    gather(kpool, k_off, j0 + 1, id1, k1);
+    gather(kpool, k_off, j0 + 2, id2, k2);
+    gather(vpool, v_off, j0 + 1, id1, v1);
+  }
+  if constexpr (S::kBf16) {
+    // nothing before the first tile: probabilities and values of 0
+#pragma unroll
+    for (int i = 0; i < KG; ++i) p1.w[i] = (u32x4){0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < VPIECES; ++i) reinterpret_cast<u32x4*>(v3.e)[tid + kThreads * i] = (u32x4){0u, 0u, 0u, 0u};
+  }
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NREG));
+  __syncthreads();
+  if (S::kBf16 && n > 0 && !idle) {
+    score_block(k0, 0, s0);
+    if (masked == 0) mask(j0 * KT, s0);
+    settle(s0);
+  }
+  auto step = [&](int t, const HalfTile<T, D>& k_cur, const HalfTile<T, D>& k_next, const HalfTile<T, D>& v_prev,
+                  HalfTile<T, D>& v_cur, HalfTile<T, D>& k_fill, HalfTile<T, D>& v_fill) __attribute__((always_inline)) {
+    gather(kpool, k_off, j0 + t + 3, id3, k_fill);
+    gather(vpool, v_off, j0 + t + 2, id2, v_fill);
+    id2 = id3, id3 = page_id(j0 + t + 4);
+    if (t >= masked) drop_odd(v_cur);
+    if (!idle) {
+      // asm: a branch where there is something to mask, not selects on every tile
+      if constexpr (S::kBf16) {
+        if (t >= masked) {
+          asm volatile("");
+          mask((j0 + t) * KT, s0);
+        }
+        turn(k_cur, 1, s0, s1, v_prev, 1, p1, p0);
+        if (t >= masked) {
+          asm volatile("");
+          mask((j0 + t) * KT + 32, s1);
+        }
+        turn(k_next, 0, s1, s0, v_cur, 0, p0, p1);
+      } else {
+        score_block(k_cur, 0, s0);
+        if (t >= masked) {
+          asm volatile("");
+          mask((j0 + t) * KT, s0);
+        }
+        check(s0, p0, probs(s0, p0));
+        value_block(v_cur, 0, p0);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NREG));
+    __syncthreads();
+  };
+  for (int t = 0; t < n; t += 4) {
+    step(t, k0, k1, v3, v0, k3, v2);
+    if (t + 1 >= n) break;
+    step(t + 1, k1, k2, v0, v1, k0, v3);
+    if (t + 2 >= n) break;
+    step(t + 2, k2, k3, v1, v2, k1, v0);
+    if (t + 3 >= n) break;
+    step(t + 3, k3, k0, v2, v3, k2, v1);
+  }
+  if (S::kBf16 && n > 0 && !idle) {
+    const HalfTile<T, D>& v_last = (n & 3) == 1 ? v0 : (n & 3) == 2 ? v1 : (n & 3) == 3 ? v2 : v3;
+    value_block(v_last, 1, p1);
+  }
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  // what drop_odd left out: the rows that see such a value get it by hand
+  if (any_odd && !idle) {
+    for (int pos = (j0 + masked) * KT; pos < min(j1 * KT, L); ++pos) {
+      const uint32_t id = min((uint32_t)bt[pos / kBlock], nb_max);
+      const T* vr = reinterpret_cast<const T*>(vpool) + ((((int64_t)id * hkv + g) << 4) + (pos & (kBlock - 1))) * D;
       bool odd = false;
-      for (int w = lane; w < WORDS; w += 64) odd = odd || non_finite<T>(words[key * WORDS + w]);
+      for (int w = lane; w < S::ROWB / 4; w += 64) odd = odd || non_finite<T>(reinterpret_cast<const unsigned*>(vr)[w]);
       if (__builtin_amdgcn_ballot_w64(odd) == 0) continue;
-      const bool seen = j * KT + key <= lim;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          constexpr int PER = 16 / (int)sizeof(T);
-          const int d = dt * 32 + 8 * (e >> 2) + 4 * hh + (e & 3);
-          const float v = (float)tl.v.e[key * D + ((d / PER) ^ S::swizzle(key)) * PER + d % PER];
-          if (seen && !__builtin_isfinite(v))
-#pragma unroll
-            for (int m = 0; m < 2; ++m) o[m][dt][e] += v;
+          const float v = (float)vr[dt * 32 + 8 * (e >> 2) + 4 * hh + (e & 3)];
+          if (pos <= lim && !__builtin_isfinite(v)) o[dt][e] += v;
         }
     }
-  };
-  // ... and its removal from the tile
-  auto clear_odd = [&](const Slot<T, D>& tl) __attribute__((always_inline)) {
-    u32x4* p = reinterpret_cast<u32x4*>(tl.v.e);
-#pragma unroll
-    for (int i = 0; i < VCHUNKS; ++i) {
-      u32x4 w = p[tid + kThreads * i];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) w[x] = finite_part<T>(w[x]);
-      p[tid + kThreads * i] = w;
-    }
-  };
-
-  // ---- main loop: step t computes tile t while tile t+1 streams into the other
-  // slot (past the last tile the gather still reads clamped, in-bounds pages
-  // into a slot no one reads); the wait + barrier publishes tile t+1 and frees
-  // the slot of tile t.
-  const int n = j1 - j0;
-  uint32_t ids[NREG];
-  page_ids(j0, ids);
-  if (n > 0) gather(j0, ids, tile0);
-  page_ids(j0 + 1, ids);
-  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-  __syncthreads();
-  const bool idle = r0 + wave * 32 >= rows_seq;   // a wave past the last row only takes part in the gather
-  auto step = [&](int t, const Slot<T, D>& cur, const Slot<T, D>& fill) __attribute__((always_inline)) {
-    gather(j0 + t + 1, ids, fill);
-    page_ids(j0 + t + 2, ids);
-    const bool odd = odd_values(j0 + t, cur);
-    f32x16 s[2][HALVES];
-    Probs pb[2][NP];
-    if (!idle) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m) scores(cur, m, s[m]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        settle(j0 + t, m, s[m]);
-        probs(m, s[m], pb[m]);
-      }
-    }
-    if (odd) {
-      if (!idle) add_odd(j0 + t, cur);
-      __syncthreads();
-      clear_odd(cur);
-      __syncthreads();
-    }
-    if (!idle) values(cur, pb);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    __syncthreads();
-  };
-  for (int t = 0; t < n; t += 2) {
-    step(t, tile0, tile1);
-    if (t + 1 >= n) break;
-    step(t + 1, tile1, tile0);
   }
 
   // ---- epilogue
-  float l_tot[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) l_tot[m] = pair_sum(l_run[m]);
-  if (nsplit == 1) {
-    const float lam = a.lambda[(int64_t)(sd.row_off + t_row) * a.lambda_stride + h_row];
-    const float inv0 = 1.0f / l_tot[0], inv1 = 1.0f / l_tot[1];
-    float sq = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float y = map_difference(o[0][dt][e], inv0, o[1][dt][e], inv1, lam);
-        o[0][dt][e] = y;
-        sq += y * y;
-      }
-    sq = pair_sum(sq);
+  const float l_tot = pair_sum(l_run);
+  if (nsplit > 1) {
     if (!row_valid) return;
-    float scale = a.out_scale;
-    if (a.norm_weight != nullptr) scale *= 1.0f / __builtin_sqrtf(sq * (1.0f / D) + a.eps);
-    T* op = reinterpret_cast<T*>(a.out) + qrow * D;
+    const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;
+    const int64_t prow = a.part_row[si] + split * rows + (int64_t)t_row * a.num_q_heads + h_row;
+    float* op = a.part_o + (prow * 2 + map) * D;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int d = dt * 32 + 8 * i + 4 * hh;
-        f32x4 w = {1.f, 1.f, 1.f, 1.f};
-        if (a.norm_weight != nullptr) w = load4(a.norm_weight + d);
-        store4(op + d, o[0][dt][4 * i] * scale * w[0], o[0][dt][4 * i + 1] * scale * w[1],
-               o[0][dt][4 * i + 2] * scale * w[2], o[0][dt][4 * i + 3] * scale * w[3]);
+        store4(op + d, o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]);
       }
-  } else {
-    if (!row_valid) return;
-    const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;
-    const int64_t prow = a.part_row[si] + split * rows + (int64_t)t_row * a.num_q_heads + h_row;
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      float* op = a.part_o + (prow * 2 + m) * D;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int d = dt * 32 + 8 * i + 4 * hh;
-          store4(op + d, o[m][dt][4 * i], o[m][dt][4 * i + 1], o[m][dt][4 * i + 2], o[m][dt][4 * i + 3]);
-        }
-    }
-    if (hh == 0)
-      *reinterpret_cast<f32x4*>(a.part_ml + prow * 4) = (f32x4){m_ref[0], l_tot[0], m_ref[1], l_tot[1]};
+    if (hh == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 4 + 2 * map) = (f32x2){m_ref, l_tot};
+    return;
   }
+  // the second map's waves hand their rows over through the rings, a block per
+  // ring slot, the 16-byte pieces of a row XOR-swizzled
+  static_assert(sizeof(HalfTile<T, D>) >= 32 * D * sizeof(float), "hand-over buffer");
+  constexpr int Q4 = D / 4;
+  f32x4* hand = reinterpret_cast<f32x4*>(rg == 0 ? k0.e : rg == 1 ? k1.e : rg == 2 ? v0.e : v1.e) + l32 * Q4;
+  __syncthreads();   // the last value products have read the rings
+  if (map == 1) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        hand[(dt * 8 + 2 * i + hh) ^ (l32 & (Q4 - 1))] =
+            (f32x4){o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    if (hh == 0) row_sum[rg * 32 + l32] = l_tot;
+  }
+  __syncthreads();
+  if (map == 1) return;
+  const float lam = a.lambda[(int64_t)(sd.row_off + t_row) * a.lambda_stride + h_row];
+  const float inv0 = 1.0f / l_tot, inv1 = 1.0f / row_sum[rg * 32 + l32];
+  float sq = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 o1 = hand[(dt * 8 + 2 * i + hh) ^ (l32 & (Q4 - 1))];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float y = map_difference(o[dt][4 * i + x], inv0, o1[x], inv1, lam);
+        o[dt][4 * i + x] = y;
+        sq += y * y;
+      }
+    }
+  sq = pair_sum(sq);
+  if (!row_valid) return;
+  float scale = a.out_scale;
+  if (a.norm_weight != nullptr) scale *= 1.0f / __builtin_sqrtf(sq * (1.0f / D) + a.eps);
+  T* op = reinterpret_cast<T*>(a.out) + qrow * D;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = dt * 32 + 8 * i + 4 * hh;
+      f32x4 w = {1.f, 1.f, 1.f, 1.f};
+      if (a.norm_weight != nullptr) w = load4(a.norm_weight + d);
+      store4(op + d, o[dt][4 * i] * scale * w[0], o[dt][4 * i + 1] * scale * w[1], o[dt][4 * i + 2] * scale * w[2],
+             o[dt][4 * i + 3] * scale * w[3]);
+    }
 }
 
 // Joins the key splits of each row (fixed order): with m* = max_s m_s and

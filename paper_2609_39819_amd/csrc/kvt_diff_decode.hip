@@ -54,9 +54,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5;
   const int l32 = lane & 31;
-  auto swizzle = [](int key) __attribute__((always_inline)) {
+  // chunk swizzles of K and V rows, as the extend kernel's
+  auto swizzle_k = [](int key) __attribute__((always_inline)) {
     if constexpr (kBf16) return swz<D>(key);
     else return key & 15;
+  };
+  auto swizzle_v = [](int key) __attribute__((always_inline)) {
+    if constexpr (kBf16) return swz<D>(key);
+    else return (key & 4) << 1;
   };
 
   // ---- which (sequence, kv-head, key split, head chunk) this workgroup owns
@@ -127,10 +132,12 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
       const int page = min(j * 2 + p, nblk - 1);
       const int key = RPR * i + lane / CHUNKS;
       const int slot = min(key & (kBlock - 1), L - 1 - page * kBlock);
-      const int64_t off = ((((int64_t)ids[p] * hkv + g) << 4) + slot) * D +
-                          ((lane % CHUNKS) ^ swizzle(key)) * (16 / (int)sizeof(T));
-      st.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kpool + off));
-      st.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vpool + off));
+      const int64_t off = ((((int64_t)ids[p] * hkv + g) << 4) + slot) * D;
+      constexpr int PER = 16 / (int)sizeof(T);
+      const T* ks = kpool + off + ((lane % CHUNKS) ^ swizzle_k(key)) * PER;
+      const T* vs = vpool + off + ((lane % CHUNKS) ^ swizzle_v(key)) * PER;
+      st.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ks));
+      st.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vs));
     }
   };
   // (and their values become 0: the last real one may be an infinity, which
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
     f32x16 s = (f32x16){};
 #pragma unroll
     for (int kk = 0; kk < KF; ++kk) {
-      const u32x4 kf = reinterpret_cast<const u32x4*>(sl.k)[l32 * CHUNKS + ((2 * kk + hh) ^ swizzle(l32))];
+      const u32x4 kf = reinterpret_cast<const u32x4*>(sl.k)[l32 * CHUNKS + ((2 * kk + hh) ^ swizzle_k(l32))];
       if constexpr (kBf16) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qreg[kk], s, 0, 0, 0);
       } else {
@@ -210,7 +217,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
           for (int r2 = 0; r2 < 2; ++r2) {
             const int key = 8 * r2 + 4 * hh + rsel;
             const int dcol = dt * 32 + g16 * 16 + 4 * (lane & 3);
-            const int off = key * D + (((dcol >> 3) ^ swizzle(key)) << 3) + (dcol & 7);
+            const int off = key * D + (((dcol >> 3) ^ swizzle_v(key)) << 3) + (dcol & 7);
             v[r2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vl + off + kg * 16 * D));
           }
           const bf16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -227,7 +234,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const int col = dt * 32 + l32;
-          const float vf = sl.v[key * D + (((col >> 2) ^ swizzle(key)) << 2) + (col & 3)];
+          const float vf = sl.v[key * D + (((col >> 2) ^ swizzle_v(key)) << 2) + (col & 3)];
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p, o[dt], 0, 0, 0);
         }
       }

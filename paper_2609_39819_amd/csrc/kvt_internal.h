@@ -27,9 +27,9 @@ constexpr int kDecWaves = 4;
 constexpr int kDecKeysPerTile = 32;
 constexpr int kDecMaxGroup = 32;
 
-// Differential attention tiling: one workgroup = 4 waves x 32 packed query rows.
-constexpr int kDiffWaves = 4;
-constexpr int kDiffTileRows = kDiffWaves * 32;
+// Differential attention tiling: one workgroup = 8 waves, two maps x 4 blocks of 32 packed query rows.
+constexpr int kDiffWaves = 8;
+constexpr int kDiffTileRows = kDiffWaves / 2 * 32;
 constexpr int kDiffDecHeads = 16;   // decode: query heads per workgroup, two maps each on one 32-row block
 
 struct SeqDesc {
