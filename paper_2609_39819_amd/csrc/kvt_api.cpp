@@ -179,6 +179,19 @@ class FreeTimes {
     }
     return last;
   }
+  // Time in which the CUs get through what they were given, if one of them works
+  // at rate `one` at most and all of them share rate `all`.
+  double drain(double one, double all) const {
+    double t = 0, at = 0;
+    int64_t left = 0;
+    for (size_t i = head_; i < runs_.size(); ++i) left += runs_[i].count;
+    for (size_t i = head_; i < runs_.size(); ++i) {
+      t += (runs_[i].time - at) * std::max(1.0 / one, (double)left / all);
+      at = runs_[i].time;
+      left -= runs_[i].count;
+    }
+    return t;
+  }
 
  private:
   struct Run {
@@ -846,6 +859,7 @@ struct DiffPlan {
   std::vector<int32_t> part_row;   // by sequence: first partial row (0 where it is not split)
   int64_t part_rows = 0;
   size_t ws_bytes = 0;
+  bool one_per_cu = false;         // decode: workgroups that do not share a CU
 };
 
 size_t diff_o_bytes(const kvt_pool* pool, int64_t part_rows) {
@@ -926,19 +940,64 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   return p;
 }
 
-// The splits of a differential decoding step: chunks that give every CU four
-// units in all, at least 256 keys each.
+// The splits of a differential decoding step.  Every sequence is cut into chunks
+// of about equal length (the nearest whole number of them), the chunk being one of
+// a few fractions of a CU's share of all keys.  Each is charged the time in which
+// the CUs, given the units longest first, stream them: one workgroup reads at up
+// to 59 GB/s (heads of 64: 42; fp32: 25), all of them at 6.7 TB/s (fp32: 5.4), a
+// unit's start and end count as 150 KB; and the joining launch, 4.5 us and its
+// partials at 4.5 TB/s.  A cut has to gain 3 %.  Batches whose longest context is
+// under half of a CU's share stay unsplit (192 of 1024..4096 keys).  Per step,
+// unsplit and as chosen, heads of 128: one context of 131072 keys, 96/8 heads,
+// 1126 and 87.5 us; 64 of 1024..16384, 96/8, 276 and 249; 8 of 2000..8000, 32/8,
+// 73.5 and 31; 40 of 8000 (320 units on 256 CUs) 235 and 209.
+//
+// Unlike contexts in long units run one workgroup per CU (one_per_cu): where two
+// share one, the longest get half its rate while the rest still runs (64 of
+// 1024..16384 keys 256 and 249 us, 90 of 2000..32768 672 and 612); with many
+// short units two hide each other's start and end (192 of 1024..4096 269.7 and
+// 275; 100 of 200 keys 19.7 and 27).
 DiffPlan diff_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
   const int64_t heads = (int64_t)pool->num_kv_heads * ((G + kvt::kDiffDecHeads - 1) / kvt::kDiffDecHeads);
   p.order = longest_first(seqs);
   p.nsplit.assign(B, 1);
-  const int64_t units = 4 * (int64_t)device_cus();
-  const int64_t chunk = std::max<int64_t>(256, (total_keys(seqs) * heads + units - 1) / units);
-  for (int b = 0; b < B; ++b)
-    p.nsplit[b] = (int)std::max<int64_t>(
-        1, std::min<int64_t>(kvt::kMaxPartials, ((int64_t)seqs->prefix_len[b] + 1 + chunk / 2) / chunk));
+  const int64_t longest = (int64_t)seqs->prefix_len[p.order.front()] + 1;
+  const int64_t shortest = (int64_t)seqs->prefix_len[p.order.back()] + 1;
+  const int64_t cus = device_cus(), all = total_keys(seqs) * heads;
+  const bool bf16 = pool->dtype == KVT_DTYPE_BF16;
+  auto splits = [&](int b, int64_t chunk) {
+    const int64_t n = ((int64_t)seqs->prefix_len[b] + 1 + chunk / 2) / chunk;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kvt::kMaxPartials, n));
+  };
+  int64_t chunk = 2 * longest;   // unsplit
+  if (2 * longest * cus >= all) {
+    const double key_bytes = 2.0 * pool->head_dim * elem_bytes(pool->dtype);
+    const double one = !bf16 ? 25e3 : pool->head_dim == 64 ? 42e3 : 59e3, every = bf16 ? 6.7e6 : 5.4e6;   // bytes per us
+    auto cost = [&](int64_t c) {
+      FreeTimes cu(0.0, cus, 0.0, 0);
+      double rows = 0;
+      for (int i = 0; i < B; ++i) {
+        const int b = p.order[i], n = splits(b, c);
+        cu.run(n * heads, std::ceil((double)(seqs->prefix_len[b] + 1) / n) * key_bytes + 150e3);
+        if (n > 1) rows += (double)n * num_q_heads;
+      }
+      return cu.drain(one, every) + (rows > 0 ? 4.5 + 2.0 * rows * 2 * pool->head_dim * 4 / 4.5e6 : 0.0);
+    };
+    double best = 0.97 * cost(chunk);
+    for (double f : {0.7, 1.0, 1.5, 2.0, 3.0, 4.0}) {   // units per CU
+      if (B > 32 && f != 1.0 && f != 1.5 && f != 3.0) continue;   // large batches: fewer, for the host's sake
+      const int64_t c = std::max<int64_t>(128, (int64_t)((double)all / (f * (double)cus)));
+      if (splits(p.order.front(), c) == 1) continue;
+      const double t = cost(c);
+      if (t < best) best = t, chunk = c;
+    }
+  }
+  int64_t units = 0;
+  for (int b = 0; b < B; ++b) units += (p.nsplit[b] = splits(b, chunk)) * heads;
+  const int64_t unit = (longest + p.nsplit[p.order.front()] - 1) / p.nsplit[p.order.front()];   // the longest one
+  p.one_per_cu = units > cus && longest > 2 * shortest && all >= 1500 * units && 40 * unit * cus >= 21 * all;
   diff_layout(&p, pool, seqs, num_q_heads);
   return p;
 }
@@ -1026,7 +1085,7 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
     a.nseq = n;
     a.unit_begin[n] = (int32_t)units;
     const int grid = (int)(units * per_unit);
-    const hipError_t e = decode ? kvt::launch_diff_decode(a, pool->dtype, pool->head_dim, grid, s)
+    const hipError_t e = decode ? kvt::launch_diff_decode(a, pool->dtype, pool->head_dim, grid, plan.one_per_cu, s)
                                 : kvt::launch_diff_extend(a, pool->dtype, pool->head_dim, grid, s);
     if (e != hipSuccess) return device_error(e);
   }

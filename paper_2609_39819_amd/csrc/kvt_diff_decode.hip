@@ -333,14 +333,24 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
   }
 }
 
+// One workgroup per CU is asked for by LDS that the kernel does not use: more
+// than half of a CU's 160 KB in all.
+template <typename T, int D>
+void launch_as(const DiffArgs& a, dim3 grid, bool one_per_cu, hipStream_t stream) {
+  constexpr unsigned kUsed = kWaves * sizeof(DecSlot<T, D>), kAlone = 84 * 1024;
+  hipLaunchKernelGGL((diff_decode_kernel<T, D>), grid, dim3(kWaves * 64),
+                     one_per_cu && kAlone > kUsed ? kAlone - kUsed : 0, stream, a);
+}
+
 }  // namespace
 
-hipError_t launch_diff_decode(const DiffArgs& a, int dtype, int head_dim, int grid, hipStream_t stream) {
-  const dim3 g(grid), b(kWaves * 64);
-  if (dtype == 0 && head_dim == 128) hipLaunchKernelGGL((diff_decode_kernel<__bf16, 128>), g, b, 0, stream, a);
-  else if (dtype == 0 && head_dim == 64) hipLaunchKernelGGL((diff_decode_kernel<__bf16, 64>), g, b, 0, stream, a);
-  else if (dtype == 1 && head_dim == 128) hipLaunchKernelGGL((diff_decode_kernel<float, 128>), g, b, 0, stream, a);
-  else hipLaunchKernelGGL((diff_decode_kernel<float, 64>), g, b, 0, stream, a);
+hipError_t launch_diff_decode(const DiffArgs& a, int dtype, int head_dim, int grid, bool one_per_cu,
+                              hipStream_t stream) {
+  const dim3 g(grid);
+  if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, g, one_per_cu, stream);
+  else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, g, one_per_cu, stream);
+  else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, g, one_per_cu, stream);
+  else launch_as<float, 64>(a, g, one_per_cu, stream);
   return hipGetLastError();
 }
 

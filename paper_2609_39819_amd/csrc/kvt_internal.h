@@ -175,7 +175,7 @@ hipError_t launch_extend(const ExtendArgs& a, int dtype, int head_dim, int grid,
 hipError_t launch_combine(const CombineArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_copy_blocks(const CopyArgs& a, int grid, hipStream_t stream);
 hipError_t launch_diff_extend(const DiffArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
-hipError_t launch_diff_decode(const DiffArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
+hipError_t launch_diff_decode(const DiffArgs& a, int dtype, int head_dim, int grid, bool one_per_cu, hipStream_t stream);
 hipError_t launch_diff_combine(const DiffArgs& a, int dtype, int head_dim, hipStream_t stream);
 // Decode: ExtendArgs with suffix 1 per sequence and nsplit units per sequence;
 // per_cu: workgroups that may share a CU (0: as many as fit).
