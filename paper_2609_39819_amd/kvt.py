@@ -323,12 +323,16 @@ def append_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len
         raise KvtError(st, "kvt_append_kv")
 
 
-def _host_values(x, name: str, dtype: str) -> np.ndarray:
-    """A host array of 32-bit values: a torch CPU tensor's or numpy array's own
-    memory where it has the type, a copy of anything else."""
-    if not isinstance(x, np.ndarray) and hasattr(x, "data_ptr"):
+def _host_values(x, name: str, dtype: str):
+    """(address, count, owner) of a host array of 32-bit values: a torch CPU
+    tensor's own memory where it has the type, else a copy of a CPU tensor's, an
+    array's or a list's values."""
+    import torch
+    if isinstance(x, torch.Tensor):
         if x.device.type != "cpu":
             raise ValueError(f"{name} is read on the host: pass a CPU tensor, an array or a list")
+        if x.dim() == 1 and x.is_contiguous() and x.dtype == (torch.int32 if dtype == "int32" else torch.float32):
+            return x.data_ptr(), x.numel(), x
         x = x.detach().numpy()
     x = np.asarray(x)
     if dtype == "int32":
@@ -338,28 +342,31 @@ def _host_values(x, name: str, dtype: str) -> np.ndarray:
             raise OverflowError(f"{name} outside the int32 range")
     if x.ndim != 1:
         raise ValueError(f"{name} must have one dimension")
-    return np.ascontiguousarray(x, dtype=dtype)
+    x = np.ascontiguousarray(x, dtype=dtype)
+    return x.ctypes.data, x.size, x
 
 
 def _rotary_args(inv_freq, axis, positions, tokens: int, parts: int, interleaved: bool, device) -> tuple:
     """The arguments of a rotation as ``_kvt_call`` takes them, and the host
     arrays that they point into."""
     import torch
-    freq = _host_values(inv_freq, "inv_freq", "float32")
-    ax = None if axis is None else _host_values(axis, "axis", "int32")
-    if ax is not None and ax.size != freq.size:
-        raise ValueError("axis must name one axis for each frequency")
-    axes = 1
+    freq, pairs, keep = _host_values(inv_freq, "inv_freq", "float32")
+    ax = None
+    if axis is not None:
+        ax, n, keep_axis = _host_values(axis, "axis", "int32")
+        if n != pairs:
+            raise ValueError("axis must name one axis for each frequency")
+        keep = (keep, keep_axis)
+    at, axes = None, 1
     if positions is not None:
-        if positions.dim() == 1:
-            positions = positions[None]
-        if (positions.dtype != torch.int32 or positions.dim() != 2 or positions.shape[1] != tokens
+        shape = positions.shape
+        if (positions.dtype != torch.int32 or len(shape) not in (1, 2) or shape[-1] != tokens
                 or not positions.is_contiguous() or positions.device != device):
             raise ValueError(f"positions must be a contiguous int32 [axes][{tokens}] tensor on {device}")
-        axes = positions.shape[0]
-    return (freq.ctypes.data, None if ax is None else ax.ctypes.data,
-            None if positions is None else positions.data_ptr(), axes, 2 * freq.size, int(parts),
-            int(bool(interleaved))), (freq, ax)
+        at = positions.data_ptr()
+        if len(shape) == 2:
+            axes = shape[0]
+    return (freq, ax, at, axes, 2 * pairs, int(parts), 1 if interleaved else 0), keep
 
 
 def _rows_of(t, name: str, tokens: int, heads: Optional[int], d: int, dtype, device) -> tuple:
