@@ -109,6 +109,7 @@ struct RotaryArgs {
   int32_t parts;
   int32_t interleaved;
   int32_t nseq;
+  int32_t head_lanes;         // set by the launch: heads that a workgroup holds at a time
   uint8_t axis[64];           // axis of each frequency
   double turns[64];           // turns per position of each frequency
   SeqDesc seq[kSeqsPerLaunch];  // in packed-row order
@@ -170,7 +171,7 @@ struct CopyArgs {
 
 // Launchers (device code files).  Return the launch status.
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, hipStream_t stream);
-hipError_t launch_rotary(const RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream);
+hipError_t launch_rotary(RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream);
 hipError_t launch_extend(const ExtendArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_combine(const CombineArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_copy_blocks(const CopyArgs& a, int grid, hipStream_t stream);

@@ -16,11 +16,13 @@
 // becomes fp32; sine and cosine of it are those of sincospif.  The rotation is
 // fp32, rounded once to the storage type.
 //
-// One launch moves q, K and V of a token: a workgroup holds a few tokens by
-// eight heads; a lane keeps the sines and cosines of eight frequencies in
-// registers and goes through the heads in steps of eight, so they are formed
-// once per token and lane, not once per row.  Bound by HBM (by the launch for a
-// decoding step).
+// One launch moves q, K and V of a token: a workgroup holds a few tokens by up to
+// eight heads.  The lanes of a token form its sines and cosines between them,
+// share them through LDS, keep those of their own columns in registers and go
+// through the heads in steps of eight.  Bound by HBM (by the launch for a
+// decoding step): 24576 tokens on three axes, 24 heads of 128, 45.5 us, 6.6 TB/s
+// (65 us with every lane forming its own sines); 14336 new tokens behind a fused
+// projection, 96/8 heads, 162 us, 5.1 TB/s.
 #include <algorithm>
 
 #include "kvt_device.h"
@@ -32,8 +34,8 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 256;
-constexpr int kHeadLanes = 8;   // heads that a workgroup holds at a time
-constexpr int kAhead = 2;       // heads per lane whose loads are in flight together
+constexpr int kHeadLanes = 8;   // heads that a workgroup holds at a time, at most
+constexpr int kAhead = 4;       // heads per lane whose loads are in flight together
 
 // Eight consecutive elements of a row, as stored.
 template <typename T>
@@ -45,13 +47,21 @@ __device__ __forceinline__ Piece<T> load_piece(const T* p) {
   Piece<T> r;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-    r.w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+    r.w[i] = reinterpret_cast<const u32x4*>(p)[i];
   return r;
 }
+// bf16 pieces go out with the nontemporal policy (24576 tokens of 24 heads of 128:
+// 52.9 us without, 45.5 with); an fp32 piece is two stores that share 32 bytes,
+// which need the cache to join them (8192 tokens of 32/8 heads of 64: 34.4 and
+// 42.4 us).  Loads are ordinary ones (nontemporal: 45.5 -> 50 us).
 template <typename T>
 __device__ __forceinline__ void store_piece(T* p, const Piece<T>& x) {
+  if constexpr (sizeof(T) == 2) {
+    __builtin_nontemporal_store(x.w[0], reinterpret_cast<u32x4*>(p));
+  } else {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u32x4*>(p)[i] = x.w[i];
+    for (int i = 0; i < 2; ++i) reinterpret_cast<u32x4*>(p)[i] = x.w[i];
+  }
 }
 __device__ __forceinline__ void widen(const Piece<__bf16>& x, float (&f)[8]) {
 #pragma unroll
@@ -82,11 +92,14 @@ __device__ __forceinline__ void narrow(const float (&f)[8], Piece<float>& x) {
 template <typename T, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
   constexpr int SLOTS = D / 16;                            // lanes per row
-  constexpr int TOKENS = kThreads / (SLOTS * kHeadLanes);  // tokens per workgroup
+  __shared__ float2 table[kThreads / SLOTS * (D / 2)];     // cosine and sine of (token, frequency)
+  const int hl_count = a.head_lanes;                       // a power of two
   const int slot = threadIdx.x % SLOTS;
-  const int hl = threadIdx.x / SLOTS % kHeadLanes;
-  const int64_t r = (int64_t)blockIdx.x * TOKENS + threadIdx.x / (SLOTS * kHeadLanes);   // launch-local row
-  if (r >= a.rows) return;
+  const int hl = threadIdx.x / SLOTS & (hl_count - 1);
+  const int lanes = SLOTS * hl_count;                      // lanes per token
+  const int token = threadIdx.x / lanes;
+  const int64_t r = min((int64_t)blockIdx.x * (kThreads / lanes) + token, a.rows - 1);   // launch-local row
+  const bool live = (int64_t)blockIdx.x * (kThreads / lanes) + token < a.rows;
   const int64_t row = a.row_begin + r;                     // packed row of the call
   const int hq = a.num_q_heads, hkv = a.num_kv_heads;
   const int jobs = hq + 2 * hkv;                           // q rows, K rows, V rows of one token
@@ -107,8 +120,20 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
     if (bid >= 0 && (int64_t)bid < a.num_blocks) page_row = (int64_t)bid * hkv * kBlock + logical % kBlock;
   }
 
-  // ---- the lane's columns of a rotated row, and its sines and cosines
-  const int width = D / a.parts, rot = a.rot_dim;
+  // ---- the token's sines and cosines
+  const int width = D / a.parts, rot = a.rot_dim, pairs = rot / 2;
+  for (int f = threadIdx.x % lanes; f < pairs; f += lanes) {
+    const int32_t pos = a.positions ? a.positions[(int64_t)a.axis[f] * a.total_rows + row] : logical;
+    double t = (double)pos * a.turns[f];
+    t -= __builtin_rint(t);
+    float sn, cs;
+    sincospif(2.0f * (float)t, &sn, &cs);
+    table[token * pairs + f] = make_float2(cs, sn);
+  }
+  __syncthreads();
+  if (!live) return;
+
+  // ---- the lane's columns of a rotated row, and their sines and cosines
   const int part = slot / (width / 16), u = slot % (width / 16);
   const bool turns = u < rot / 16;
   const int col0 = part * width + (turns ? 8 * u : rot + 8 * (u - rot / 16));
@@ -119,10 +144,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
     for (int i = 0; i < 8; ++i) {
       // split pairs: frequencies 8u .. 8u+7 turn both runs; neighbours: four each
       const int f = PAIRS ? (i < 4 ? 4 * u + i : rot / 4 + 4 * u + i - 4) : 8 * u + i;
-      const int32_t pos = a.positions ? a.positions[(int64_t)a.axis[f] * a.total_rows + row] : logical;
-      double t = (double)pos * a.turns[f];
-      t -= __builtin_rint(t);
-      sincospif(2.0f * (float)t, &sn[i], &cs[i]);
+      const float2 e = table[token * pairs + f];
+      cs[i] = e.x, sn[i] = e.y;
     }
   }
 
@@ -131,8 +154,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
   const T* k = reinterpret_cast<const T*>(a.k_new) + row * a.k_stride;
   const T* v = reinterpret_cast<const T*>(a.v_new) + row * a.v_stride;
   T* qo = reinterpret_cast<T*>(a.q_out) + row * a.q_out_stride;
-  const int step = kHeadLanes * gridDim.y;
-  for (int j0 = hl + kHeadLanes * blockIdx.y; j0 < jobs; j0 += step * kAhead) {
+  const int step = hl_count * gridDim.y;
+  for (int j0 = hl + hl_count * blockIdx.y; j0 < jobs; j0 += step * kAhead) {
     Piece<T> p0[kAhead], p1[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -188,10 +211,12 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
 }
 
 template <typename T, int D>
-void launch_as(const RotaryArgs& a, int cus, hipStream_t stream) {
-  constexpr int TOKENS = kThreads / (D / 16 * kHeadLanes);
-  const int64_t tiles = ((int64_t)a.rows + TOKENS - 1) / TOKENS;
-  const int64_t steps = (a.num_q_heads + 2 * (int64_t)a.num_kv_heads + kHeadLanes - 1) / kHeadLanes;
+void launch_as(RotaryArgs& a, int cus, hipStream_t stream) {
+  const int64_t jobs = a.num_q_heads + 2 * (int64_t)a.num_kv_heads;
+  a.head_lanes = 1;   // no more lanes than there are heads
+  while (a.head_lanes < kHeadLanes && a.head_lanes < jobs) a.head_lanes *= 2;
+  const int64_t tokens = kThreads / (D / 16 * a.head_lanes);
+  const int64_t tiles = (a.rows + tokens - 1) / tokens, steps = (jobs + a.head_lanes - 1) / a.head_lanes;
   // few tokens: the heads are spread over workgroups until there are four per CU
   const int64_t gy = std::max<int64_t>(1, std::min<int64_t>({steps, (4 * (int64_t)cus + tiles - 1) / tiles, 65535}));
   const dim3 grid((unsigned)tiles, (unsigned)gy), block(kThreads);
@@ -201,7 +226,7 @@ void launch_as(const RotaryArgs& a, int cus, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_rotary(const RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream) {
+hipError_t launch_rotary(RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream) {
   if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, cus, stream);
   else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, cus, stream);
   else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, cus, stream);
