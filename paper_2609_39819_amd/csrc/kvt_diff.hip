@@ -360,14 +360,29 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
   };
   // bf16, 32 keys: probabilities of `cur` while the matrix cores form the scores of
   // the next 32 keys and the value product of the 32 before, three streams that
-  // do not depend on each other
+  // do not depend on each other.  Heads of 128 read the K fragments of those scores
+  // in the turn before (kf; kt, khalf is the block of the turn after), so that a
+  // turn's first products have nothing to wait for, and ask for the softmax between
+  // the products: 1.22 us per tile, 1.27 without kf.  With heads of 64, whose scores
+  // take two products, kf and that order cost 5%: kt, khalf is this turn's block.
+  constexpr bool kReadAhead = D == 128;
+  u32x4 kf[QK];
   auto turn = [&](const HalfTile<T, D>& kt, int khalf, const f32x16& cur, f32x16& next, const HalfTile<T, D>& vt, int vhalf,
                   const Probs& prev, Probs& out) __attribute__((always_inline)) {
-    score_block(kt, khalf, next);
+    if constexpr (kReadAhead) {
+      next = (f32x16){};
+#pragma unroll
+      for (int k = 0; k < QK; ++k) next = score_product(kf[k], k, next);
+    } else {
+      score_block(kt, khalf, next);
+    }
     value_block(vt, vhalf, prev);
+    if constexpr (kReadAhead) {
+#pragma unroll
+      for (int k = 0; k < QK; ++k) kf[k] = read_k(kt, k, khalf);
+    }
     const float rs = probs(cur, out);
-    if constexpr (D == 128) {   // operands read ahead, softmax between the products (with heads of 64 the compiler's order is faster)
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+    if constexpr (kReadAhead) {
 #pragma unroll
       for (int i = 0; i < QK + KG * DT; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -408,6 +423,10 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
     score_block(k0, 0, s0);
     if (masked == 0) mask(j0 * KT, s0);
     settle(s0);
+    if constexpr (kReadAhead) {
+#pragma unroll
+      for (int k = 0; k < QK; ++k) kf[k] = read_k(k0, k, 1);
+    }
   }
   auto step = [&](int t, const HalfTile<T, D>& k_cur, const HalfTile<T, D>& k_next, const HalfTile<T, D>& v_prev,
                   HalfTile<T, D>& v_cur, HalfTile<T, D>& k_fill, HalfTile<T, D>& v_fill) __attribute__((always_inline)) {
@@ -422,12 +441,12 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
           asm volatile("");
           mask((j0 + t) * KT, s0);
         }
-        turn(k_cur, 1, s0, s1, v_prev, 1, p1, p0);
+        turn(kReadAhead ? k_next : k_cur, kReadAhead ? 0 : 1, s0, s1, v_prev, 1, p1, p0);
         if (t >= masked) {
           asm volatile("");
           mask((j0 + t) * KT + 32, s1);
         }
-        turn(k_next, 0, s1, s0, v_cur, 0, p0, p1);
+        turn(k_next, kReadAhead ? 1 : 0, s1, s0, v_cur, 0, p0, p1);
       } else {
         score_block(k_cur, 0, s0);
         if (t >= masked) {
