@@ -346,13 +346,15 @@ typedef struct {
  * no row is empty.
  *
  * bf16 inputs feed bf16 MFMA, the probabilities rounded to bf16 for the value
- * product; fp32 inputs run fp32 MFMA (unlike the other attention calls, which
- * round them to bf16: here the difference of two maps would keep that error).
+ * product (kvt_diff_decode_attention: given as the sum of two bf16 numbers);
+ * fp32 inputs run fp32 MFMA (unlike the other attention calls, which round
+ * them to bf16: here the difference of two maps would keep that error).
  * Softmax statistics, accumulation and the norm are fp32.
  *
  * Other arguments, alignments and errors as for kvt_extend_attention (there
  * is no lse: the maps' difference cannot be merged by one).  lambda and
- * norm_weight may not overlap out, nor the workspace q or out.  workspace:
+ * norm_weight may not overlap out, nor the workspace any of q, out, lambda and
+ * norm_weight.  workspace:
  * NULL/0 runs without splitting, otherwise at least
  * kvt_diff_extend_workspace_bytes() for the same arguments, 16-byte aligned
  * (else KVT_ERR_WORKSPACE, KVT_ERR_INVALID_ARG; any workspace will do where

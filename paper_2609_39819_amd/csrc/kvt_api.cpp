@@ -886,22 +886,25 @@ void diff_layout(DiffPlan* p, const kvt_pool* pool, const kvt_seqs* seqs, int32_
   p->ws_bytes = p->part_rows > 0 ? diff_o_bytes(pool, p->part_rows) + (size_t)p->part_rows * 4 * sizeof(float) : 0;
 }
 
+int diff_row_tiles(int32_t suffix, int group) {
+  return (int)(((int64_t)suffix * group + kvt::kDiffTileRows - 1) / kvt::kDiffTileRows);
+}
+
 // The splits of a differential extend call.  Every sequence's keys are cut into
 // chunks of about equal length, the longest one's range divided by k, for a
 // range of k; each k is charged the finish of its units (list scheduling, longest
 // first, one XCD's eighth of the units on its CUs; with many sequences the work
 // spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and a launch.
-// The best k is taken if it beats no split by more than 5 %.
-int diff_row_tiles(int32_t suffix, int group) {
-  return (int)(((int64_t)suffix * group + kvt::kDiffTileRows - 1) / kvt::kDiffTileRows);
-}
+// The best k is taken if it beats no split by more than 5 %.  Times are in tiles of
+// 64 keys: 1.22 us each with a few busy CUs, 1.48 with all (heads of 128, bf16),
+// 11 us in fp32, half of that for heads of 64.
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
   const int cus = device_cus(), KT = 64;
   p.order = longest_first(seqs);
   p.nsplit.assign(B, 1);
-  const double tile_us = (pool->dtype == KVT_DTYPE_BF16 ? 1.0 : 11.0) * pool->head_dim / 128;
+  const double tile_us = (pool->dtype == KVT_DTYPE_BF16 ? 1.3 : 11.0) * pool->head_dim / 128;
   std::vector<int64_t> jobs(B), kt(B);
   for (int i = 0; i < B; ++i) {
     const int b = p.order[i];
@@ -1002,6 +1005,10 @@ DiffPlan diff_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   return p;
 }
 
+size_t diff_lambda_bytes(const kvt_diff* diff, int32_t num_q_heads, int64_t T) {
+  return ((size_t)(T - 1) * diff->lambda_stride + num_q_heads) * sizeof(float);
+}
+
 // The checks of both differential attention calls; fills the total token count.
 kvt_status check_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
                       const kvt_diff* diff, const void* out, int64_t* T) {
@@ -1013,8 +1020,7 @@ kvt_status check_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q,
     return KVT_ERR_INVALID_ARG;
   if (!std::isfinite(diff->out_scale)) return KVT_ERR_INVALID_ARG;
   const size_t out_bytes = (size_t)*T * num_q_heads * pool->head_dim * elem_bytes(pool->dtype);
-  const size_t lambda_bytes = ((size_t)(*T - 1) * diff->lambda_stride + num_q_heads) * sizeof(float);
-  if (overlaps(out, out_bytes, diff->lambda, lambda_bytes)) return KVT_ERR_INVALID_ARG;
+  if (overlaps(out, out_bytes, diff->lambda, diff_lambda_bytes(diff, num_q_heads, *T))) return KVT_ERR_INVALID_ARG;
   if (diff->norm_weight != nullptr) {
     if (!aligned16(diff->norm_weight) || !(diff->eps > 0.f) || !std::isfinite(diff->eps)) return KVT_ERR_INVALID_ARG;
     if (overlaps(out, out_bytes, diff->norm_weight, pool->head_dim * sizeof(float))) return KVT_ERR_INVALID_ARG;
@@ -1036,7 +1042,10 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
       if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
       if (!aligned16(workspace)) return KVT_ERR_INVALID_ARG;
       const size_t io = (size_t)T * num_q_heads * pool->head_dim * elem_bytes(pool->dtype);
-      if (overlaps(workspace, plan.ws_bytes, q, io) || overlaps(workspace, plan.ws_bytes, out, io))
+      if (overlaps(workspace, plan.ws_bytes, q, io) || overlaps(workspace, plan.ws_bytes, out, io) ||
+          overlaps(workspace, plan.ws_bytes, diff->lambda, diff_lambda_bytes(diff, num_q_heads, T)) ||
+          (diff->norm_weight != nullptr &&
+           overlaps(workspace, plan.ws_bytes, diff->norm_weight, pool->head_dim * sizeof(float))))
         return KVT_ERR_INVALID_ARG;
     }
   }
