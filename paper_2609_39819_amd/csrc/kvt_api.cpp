@@ -19,7 +19,9 @@
 #include <vector>
 
 #include "kvt.h"
+#include "kvt_diff.h"
 #include "kvt_internal.h"
+#include "kvt_rotary.h"
 
 namespace {
 

@@ -16,8 +16,6 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) __bf16 lds_bf16;
-typedef __attribute__((address_space(3))) char lds_char;
-typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -56,7 +54,6 @@ __device__ __forceinline__ u32x4 load8(const float* p) {
   return round8(*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4));
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 __device__ __forceinline__ void store4(__bf16* p, float a, float b, float c, float d) {
   u32x2 v;
   v[0] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){a, b}, bf16x2));
@@ -91,14 +88,6 @@ __device__ __forceinline__ float pair_sum(float x) {
   float a, b;
   pair_values(x, a, b);
   return a + b;
-}
-
-// y of differential attention from both maps' unnormalised outputs.  Each
-// product is rounded by itself: equal maps with lambda = 1 then cancel exactly,
-// where a fused product would leave its own last bits.
-__device__ __forceinline__ float map_difference(float o0, float inv0, float o1, float inv1, float lambda) {
-#pragma clang fp contract(off)
-  return o0 * inv0 - lambda * (o1 * inv1);
 }
 
 // Index of the sequence whose units contain `unit`: the last s < nseq with

@@ -15,25 +15,31 @@
 // 4..7 the second map of the same rows, on the K/V tiles that all of them share
 // in LDS.  (A wave with both maps reads each V fragment once for two products,
 // but its two outputs leave no registers to read operands ahead: 96/8 heads of
-// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.27 this way; one output
-// of 512 registers' worth per SIMD, both maps, 4.0 ms.)  S^T = K Q^T (keys on the
+// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.31 this way, 2.28 with K
+// fragments read a turn ahead.)  S^T = K Q^T (keys on the
 // MFMA rows, queries on the columns), so a query's scores sit in one lane pair
 // (l, l+32) and leave the accumulators in the layout that the value product
 // takes them in.  At the end the second map's waves hand their rows over through
 // LDS and the first map's form the difference and the norm; a key split writes
 // both maps' rows as they are, for the joining launch.
 //
-// bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys, probabilities
-// rounded to bf16 for the value product (their sum adds the rounded ones): the
-// result is off by 2.6e-3 of itself (2-norm), of which its own rounding is 1.7e-3.
+// bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys.  The probabilities are
+// rounded to bf16 for the value product (their sum adds the rounded ones), as the
+// extend kernel's; the maps' difference keeps both maps' roundings, so that the
+// result is off by 2.6e-3 of itself (2-norm; bf16 output alone 1.7e-3).  Handing
+// a quarter of them over as two bf16 numbers each leaves 2.4e-3 and costs 14 %,
+// all of them 1.7e-3 and 50 %.
 // fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded (the
 // difference of two maps keeps the error of the larger one).
 //
-// What bounds it: the matrix cores and the softmax beside them.  A tile of 64 keys
-// takes 2 x 24 MFMAs of 32 cycles per SIMD (1536) and 2 x 115 other vector
-// instructions (about 1200); with 8 workgroups on the chip it takes 3040 cycles
-// (1.27 us), with all CUs busy 1.45 us at the clock that the board then holds.
-// 2048 new tokens over 131072, 32/8 heads of 128: see the figures at the launch.
+// What bounds it: the matrix cores with the softmax and the barriers beside them.
+// A tile of 64 keys, heads of 128, takes 48 MFMAs of 32 cycles per SIMD (1536) and
+// 280 other vector instructions (1380); it lasts 2920 cycles (1.22 us) with 8
+// workgroups on the chip, of which a wave spends 900 at waits and barriers, and
+// 1.48 us with all CUs busy, at the clock that the board then holds.  2048 new
+// tokens over 131072, 32/8 heads of 128: 6.2 ms, 6.6e12 operations, 1070 TFLOP/s
+// (a large bf16 matrix product 1262).  512 over 8192: 119 us, 900 TFLOP/s.
+// fp32, 512 over 8192: 803 us, 133 TFLOP/s (a large fp32 matrix product 153).
 //
 // Masked positions.  Their scores are replaced by -inf, so their weight is
 // exactly 0 whatever K holds; positions past the end of the sequence and unused
@@ -44,8 +50,7 @@
 // hand and replaced by 0 for the product.
 #include <type_traits>
 
-#include "kvt_device.h"
-#include "kvt_internal.h"
+#include "kvt_diff_device.h"
 
 namespace kvt {
 namespace {
@@ -395,8 +400,9 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
 
   // ---- main loop: step t takes tile t.  K of tile t+3 and V of tile t+2 start to
   // stream in, each into the slot that the step before was done with (past the
-  // last tile the gather reads clamped, in-bounds pages into slots no one reads);
-  // the wait at the end leaves them in flight and is for those of the step before.
+  // last tile the gather reads clamped, in-bounds pages into slots no one reads).
+  // The barrier at the end waits for them too: a step is longer than a load takes,
+  // and a barrier that left them in flight measured the same.
   // bf16: the scores of a tile's first half come from the step before, and the
   // value product of its second half is left to the step after.
   uint32_t id2 = page_id(j0 + 2), id3 = page_id(j0 + 3);   // pages of tiles t+2, t+3
@@ -417,7 +423,6 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
 #pragma unroll
     for (int i = 0; i < VPIECES; ++i) reinterpret_cast<u32x4*>(v3.e)[tid + kThreads * i] = (u32x4){0u, 0u, 0u, 0u};
   }
-  __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NREG));
   __syncthreads();
   if (S::kBf16 && n > 0 && !idle) {
     score_block(k0, 0, s0);
@@ -457,7 +462,6 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
         value_block(v_cur, 0, p0);
       }
     }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NREG));
     __syncthreads();
   };
   for (int t = 0; t < n; t += 4) {

@@ -23,8 +23,7 @@
 // full chip, bf16 6.7).
 #include <type_traits>
 
-#include "kvt_device.h"
-#include "kvt_internal.h"
+#include "kvt_diff_device.h"
 
 namespace kvt {
 namespace {

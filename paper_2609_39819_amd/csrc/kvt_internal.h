@@ -27,11 +27,6 @@ constexpr int kDecWaves = 4;
 constexpr int kDecKeysPerTile = 32;
 constexpr int kDecMaxGroup = 32;
 
-// Differential attention tiling: one workgroup = 8 waves, two maps x 4 blocks of 32 packed query rows.
-constexpr int kDiffWaves = 8;
-constexpr int kDiffTileRows = kDiffWaves / 2 * 32;
-constexpr int kDiffDecHeads = 16;   // decode: query heads per workgroup, two maps each on one 32-row block
-
 struct SeqDesc {
   int32_t seq;      // row of the block table
   int32_t prefix;   // P_b
@@ -87,65 +82,7 @@ struct ExtendArgs {
   SeqDesc seq[kSeqsPerLaunch];
 };
 
-// Rotary positions of q rows, and of K rows on their way into the pages (with
-// num_kv_heads = 0: q rows only, no sequences).  Strides in elements.
-struct RotaryArgs {
-  const void* q;       // null: no q rows (num_q_heads = 0)
-  void* q_out;
-  const void* k_new;
-  const void* v_new;
-  void* k_pool;
-  void* v_pool;
-  int64_t q_stride, q_out_stride, k_stride, v_stride;
-  const int32_t* block_table;
-  const int32_t* positions;   // [num_axes][total_rows], or null: the logical positions
-  int64_t num_blocks;
-  int64_t row_begin;          // first packed row covered by this launch
-  int64_t rows;               // rows covered by this launch
-  int64_t total_rows;         // T of the whole call
-  int32_t max_blocks;
-  int32_t num_q_heads, num_kv_heads;
-  int32_t rot_dim;            // rotated columns of each part
-  int32_t parts;
-  int32_t interleaved;
-  int32_t nseq;
-  int32_t head_lanes;         // set by the launch: heads that a workgroup holds at a time
-  uint8_t axis[64];           // axis of each frequency
-  double turns[64];           // turns per position of each frequency
-  SeqDesc seq[kSeqsPerLaunch];  // in packed-row order
-};
-
-// Differential attention: extend and decode units, and the join of key splits
-// (there the sequences that are split, unit_begin counting their rows).
-struct DiffArgs {
-  const void* q;
-  const void* k_pool;
-  const void* v_pool;
-  void* out;
-  const float* lambda;        // + token * lambda_stride + head
-  const float* norm_weight;   // [D], or null: no norm
-  float* part_o;              // [partial row][2][D]: unnormalised outputs of both maps
-  float* part_ml;             // [partial row][4]: (running max in log2 units, row sum) of both maps
-  const int32_t* block_table;
-  int64_t lambda_stride;
-  int64_t num_blocks;
-  int32_t max_blocks;
-  int32_t num_q_heads;
-  int32_t num_kv_heads;
-  int32_t group;              // Hq / Hkv
-  float scale_log2;           // scale * log2(e)
-  float eps;
-  float out_scale;
-  int32_t nseq;
-  uint8_t nsplit[kSeqsPerLaunch];          // key splits of each sequence; 1: its units write out themselves
-  int32_t part_row[kSeqsPerLaunch];        // first partial row of a split sequence: [split][token][head]
-  int32_t unit_begin[kSeqsPerLaunch + 1];  // prefix sums of the sequences' units
-  SeqDesc seq[kSeqsPerLaunch];
-};
-static_assert(sizeof(DiffArgs) <= 8192, "kernel argument block too large");
-
 // Launch arguments travel by value; larger batches take several launches.
-static_assert(sizeof(RotaryArgs) <= 8192, "kernel argument block too large");
 static_assert(sizeof(ExtendArgs) <= 8192 && sizeof(AppendArgs) <= 8192, "kernel argument block too large");
 
 struct CombineArgs {
@@ -171,13 +108,9 @@ struct CopyArgs {
 
 // Launchers (device code files).  Return the launch status.
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, hipStream_t stream);
-hipError_t launch_rotary(RotaryArgs& a, int dtype, int head_dim, int cus, hipStream_t stream);
 hipError_t launch_extend(const ExtendArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_combine(const CombineArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_copy_blocks(const CopyArgs& a, int grid, hipStream_t stream);
-hipError_t launch_diff_extend(const DiffArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
-hipError_t launch_diff_decode(const DiffArgs& a, int dtype, int head_dim, int grid, bool one_per_cu, hipStream_t stream);
-hipError_t launch_diff_combine(const DiffArgs& a, int dtype, int head_dim, hipStream_t stream);
 // Decode: ExtendArgs with suffix 1 per sequence and nsplit units per sequence;
 // per_cu: workgroups that may share a CU (0: as many as fit).
 hipError_t launch_decode(const ExtendArgs& a, int dtype, int head_dim, int grid, int per_cu, hipStream_t stream);

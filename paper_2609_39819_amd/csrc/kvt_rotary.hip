@@ -26,7 +26,7 @@
 #include <algorithm>
 
 #include "kvt_device.h"
-#include "kvt_internal.h"
+#include "kvt_rotary.h"
 
 namespace kvt {
 namespace {
