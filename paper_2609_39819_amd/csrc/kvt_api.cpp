@@ -898,15 +898,19 @@ int diff_row_tiles(int32_t suffix, int group) {
 // first, one XCD's eighth of the units on its CUs; with many sequences the work
 // spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and a launch.
 // The best k is taken if it beats no split by more than 5 %.  Times are in tiles of
-// 64 keys: 1.22 us each with a few busy CUs, 1.48 with all (heads of 128, bf16),
-// 11 us in fp32, half of that for heads of 64.
+// 64 keys: 1.13 us each with a few busy CUs, 1.4 with all (heads of 128, bf16; of 64
+// 1.0), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
+// to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8 heads:
+// unsplit 272 us, 2 splits 253; 67 over 30011: 10 splits 59.2 us, 20 55.0).
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
   const int cus = device_cus(), KT = 64;
   p.order = longest_first(seqs);
   p.nsplit.assign(B, 1);
-  const double tile_us = (pool->dtype == KVT_DTYPE_BF16 ? 1.3 : 11.0) * pool->head_dim / 128;
+  const bool pairs = pool->dtype == KVT_DTYPE_BF16 && pool->head_dim == 64;
+  const double both = pairs ? 1.15 : 1.0;   // rate of a CU with two units
+  const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.0 : 1.3;
   std::vector<int64_t> jobs(B), kt(B);
   for (int i = 0; i < B; ++i) {
     const int b = p.order[i];
@@ -930,6 +934,7 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
       if (ns > 1) rows += (double)ns * seqs->suffix_len[p.order[i]] * num_q_heads;
     }
     if (B > kListed) span = std::max(longest, work / cus + 0.5 * longest);
+    span = std::max(longest, span / both);
     return span + (rows > 0 ? (4.0 + 2.0 * rows * 2 * pool->head_dim * 4 / 4.5e6) / tile_us : 0.0);
   };
   int64_t best = kt[0];

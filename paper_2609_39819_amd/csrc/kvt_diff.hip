@@ -15,8 +15,7 @@
 // 4..7 the second map of the same rows, on the K/V tiles that all of them share
 // in LDS.  (A wave with both maps reads each V fragment once for two products,
 // but its two outputs leave no registers to read operands ahead: 96/8 heads of
-// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.31 this way, 2.28 with K
-// fragments read a turn ahead.)  S^T = K Q^T (keys on the
+// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.31 this way, 2.20 since.)  S^T = K Q^T (keys on the
 // MFMA rows, queries on the columns), so a query's scores sit in one lane pair
 // (l, l+32) and leave the accumulators in the layout that the value product
 // takes them in.  At the end the second map's waves hand their rows over through
@@ -34,12 +33,12 @@
 //
 // What bounds it: the matrix cores with the softmax and the barriers beside them.
 // A tile of 64 keys, heads of 128, takes 48 MFMAs of 32 cycles per SIMD (1536) and
-// 280 other vector instructions (1380); it lasts 2920 cycles (1.22 us) with 8
-// workgroups on the chip, of which a wave spends 900 at waits and barriers, and
-// 1.48 us with all CUs busy, at the clock that the board then holds.  2048 new
-// tokens over 131072, 32/8 heads of 128: 6.2 ms, 6.6e12 operations, 1070 TFLOP/s
-// (a large bf16 matrix product 1262).  512 over 8192: 119 us, 900 TFLOP/s.
-// fp32, 512 over 8192: 803 us, 133 TFLOP/s (a large fp32 matrix product 153).
+// 210 other vector instructions (1150); it lasts 2720 cycles (1.13 us) with 8
+// workgroups on the chip and 1.4 us with all CUs busy, at the clock that the board
+// then holds.  2048 new tokens over 131072, 32/8 heads of 128: 5.78 ms, 6.6e12
+// operations, 1150 TFLOP/s (a large bf16 matrix product 1262).  512 over 8192:
+// 114 us, 930 TFLOP/s.  fp32, 512 over 8192: 801 us, 133 TFLOP/s (a large fp32
+// matrix product 153).
 //
 // Masked positions.  Their scores are replaced by -inf, so their weight is
 // exactly 0 whatever K holds; positions past the end of the sequence and unused
@@ -65,7 +64,6 @@ template <typename T, int D>
 struct Shape {
   static constexpr bool kBf16 = sizeof(T) == 2;
   static constexpr int KT = kBf16 ? 64 : 32;            // keys per tile
-  static constexpr int HALVES = KT / 32;                // 32-key MFMA blocks per tile
   static constexpr int ROWB = D * (int)sizeof(T);       // bytes per key row
   static constexpr int CHUNKS = ROWB / 16;
   static constexpr int RPR = 1024 / ROWB;               // key rows per 1 KiB wave load
@@ -124,10 +122,12 @@ struct Queries<float, D> {
   }
 };
 
+// bf16 heads of 64 hold to 128 registers and share a CU between two workgroups
+// (4096 new tokens over 16384, 32/8 heads: 1155 us one to a CU, 1036 two).
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs a) {
+__global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void diff_extend_kernel(const DiffArgs a) {
   using S = Shape<T, D>;
-  constexpr int KT = S::KT, HALVES = S::HALVES, DT = S::DT, RPR = S::RPR;
+  constexpr int KT = S::KT, DT = S::DT, RPR = S::RPR;
   constexpr int PAGES = KT / kBlock;                              // pages per tile
   constexpr int NREG = KT * S::ROWB / 1024 / kDiffWaves;          // 1 KiB loads per wave per tensor
   constexpr int QK = S::kBf16 ? D / 32 : D / 16;                  // query fragments
@@ -230,13 +230,15 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16){};
-  float m_ref = -INFINITY, l_run = 0.f;   // reference max of scale*log2e*score; this lane's share of sum 2^(s*c - m_ref)
+  float m_ref = -INFINITY, m_neg = NAN, l_run = 0.f;   // reference max of scale*log2e*score; this lane's share of sum 2^(s*c - m_ref)
   const float c = a.scale_log2;
 
   // ---- S^T = K Q^T: product k of a 32-key block takes 16 of the map's columns (fp32: 8)
+  int k_at[QK];   // this lane's byte offset in a K tile
+#pragma unroll
+  for (int k = 0; k < QK; ++k) k_at[k] = l32 * S::ROWB + (((2 * (map * QK + k) + hh) ^ S::swizzle_k(l32)) << 4);
   auto read_k = [&](const HalfTile<T, D>& tl, int k, int half) __attribute__((always_inline)) {
-    const int chunk = 2 * (map * QK + k) + hh;
-    return reinterpret_cast<const u32x4*>(tl.e)[(half * 32 + l32) * S::CHUNKS + (chunk ^ S::swizzle_k(l32))];
+    return *(const lds_u32x4*)((const lds_char*)tl.e + half * 32 * S::ROWB + k_at[k]);
   };
   auto score_product = [&](u32x4 kf, int k, f32x16 acc) __attribute__((always_inline)) {
     if constexpr (S::kBf16) {
@@ -256,7 +258,9 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
       if (8 * (e >> 2) + (e & 3) > thr) s[e] = -INFINITY;
   };
   // ---- moves the reference to the row maxima of these scores where they pass it
-  // by more than the slack; returns the factor for what was summed before
+  // by more than the slack; returns the factor for what was summed before.  m_neg,
+  // which the probabilities are formed with, is NaN until the row has a reference:
+  // their sum then tells check
   auto settle = [&](const f32x16& s) __attribute__((always_inline)) {
     float mx = -INFINITY;
 #pragma unroll
@@ -266,16 +270,16 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
     // 1 when unchanged, 0 when leaving -inf; kept at 1 while the row has seen no visible key
     const float alpha = (m_new == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);
     m_ref = m_new;
+    m_neg = (m_ref == -INFINITY) ? NAN : -m_ref;
     return alpha;
   };
   // ---- probabilities of 32 keys as B operands of the value product; returns their sum
-  auto probs = [&](const f32x16& s, Probs& p) __attribute__((always_inline)) {
-    const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
+  auto probs = [&](const f32x16& s, Probs& p, float neg) __attribute__((always_inline)) {
     float rs = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m_use));
-      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, -m_use));
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, neg));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, neg));
       if constexpr (S::kBf16) {
         const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
         rs = __builtin_amdgcn_fdot2_f32_bf16(pp, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, rs, false);
@@ -291,16 +295,25 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
   // ---- O^T += V^T P^T: product kg takes 16 keys (fp32: keys 8 (kg/4) + kg%4 and the
   // fourth after it, one per lane half) of 32 columns
   const int g16 = (lane >> 4) & 1, rsel = (lane & 15) >> 2;
+  // bf16: this lane's byte offsets in a V tile; with the bias in them what is left to
+  // add fits the 16 bits of a read's immediate offset where the K slots take 64 KiB
+  constexpr int kBias = 4 * sizeof(HalfTile<T, D>) >= 65536 ? 65536 : 0;
+  int v_at[2][DT];
+#pragma unroll
+  for (int r2 = 0; r2 < 2; ++r2)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int key = 8 * r2 + 4 * hh + rsel;            // key within a 16-key group
+      const int dcol = dt * 32 + g16 * 16 + 4 * (lane & 3);
+      v_at[r2][dt] = (key * D + (((dcol >> 3) ^ S::swizzle_v(key)) << 3) + (dcol & 7)) * (int)sizeof(T) + kBias;
+    }
   auto read_v = [&](const HalfTile<T, D>& tl, int half, int kg, int dt) __attribute__((always_inline)) {
     if constexpr (S::kBf16) {
       bf16x4 v[2];
 #pragma unroll
-      for (int r2 = 0; r2 < 2; ++r2) {
-        const int key = 8 * r2 + 4 * hh + rsel;          // key within a 16-key group
-        const int dcol = dt * 32 + g16 * 16 + 4 * (lane & 3);
-        const int off = key * D + (((dcol >> 3) ^ S::swizzle_v(key)) << 3) + (dcol & 7);
-        v[r2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)((const lds_bf16*)tl.e + off + (half * 32 + kg * 16) * D));
-      }
+      for (int r2 = 0; r2 < 2; ++r2)
+        v[r2] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+            (lds_bf16x4*)((const lds_char*)tl.e + (v_at[r2][dt] + ((half * 32 + kg * 16) * S::ROWB - kBias))));
       return (VFrag)__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       const int key = 8 * (kg >> 2) + 4 * hh + (kg & 3), col = dt * 32 + l32;
@@ -352,11 +365,11 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
   };
   // whether the probabilities p of the scores s hold; rs: their sum.  Where the
   // reference is not set yet, or some score passed it by far, or is a NaN, they
-  // are done again from the row maxima.
+  // are done again from the row maxima (a row that still sees nothing has weights 0).
   auto check = [&](const f32x16& s, Probs& p, float rs) __attribute__((always_inline)) {
-    if (__builtin_amdgcn_ballot_w64(!(rs < kSumLimit) || m_ref == -INFINITY) != 0) {
+    if (__builtin_amdgcn_ballot_w64(!(rs < kSumLimit)) != 0) {
       const float alpha = settle(s);
-      rs = probs(s, p);
+      rs = probs(s, p, m_ref == -INFINITY ? 0.f : -m_ref);
       l_run *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
@@ -367,9 +380,8 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
   // the next 32 keys and the value product of the 32 before, three streams that
   // do not depend on each other.  Heads of 128 read the K fragments of those scores
   // in the turn before (kf; kt, khalf is the block of the turn after), so that a
-  // turn's first products have nothing to wait for, and ask for the softmax between
-  // the products: 1.22 us per tile, 1.27 without kf.  With heads of 64, whose scores
-  // take two products, kf and that order cost 5%: kt, khalf is this turn's block.
+  // turn's first products have nothing to wait for (4 % of a tile).  With heads of
+  // 64, whose scores take two products, that costs 5 %: kt, khalf is this turn's block.
   constexpr bool kReadAhead = D == 128;
   u32x4 kf[QK];
   auto turn = [&](const HalfTile<T, D>& kt, int khalf, const f32x16& cur, f32x16& next, const HalfTile<T, D>& vt, int vhalf,
@@ -386,14 +398,13 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
 #pragma unroll
       for (int k = 0; k < QK; ++k) kf[k] = read_k(kt, k, khalf);
     }
-    const float rs = probs(cur, out);
-    if constexpr (kReadAhead) {
+    const float rs = probs(cur, out, m_neg);
+    // after each product two operand reads and a share of the softmax
 #pragma unroll
-      for (int i = 0; i < QK + KG * DT; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      }
+    for (int i = 0; i < QK + KG * DT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, kReadAhead ? 2 : 8, 0);
     }
     check(cur, out, rs);
   };
@@ -439,6 +450,14 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
     gather(vpool, v_off, j0 + t + 2, id2, v_fill);
     id2 = id3, id3 = page_id(j0 + t + 4);
     if (t >= masked) drop_odd(v_cur);
+    // opaque, so that the slots' bases go into the reads' immediate offsets and not
+    // into a register for each slot and offset (46 registers)
+    if constexpr (S::kBf16) {
+#pragma unroll
+      for (int k = 0; k < QK; ++k) asm("" : "+v"(k_at[k]));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) asm("" : "+v"(v_at[0][dt]), "+v"(v_at[1][dt]));
+    }
     if (!idle) {
       // asm: a branch where there is something to mask, not selects on every tile
       if constexpr (S::kBf16) {
@@ -458,7 +477,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
           asm volatile("");
           mask((j0 + t) * KT, s0);
         }
-        check(s0, p0, probs(s0, p0));
+        check(s0, p0, probs(s0, p0, m_neg));
         value_block(v_cur, 0, p0);
       }
     }
@@ -570,7 +589,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_extend_kernel(const DiffArgs
 // weight, be it 0, so an infinity or a NaN among the values gives the unsplit
 // call's.  args: the sequences with more than one split; unit_begin counts
 // their rows.
-constexpr int kAhead = 8;   // splits whose pieces are in flight at once
+constexpr int kAhead = 4;   // splits whose pieces are in flight at once, the first from before the weights are known
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
@@ -589,6 +608,16 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
   const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;
   const int64_t first = a.part_row[si] + (int64_t)local;
 
+  const float* po = a.part_o + first * 2 * D + lq * 4;
+  f32x4 v[kAhead][2];
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (s0 + i < nsplit)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) v[i][x] = load4(po + ((s0 + i) * rows * 2 + x) * D);
+  };
+  load(0);
   float m[2][PER], l[2][PER], top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
@@ -617,14 +646,8 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
   }
   __syncthreads();
   f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  const float* po = a.part_o + first * 2 * D + lq * 4;
   for (int s0 = 0; s0 < nsplit; s0 += kAhead) {
-    f32x4 v[kAhead][2];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (s0 + i < nsplit)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) v[i][x] = load4(po + ((s0 + i) * rows * 2 + x) * D);
+    if (s0 > 0) load(s0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (s0 + i < nsplit)

@@ -53,7 +53,8 @@ def demangle(name: str) -> str:
     """Readable form of this library's kernel symbols (c++filt does not know
     the bf16 mangling DF16b)."""
     import re
-    m = re.search(r"(extend_fwd_kernel|extend_combine_few_kernel|extend_combine_kernel|decode_kernel)I(DF16b|f)Li(\d+)E", name)
+    m = re.search(r"(extend_fwd_kernel|extend_combine_few_kernel|extend_combine_kernel|diff_extend_kernel|diff_combine_kernel|"
+                  r"diff_decode_kernel|decode_kernel|rotary_kernel)I(DF16b|f)Li(\d+)E", name)
     if m:
         return f"{m.group(1)}<{'bf16' if m.group(2) == 'DF16b' else 'float'}, {m.group(3)}>"
     return name
@@ -61,7 +62,8 @@ def demangle(name: str) -> str:
 
 def short_name(name: str) -> str:
     name = demangle(name)
-    for key in ("extend_fwd_kernel", "extend_combine_kernel", "decode_kernel", "append_kv_kernel"):
+    for key in ("diff_extend_kernel", "diff_combine_kernel", "diff_decode_kernel", "rotary_kernel", "extend_fwd_kernel",
+                "extend_combine_kernel", "decode_kernel", "append_kv_kernel"):
         if key in name:
             tmpl = name[name.find(key):]
             return tmpl.split("(")[0].replace("kvt::(anonymous namespace)::", "")
