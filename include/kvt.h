@@ -346,7 +346,8 @@ typedef struct {
  * no row is empty.
  *
  * bf16 inputs feed bf16 MFMA, the probabilities rounded to bf16 for the value
- * product (kvt_diff_decode_attention: given as the sum of two bf16 numbers);
+ * product, those of every fourth 16 keys (kvt_diff_decode_attention: of all)
+ * given as the sum of two bf16 numbers;
  * fp32 inputs run fp32 MFMA (unlike the other attention calls, which round
  * them to bf16: here the difference of two maps would keep that error).
  * Softmax statistics, accumulation and the norm are fp32.

@@ -898,10 +898,10 @@ int diff_row_tiles(int32_t suffix, int group) {
 // first, one XCD's eighth of the units on its CUs; with many sequences the work
 // spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and a launch.
 // The best k is taken if it beats no split by more than 5 %.  Times are in tiles of
-// 64 keys: 1.13 us each with a few busy CUs, 1.4 with all (heads of 128, bf16; of 64
-// 1.0), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
+// 64 keys: 1.28 us each with a few busy CUs, 1.55 with all (heads of 128, bf16; of 64
+// 1.1), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
 // to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8 heads:
-// unsplit 272 us, 2 splits 253; 67 over 30011: 10 splits 59.2 us, 20 55.0).
+// unsplit 309 us, 2 splits 279; 512 over 8192: 2 splits 90.7 us, 4 84.0).
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
@@ -910,7 +910,7 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   p.nsplit.assign(B, 1);
   const bool pairs = pool->dtype == KVT_DTYPE_BF16 && pool->head_dim == 64;
   const double both = pairs ? 1.15 : 1.0;   // rate of a CU with two units
-  const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.0 : 1.3;
+  const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.1 : 1.4;
   std::vector<int64_t> jobs(B), kt(B);
   for (int i = 0; i < B; ++i) {
     const int b = p.order[i];
