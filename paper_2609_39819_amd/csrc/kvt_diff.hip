@@ -11,9 +11,10 @@
 //
 // Work decomposition: one workgroup per (sequence, kv-head, 128 packed query
 // rows, key split), as the extend kernel's (row r = token r/G, head g*G + r%G);
-// 8 waves, two per SIMD: waves 0..3 take the first map of 32 rows each, waves
-// 4..7 the second map of the same rows, on the K/V tiles that all of them share
-// in LDS.  (A wave with both maps reads each V fragment once for two products,
+// 8 waves, two per SIMD: waves 2 i and 2 i + 1 take the two maps of 32
+// rows each, on the K/V tiles that all of them share in LDS (up to 64 rows then
+// have a wave per SIMD: 16 new tokens over 30000, 32/8 heads of 128, 34.1 us, 37.7
+// with the maps four waves apart).  (A wave with both maps reads each V fragment once for two products,
 // but its two outputs leave no registers to read operands ahead: 96/8 heads of
 // 128, 1024 new tokens over 32768, 2.38 ms that way, 2.31 this way.)  S^T = K Q^T (keys on the
 // MFMA rows, queries on the columns), so a query's scores sit in one lane pair
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int map = wave >> 2, rg = wave & 3;   // this wave's map and 32-row block
+  const int map = wave & 1, rg = wave >> 1;   // this wave's map and 32-row block
   const int hh = lane >> 5;     // lane half
   const int l32 = lane & 31;
   if (tid == 0) odd_seen = 0;
