@@ -343,20 +343,20 @@ typedef struct {
  * or out_scale * y without norm_weight.  K_b/V_b are read through the block
  * table from pools that kvt_append_kv or kvt_append_kv_rotary (parts = 2)
  * filled; scale is usually 1/sqrt(d).  Each row's own position is visible, so
- * no row is empty.
+ * no row is empty.  Infinities and NaN in V reach the rows that see them and no
+ * others; a non-finite key leaves the rows that see it unspecified.
  *
  * bf16 inputs feed bf16 MFMA, the probabilities rounded to bf16 for the value
- * product, those of every fourth 16 keys (kvt_diff_decode_attention: of all)
- * given as the sum of two bf16 numbers;
- * fp32 inputs run fp32 MFMA (unlike the other attention calls, which round
- * them to bf16: here the difference of two maps would keep that error).
- * Softmax statistics, accumulation and the norm are fp32.
+ * product (those of the first 16 of every 64 keys, and all of
+ * kvt_diff_decode_attention's, given as the sum of two bf16 numbers); fp32
+ * inputs run fp32 MFMA (unlike the other attention calls, which round them to
+ * bf16: here the difference of two maps would keep that error).  Softmax
+ * statistics, accumulation and the norm are fp32.
  *
  * Other arguments, alignments and errors as for kvt_extend_attention (there
  * is no lse: the maps' difference cannot be merged by one).  lambda and
  * norm_weight may not overlap out, nor the workspace any of q, out, lambda and
- * norm_weight.  workspace:
- * NULL/0 runs without splitting, otherwise at least
+ * norm_weight.  workspace: NULL/0 runs without splitting, otherwise at least
  * kvt_diff_extend_workspace_bytes() for the same arguments, 16-byte aligned
  * (else KVT_ERR_WORKSPACE, KVT_ERR_INVALID_ARG; any workspace will do where
  * that is 0).  Results are bit-reproducible for given arguments.

@@ -896,10 +896,10 @@ int diff_row_tiles(int32_t suffix, int group) {
 // chunks of about equal length, the longest one's range divided by k, for a
 // range of k; each k is charged the finish of its units (list scheduling, longest
 // first, one XCD's eighth of the units on its CUs; with many sequences the work
-// spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and a launch.
-// The best k is taken if it beats no split by more than 5 %.  Times are in tiles of
-// 64 keys: 1.28 us each with a few busy CUs, 1.55 with all (heads of 128, bf16; of 64
-// 1.1), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
+// spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and
+// a launch.  The best k is taken if it beats no split by more than 5 %.  Times are
+// in tiles of 64 keys: 1.28 us each with a few busy CUs, 1.55 with all (heads of
+// 128, bf16; of 64 1.1), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
 // to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8 heads:
 // unsplit 309 us, 2 splits 279; 512 over 8192: 2 splits 90.7 us, 4 84.0).
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {

@@ -11,17 +11,17 @@
 //
 // Work decomposition: one workgroup per (sequence, kv-head, 128 packed query
 // rows, key split), as the extend kernel's (row r = token r/G, head g*G + r%G);
-// 8 waves, two per SIMD: waves 2 i and 2 i + 1 take the two maps of 32
-// rows each, on the K/V tiles that all of them share in LDS (up to 64 rows then
-// have a wave per SIMD: 16 new tokens over 30000, 32/8 heads of 128, 34.1 us, 37.7
-// with the maps four waves apart).  (A wave with both maps reads each V fragment once for two products,
-// but its two outputs leave no registers to read operands ahead: 96/8 heads of
-// 128, 1024 new tokens over 32768, 2.38 ms that way, 2.31 this way.)  S^T = K Q^T (keys on the
-// MFMA rows, queries on the columns), so a query's scores sit in one lane pair
-// (l, l+32) and leave the accumulators in the layout that the value product
-// takes them in.  At the end the second map's waves hand their rows over through
-// LDS and the first map's form the difference and the norm; a key split writes
-// both maps' rows as they are, for the joining launch.
+// 8 waves, two per SIMD: waves 2 i and 2 i + 1 take the two maps of 32 rows each,
+// on the K/V tiles that all of them share in LDS.  Row tiles of up to 64 rows
+// then have a wave per SIMD (16 new tokens over 30000, 32/8 heads of 128, 34.1 us;
+// with the maps four waves apart 37.7).  A wave with both maps would read each V
+// fragment once for two products, but its two outputs leave no registers to read
+// operands ahead (96/8 heads of 128, 1024 new tokens over 32768, 2.38 and 2.31 ms).
+// S^T = K Q^T (keys on the MFMA rows, queries on the columns), so a query's scores
+// sit in one lane pair (l, l+32) and leave the accumulators in the layout that the
+// value product takes them in.  At the end the second map's waves hand their rows
+// over through LDS and the first map's form the difference and the norm; a key
+// split writes both maps' rows as they are, for the joining launch.
 //
 // bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys.  The value product
 // takes the probabilities in bf16, and the maps' difference keeps both maps'
