@@ -346,9 +346,10 @@ def _host_values(x, name: str, dtype: str):
     return x.ctypes.data, x.size, x
 
 
-def _rotary_args(inv_freq, axis, positions, tokens: int, parts: int, interleaved: bool, device) -> tuple:
+def _rotary_args(inv_freq, axis, positions, tokens: int, parts: int, interleaved: bool, device: int) -> tuple:
     """The arguments of a rotation as ``_kvt_call`` takes them, and the host
-    arrays that they point into."""
+    arrays that they point into.  ``device``: ``get_device()`` of the call's
+    tensors, here and below (a device object costs several times as much)."""
     import torch
     freq, pairs, keep = _host_values(inv_freq, "inv_freq", "float32")
     ax = None
@@ -361,23 +362,23 @@ def _rotary_args(inv_freq, axis, positions, tokens: int, parts: int, interleaved
     if positions is not None:
         shape = positions.shape
         if (positions.dtype != torch.int32 or len(shape) not in (1, 2) or shape[-1] != tokens
-                or not positions.is_contiguous() or positions.device != device):
-            raise ValueError(f"positions must be a contiguous int32 [axes][{tokens}] tensor on {device}")
+                or not positions.is_contiguous() or positions.get_device() != device):
+            raise ValueError(f"positions must be a contiguous int32 [axes][{tokens}] tensor on the call's GPU")
         at = positions.data_ptr()
         if len(shape) == 2:
             axes = shape[0]
     return (freq, ax, at, axes, 2 * pairs, int(parts), 1 if interleaved else 0), keep
 
 
-def _rows_of(t, name: str, tokens: int, heads: Optional[int], d: int, dtype, device) -> tuple:
+def _rows_of(t, name: str, tokens: int, heads: Optional[int], d: int, dtype, device: int) -> tuple:
     """(address, token stride) of a [tokens][heads][d] tensor whose tokens may lie apart."""
     shape = t.shape
     if (t.dtype != dtype or len(shape) != 3 or shape[0] != tokens or (heads is not None and shape[1] != heads)
             or shape[2] != d):
         raise ValueError(f"{name} must be a [{tokens}][{'heads' if heads is None else heads}][{d}] {dtype} tensor, "
                          f"got {tuple(shape)} {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on the call's GPU {device}")
     packed = shape[1] * d
     strides = t.stride()
     if strides[2] != 1 or (shape[1] > 1 and strides[1] != d) or (tokens > 1 and strides[0] < packed):
@@ -385,12 +386,16 @@ def _rows_of(t, name: str, tokens: int, heads: Optional[int], d: int, dtype, dev
     return t.data_ptr(), strides[0] if tokens > 1 else packed
 
 
-def _check_table(block_table, sequences: int, device, *others):
+def _check_table(block_table, sequences: int, device: int, *others):
     """A table row for every sequence, everything on one device."""
     if block_table.shape[0] < sequences:
         raise ValueError(f"block_table has {block_table.shape[0]} rows for {sequences} sequences")
-    if any(t.device != device for t in (block_table, *others)):
-        raise ValueError(f"every tensor of the call must be on {device}")
+    for t in (block_table, *others):
+        if t.get_device() != device:
+            raise ValueError(f"every tensor of the call must be on the pool's GPU {device}, got {t.device}")
+
+
+_NO_SWITCH = contextlib.nullcontext()
 
 
 def _on_device(t):
@@ -398,8 +403,8 @@ def _on_device(t):
     import torch
     if not t.is_cuda:
         raise ValueError("expected GPU tensors")
-    if t.get_device() == torch.cuda.current_device():
-        return contextlib.nullcontext()
+    if t.get_device() == torch._C._cuda_getDevice():   # a GPU tensor: the runtime is up
+        return _NO_SWITCH
     return torch.cuda.device(t.device)
 
 
@@ -422,13 +427,16 @@ def rotate(x, positions, inv_freq, *, axis=None, interleaved: bool = False, part
     T, H, d = x.shape
     if positions is None:
         raise ValueError("rotate needs positions")
-    rotary, keep = _rotary_args(inv_freq, axis, positions, T, parts, interleaved, x.device)
-    rows = _rows_of(x, "x", T, H, d, x.dtype, x.device)
+    device = x.get_device()
+    rotary, keep = _rotary_args(inv_freq, axis, positions, T, parts, interleaved, device)
+    rows = _rows_of(x, "x", T, H, d, x.dtype, device)
     code = _dtype_code(x)
     with _on_device(x):
         if out is None:
-            out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
-        to = _rows_of(out, "out", T, H, d, x.dtype, x.device)
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            to = out.data_ptr(), H * d
+        else:
+            to = _rows_of(out, "out", T, H, d, x.dtype, device)
         st = _native().rotate(lib().address["kvt_rotate"], *rotary, *rows, T, H, d, code, *to, _stream_handle(x))
     del keep
     if st != KVT_OK:
@@ -454,7 +462,7 @@ def append_kv_rotary(k_pool, v_pool, block_table, prefix_len: Sequence[int], suf
                                     axis=axis, interleaved=interleaved, parts=parts, positions=positions, q=q,
                                     q_out=q_out, checked=checked)
     pool = _pool_args(k_pool, v_pool)
-    hkv, d, dtype, device = pool[3], pool[4], k_pool.dtype, k_pool.device
+    hkv, d, dtype, device = pool[3], pool[4], k_pool.dtype, k_pool.get_device()
     head, T = _head("kvt_append_kv_rotary", pool, prefix_len, suffix_len, block_table, checked)
     _check_table(block_table, head[8], device, v_pool)
     rotary, keep = _rotary_args(inv_freq, axis, positions, T, parts, interleaved, device)
@@ -470,8 +478,10 @@ def append_kv_rotary(k_pool, v_pool, block_table, prefix_len: Sequence[int], suf
     with _on_device(k_pool):
         if q is not None:
             if q_out is None:
-                q_out = torch.empty((T, hq, d), dtype=dtype, device=device)
-            to = _rows_of(q_out, "q_out", T, hq, d, dtype, device)
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                to = q_out.data_ptr(), hq * d
+            else:
+                to = _rows_of(q_out, "q_out", T, hq, d, dtype, device)
         st = _native().append_rotary(*head, *rotary, *k_rows, *v_rows, *q_rows, hq, *to, _stream_handle(k_pool))
     del keep
     if st != KVT_OK:
@@ -696,7 +706,7 @@ def _diff_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, p
     native = _native()
     pool = _pool_args(k_pool, v_pool)
     head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
-    Hq, d, device = int(q.shape[1]), pool[4], k_pool.device
+    Hq, d, device = int(q.shape[1]), pool[4], k_pool.get_device()
     _check_tokens(q, "q", T, Hq, d, k_pool.dtype)
     if lam.dtype != torch.float32 or lam.shape not in ((Hq,), (T, Hq)) or (Hq > 1 and lam.stride(-1) != 1):
         raise ValueError(f"lam must be a float32 [{Hq}] or [{T}][{Hq}] tensor, its heads contiguous")
@@ -725,7 +735,7 @@ def _diff_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, p
         elif use_workspace:
             ws_bytes = native.workspace(lib().address[ws_entry], *head[1:], Hq)
             if ws_bytes:
-                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
+                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=k_pool.device)
                 ws_ptr = workspace.data_ptr()
         st = native.diff_attend(*head, q.data_ptr(), Hq, float(scale), lam.data_ptr(), stride,
                                 None if norm_weight is None else norm_weight.data_ptr(), float(eps), float(out_scale),
