@@ -858,6 +858,7 @@ kvt_status launch_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, const 
 struct DiffPlan {
   std::vector<int> order;          // sequences, longest key range first
   std::vector<int32_t> nsplit;     // by sequence
+  std::vector<int32_t> nlast;      // by sequence: of its last row tile (extend)
   std::vector<int32_t> part_row;   // by sequence: first partial row (0 where it is not split)
   int64_t part_rows = 0;
   size_t ws_bytes = 0;
@@ -880,6 +881,7 @@ void diff_layout(DiffPlan* p, const kvt_pool* pool, const kvt_seqs* seqs, int32_
     p->part_rows += (int64_t)p->nsplit[b] * seqs->suffix_len[b] * num_q_heads;
     if (p->part_rows > INT32_MAX) {
       p->nsplit.assign(B, 1);
+      p->nlast.assign(B, 1);
       p->part_row.assign(B, 0);
       p->part_rows = 0;
       break;
@@ -902,6 +904,9 @@ int diff_row_tiles(int32_t suffix, int group) {
 // 128, bf16; of 64 1.1), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
 // to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8 heads:
 // unsplit 309 us, 2 splits 279; 512 over 8192: 2 splits 90.7 us, 4 84.0).
+//
+// A last row tile of up to 64 rows has a wave per SIMD and takes 0.76 of a tile's
+// time (fp32 0.53); beside full ones it gets as many splits less.
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
@@ -911,10 +916,14 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   const bool pairs = pool->dtype == KVT_DTYPE_BF16 && pool->head_dim == 64;
   const double both = pairs ? 1.15 : 1.0;   // rate of a CU with two units
   const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.1 : 1.4;
-  std::vector<int64_t> jobs(B), kt(B);
+  const double light = pool->dtype == KVT_DTYPE_BF16 ? 0.76 : 0.53;
+  std::vector<int64_t> jobs(B), kt(B);   // jobs: full row tiles of all kv-heads
+  std::vector<uint8_t> rest(B);          // whether a light one follows
   for (int i = 0; i < B; ++i) {
     const int b = p.order[i];
-    jobs[i] = (int64_t)diff_row_tiles(seqs->suffix_len[b], G) * H;
+    const int tiles = diff_row_tiles(seqs->suffix_len[b], G);
+    rest[i] = (int64_t)seqs->suffix_len[b] * G - (int64_t)(tiles - 1) * kvt::kDiffTileRows <= kvt::kDiffTileRows / 2;
+    jobs[i] = (int64_t)(tiles - rest[i]) * H;
     kt[i] = ((int64_t)seqs->prefix_len[b] + seqs->suffix_len[b] + KT - 1) / KT;
   }
   constexpr int kXcds = 8, kListed = 32;
@@ -922,15 +931,21 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   auto splits = [&](int i, int64_t chunk) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(kvt::kMaxPartials, (kt[i] + chunk - 1) / chunk));
   };
+  auto light_splits = [&](int i, int ns) {
+    return rest[i] && jobs[i] > 0 ? std::max(1, (int)std::ceil(light * ns)) : ns;
+  };
   auto cost = [&](int64_t chunk) {
     double span = 0.0, work = 0.0, longest = 0.0, rows = 0.0;
     FreeTimes free_at(0.0, xcd_cus, 0.0, 0);
-    for (int i = 0; i < B; ++i) {
-      const int ns = splits(i, chunk);
-      const double len = std::ceil((double)kt[i] / ns) + kUnitTiles;
-      if (B <= kListed) span = std::max(span, free_at.run((jobs[i] * ns + kXcds - 1) / kXcds, len));
-      work += (double)jobs[i] * ns * len;
+    auto put = [&](int64_t units, double len) {
+      if (B <= kListed) span = std::max(span, free_at.run((units + kXcds - 1) / kXcds, len));
+      work += (double)units * len;
       longest = std::max(longest, len);
+    };
+    for (int i = 0; i < B; ++i) {
+      const int ns = splits(i, chunk), nl = light_splits(i, ns);
+      if (jobs[i] > 0) put(jobs[i] * ns, std::ceil((double)kt[i] / ns) + kUnitTiles);
+      if (rest[i]) put((int64_t)H * nl, light * (std::ceil((double)kt[i] / nl) + kUnitTiles));
       if (ns > 1) rows += (double)ns * seqs->suffix_len[p.order[i]] * num_q_heads;
     }
     if (B > kListed) span = std::max(longest, work / cus + 0.5 * longest);
@@ -939,13 +954,19 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   };
   int64_t best = kt[0];
   double best_cost = 0.95 * cost(kt[0]);
-  for (int k : {2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32, 40, 48, 64}) {
+  for (int k : {2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16, 18, 20, 22, 24, 26, 28, 30, 32, 36, 40, 48, 64}) {
     if (k > kt[0]) break;
+    if (B > 8 && k > 8 && k % 4 != 0) continue;   // large batches: fewer, for the host's sake
     const int64_t chunk = (kt[0] + k - 1) / k;
     const double c = cost(chunk);
     if (c < best_cost - 1e-9) best = chunk, best_cost = c;
   }
-  for (int i = 0; i < B; ++i) p.nsplit[p.order[i]] = best == kt[0] ? 1 : splits(i, best);
+  p.nlast.assign(B, 1);
+  for (int i = 0; i < B && best != kt[0]; ++i) {
+    const int ns = splits(i, best);
+    p.nsplit[p.order[i]] = ns;
+    p.nlast[p.order[i]] = light_splits(i, ns);
+  }
   diff_layout(&p, pool, seqs, num_q_heads);
   return p;
 }
@@ -1006,6 +1027,7 @@ DiffPlan diff_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   }
   int64_t units = 0;
   for (int b = 0; b < B; ++b) units += (p.nsplit[b] = splits(b, chunk)) * heads;
+  p.nlast = p.nsplit;
   const int64_t unit = (longest + p.nsplit[p.order.front()] - 1) / p.nsplit[p.order.front()];   // the longest one
   p.one_per_cu = units > cus && longest > 2 * shortest && all >= 1500 * units && 40 * unit * cus >= 21 * all;
   diff_layout(&p, pool, seqs, num_q_heads);
@@ -1044,6 +1066,7 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
   if (plan.ws_bytes > 0) {
     if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
       plan.nsplit.assign(B, 1);
+      plan.nlast.assign(B, 1);
       plan.ws_bytes = 0;
     } else {
       if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
@@ -1084,6 +1107,7 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
   auto describe = [&](int i, int b) {
     a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
     a.nsplit[i] = (uint8_t)plan.nsplit[b];
+    a.nlast[i] = (uint8_t)plan.nlast[b];
     a.part_row[i] = plan.part_row[b];
   };
   const int64_t per_unit = (int64_t)pool->num_kv_heads *
@@ -1095,7 +1119,7 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
       const int b = plan.order[c0 + i];
       describe(i, b);
       a.unit_begin[i] = (int32_t)units;
-      units += (int64_t)(decode ? 1 : diff_row_tiles(seqs->suffix_len[b], G)) * plan.nsplit[b];
+      units += (decode ? 0 : (int64_t)diff_row_tiles(seqs->suffix_len[b], G) - 1) * plan.nsplit[b] + plan.nlast[b];
       if (units * per_unit > INT32_MAX) return KVT_ERR_INVALID_ARG;
     }
     a.nseq = n;

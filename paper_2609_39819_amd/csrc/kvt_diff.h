@@ -34,6 +34,7 @@ struct DiffArgs {
   float out_scale;
   int32_t nseq;
   uint8_t nsplit[kSeqsPerLaunch];          // key splits of each sequence; 1: its units write out themselves
+  uint8_t nlast[kSeqsPerLaunch];           // extend: key splits of its last row tile (at most nsplit)
   int32_t part_row[kSeqsPerLaunch];        // first partial row of a split sequence: [split][token][head]
   int32_t unit_begin[kSeqsPerLaunch + 1];  // prefix sums of the sequences' units
   SeqDesc seq[kSeqsPerLaunch];

@@ -162,13 +162,15 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   const int unit = blockIdx.x / hkv;
   const int si = find_seq(a.unit_begin, a.nseq, unit);
   const SeqDesc sd = a.seq[si];
-  const int nsplit = a.nsplit[si];
+  const int nsplit = a.nsplit[si], nlast = a.nlast[si];
   const int local = unit - a.unit_begin[si];
   const int G = a.group;
   const int rows_seq = sd.suffix * G;
   const int ntile = (rows_seq + kDiffTileRows - 1) / kDiffTileRows;
-  const int rt = ntile - 1 - local / nsplit;   // longest (last) row tile first
-  const int split = local % nsplit;
+  // longest (last) row tile first
+  const bool last = local < nlast;
+  const int rt = last ? ntile - 1 : ntile - 2 - (local - nlast) / nsplit;
+  const int split = last ? local : (local - nlast) % nsplit;
   const int r0 = rt * kDiffTileRows;
   const int P = sd.prefix;
   const int L = P + sd.suffix;                 // positions that can be read
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   // keys up to the tile's last query's own position, evenly over the splits
   const int t_last = min(sd.suffix - 1, (r0 + kDiffTileRows - 1) / G);
   const int ntiles_kv = (P + t_last + KT) / KT;
-  const int per_split = (ntiles_kv + nsplit - 1) / nsplit;
+  const int per_split = last ? (ntiles_kv + nlast - 1) / nlast : (ntiles_kv + nsplit - 1) / nsplit;
   const int j0 = split * per_split;
   const int j1 = min(ntiles_kv, j0 + per_split);
   const int n = j1 - j0;                       // tiles (none: a split past the keys)
@@ -630,8 +632,9 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
   const int row = live ? idx : total - 1;
   const int si = find_seq(a.unit_begin, a.nseq, row);
   const SeqDesc sd = a.seq[si];
-  const int nsplit = a.nsplit[si];
   const int local = row - a.unit_begin[si];        // token * Hq + head within the sequence
+  const int packed = local / a.num_q_heads * a.group + local % a.num_q_heads % a.group;
+  const int nsplit = packed / kDiffTileRows == (sd.suffix * a.group - 1) / kDiffTileRows ? a.nlast[si] : a.nsplit[si];
   const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;
   const int64_t first = a.part_row[si] + (int64_t)local;
 
