@@ -135,7 +135,7 @@ typedef struct {
  *
  * x, out: rows of head_dim 64 or 128 in `dtype` (else KVT_ERR_UNSUPPORTED).
  * out may be x itself (same data, same stride) and must not touch x's rows
- * otherwise.  num_tokens = 0 is a no-op; num_tokens * num_heads at most
+ * otherwise, nor the positions.  num_tokens = 0 is a no-op; num_tokens * num_heads at most
  * INT32_MAX.  rotary->positions is required, [num_axes][num_tokens].
  */
 kvt_status kvt_rotate(const kvt_rotary* rotary, const kvt_rows* x, int64_t num_tokens, int32_t num_heads,
@@ -154,8 +154,8 @@ kvt_status kvt_rotate(const kvt_rotary* rotary, const kvt_rows* x, int64_t num_t
  * k_new, v_new: rows of Hkv heads; q, q_out: rows of num_q_heads heads (a
  * multiple of Hkv, T * num_q_heads at most INT32_MAX), or both NULL with
  * num_q_heads = 0.  q_out may be q itself (same data, same stride) and must
- * not touch q, k_new or v_new otherwise; nothing may overlap a pool.  Pool,
- * table, checked mode and ordering as for kvt_append_kv.
+ * not touch q, k_new, v_new or the positions otherwise; no rows may overlap a
+ * pool.  Pool, table, checked mode and ordering as for kvt_append_kv.
  */
 kvt_status kvt_append_kv_rotary(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rotary* rotary,
                                 const kvt_rows* k_new, const kvt_rows* v_new,

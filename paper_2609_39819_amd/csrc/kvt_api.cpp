@@ -786,6 +786,12 @@ bool rows_touch(const Rows& x, const Rows& y) {
 }
 bool rows_same(const Rows& x, const Rows& y) { return x.first == y.first && x.width == y.width && x.step == y.step; }
 
+// Whether rows that a call writes reach into the positions that it reads.
+bool covers_positions(const Rows& out, const kvt_rotary* r) {
+  return r->positions != nullptr && overlaps((const void*)out.first, out.extent(), r->positions,
+                                             (size_t)r->num_axes * out.n * sizeof(int32_t));
+}
+
 // The rotary description; fills the launch's frequencies.
 kvt_status check_rotary(const kvt_rotary* r, int32_t head_dim, kvt::RotaryArgs* a) {
   if (r == nullptr || r->inv_freq == nullptr) return KVT_ERR_INVALID_ARG;
@@ -1227,6 +1233,7 @@ kvt_status kvt_rotate(const kvt_rotary* rotary, const kvt_rows* x, int64_t num_t
   if ((st = check_rows(x, num_tokens, width, elem_bytes(dtype), &from)) != KVT_OK) return st;
   if ((st = check_rows(out, num_tokens, width, elem_bytes(dtype), &to)) != KVT_OK) return st;
   if (!rows_same(from, to) && rows_touch(from, to)) return KVT_ERR_INVALID_ARG;
+  if (covers_positions(to, rotary)) return KVT_ERR_INVALID_ARG;
   a.q = x->data;
   a.q_out = out->data;
   a.q_stride = x->stride;
@@ -1267,6 +1274,7 @@ kvt_status kvt_append_kv_rotary(const kvt_pool* pool, const kvt_seqs* seqs, cons
     if ((st = check_rows(q_out, T, q_width, es, &qo)) != KVT_OK) return st;
     if (in_pool(qi) || in_pool(qo) || rows_touch(qo, k) || rows_touch(qo, v)) return KVT_ERR_INVALID_ARG;
     if (!rows_same(qi, qo) && rows_touch(qi, qo)) return KVT_ERR_INVALID_ARG;
+    if (covers_positions(qo, rotary)) return KVT_ERR_INVALID_ARG;
     a.q = q->data;
     a.q_out = q_out->data;
     a.q_stride = q->stride;

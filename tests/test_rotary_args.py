@@ -100,6 +100,18 @@ def test_append_rotary_rejects_bad_rows():
 
 
 @no_gpu_only
+def test_outputs_over_the_positions_are_rejected():
+    """16 tokens of 4 heads of 64 are 8192 bytes; positions of two axes 128 bytes."""
+    for at, bad in ((POS, True), (POS + 112, True), (POS - 8192 + 16, True), (POS + 128, False), (POS - 8192, False)):
+        r = Rot(axes=2)
+        st = rotate(r, out=rows(at, 256))
+        assert (st == E) == bad, hex(at)
+        st = append(r, q=rows(FAKE_K + (1 << 36), 256), hq=4, qo=rows(at, 256),
+                    seqs=kvt.RawSeqs([240], [16], FAKE_BT, 16, [[64] * 16]))
+        assert st == (E if bad else kvt.KVT_ERR_OUT_OF_RANGE), hex(at)
+
+
+@no_gpu_only
 def test_append_rotary_rejects_bad_sequences_and_pools():
     r = Rot()
     assert append(r, pool=kvt.raw_pool(FAKE_K, FAKE_V, 64, 1, 96, 0)) == U
