@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
     typename std::conditional<S::kBf16, u32x4, float>::type w[KG];
   };
   typedef typename std::conditional<S::kBf16, bf16x8, float>::type VFrag;
-  // rings of two K and two V tiles; distinct objects, so that the compiler can
+  // rings of four K and four V tiles; distinct objects, so that the compiler can
   // tell the page gather into one from the operand reads of another
   __shared__ __attribute__((aligned(1024))) HalfTile<T, D> k0, k1, k2, k3, v0, v1, v2, v3;
   __shared__ float row_sum[kDiffTileRows];   // of the second map, for the epilogue

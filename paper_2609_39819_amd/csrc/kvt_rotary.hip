@@ -16,13 +16,14 @@
 // becomes fp32; sine and cosine of it are those of sincospif.  The rotation is
 // fp32, rounded once to the storage type.
 //
-// One launch moves q, K and V of a token: a workgroup holds a few tokens by up to
-// eight heads.  The lanes of a token form its sines and cosines between them,
-// share them through LDS, keep those of their own columns in registers and go
-// through the heads in steps of eight.  Bound by HBM (by the launch for a
-// decoding step): 24576 tokens on three axes, 24 heads of 128, 45.5 us, 6.6 TB/s
-// (65 us with every lane forming its own sines); 14336 new tokens behind a fused
-// projection, 96/8 heads, 162 us, 5.1 TB/s.
+// One launch moves q, K and V of a token.  The lanes of a token form its sines and
+// cosines between them, share them through LDS, keep those of their own columns in
+// registers and take two rows each, all in flight at once: a workgroup reads and
+// writes whole tokens, about 24 KB of consecutive bytes each way.  (Eight heads of
+// four tokens at a time, four rows in flight per lane: 14336 tokens behind a fused
+// projection, 96/8 heads, 162.5 us, 139.4 so; 24576 tokens of 24 heads 55.2 and
+// 52.9, inputs not in a cache.)  Bound by HBM: 5.9 and 5.7 TB/s in these two, a plain
+// copy of as many bytes 5.4; by the launch for a decoding step.
 #include <algorithm>
 
 #include "kvt_device.h"
@@ -33,9 +34,8 @@ namespace {
 
 using namespace dev;
 
-constexpr int kThreads = 256;
-constexpr int kHeadLanes = 8;   // heads that a workgroup holds at a time, at most
-constexpr int kAhead = 4;       // heads per lane whose loads are in flight together
+constexpr int kThreads = 512;
+constexpr int kAhead = 2;   // heads per lane whose loads are in flight together
 
 // Eight consecutive elements of a row, as stored.
 template <typename T>
@@ -51,9 +51,9 @@ __device__ __forceinline__ Piece<T> load_piece(const T* p) {
   return r;
 }
 // bf16 pieces go out with the nontemporal policy (24576 tokens of 24 heads of 128:
-// 52.9 us without, 45.5 with); an fp32 piece is two stores that share 32 bytes,
+// 55.7 us without, 52.8 with); an fp32 piece is two stores that share 32 bytes,
 // which need the cache to join them (8192 tokens of 32/8 heads of 64: 34.4 and
-// 42.4 us).  Loads are ordinary ones (nontemporal: 45.5 -> 50 us).
+// 42.4 us).  Loads are ordinary ones (nontemporal 10 % slower).
 template <typename T>
 __device__ __forceinline__ void store_piece(T* p, const Piece<T>& x) {
   if constexpr (sizeof(T) == 2) {
@@ -213,8 +213,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a) {
 template <typename T, int D>
 void launch_as(RotaryArgs& a, int cus, hipStream_t stream) {
   const int64_t jobs = a.num_q_heads + 2 * (int64_t)a.num_kv_heads;
-  a.head_lanes = 1;   // no more lanes than there are heads
-  while (a.head_lanes < kHeadLanes && a.head_lanes < jobs) a.head_lanes *= 2;
+  a.head_lanes = 1;   // a token's rows in one go, as far as the workgroup's lanes reach
+  while (a.head_lanes * kAhead < jobs && a.head_lanes < kThreads / (D / 16)) a.head_lanes *= 2;
   const int64_t tokens = kThreads / (D / 16 * a.head_lanes);
   const int64_t tiles = (a.rows + tokens - 1) / tokens, steps = (jobs + a.head_lanes - 1) / a.head_lanes;
   // few tokens: the heads are spread over workgroups until there are four per CU
