@@ -36,7 +36,7 @@
 //
 // What bounds it: the matrix cores with the softmax and the barriers beside them.
 // A tile of 64 keys, heads of 128, takes 56 MFMAs of 32 cycles per SIMD (1792) and
-// 250 other vector instructions (1300); it lasts 3060 cycles (1.275 us) with 8
+// 270 other vector instructions (1340); it lasts 3060 cycles (1.275 us) with 8
 // workgroups on the chip and 1.55 us with all CUs busy, at the clock that the board
 // then holds.  2048 new tokens over 131072, 32/8 heads of 128: 6.55 ms, 7.8e12
 // operations, 1180 TFLOP/s (a large bf16 matrix product 1262).  512 over 8192:
