@@ -50,6 +50,7 @@
 // another: in the tiles that reach past some row's limit a non-finite value is
 // looked for first, and if there is one it is added to the rows that see it by
 // hand and replaced by 0 for the product.
+#include <algorithm>
 #include <type_traits>
 
 #include "kvt_diff_device.h"
@@ -612,20 +613,22 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
 
 // Joins the key splits of each row (fixed order): with m* = max_s m_s and
 // w_s = 2^(m_s - m*), map m is sum_s w_s O_s / sum_s w_s l_s; then the maps'
-// difference and its norm as in the kernel's own epilogue.  D/4 lanes per row,
-// four columns each; the weights of the splits are formed once per row, one
-// split per lane, and shared through LDS.  Every split is multiplied by its
-// weight, be it 0, so an infinity or a NaN among the values gives the unsplit
-// call's.  args: the sequences with more than one split; unit_begin counts
-// their rows.
+// difference and its norm as in the kernel's own epilogue.  A group of D/4 lanes
+// holds a row, four columns a lane (GROUPS > 1: that many groups share the row's
+// splits, and a workgroup holds one row); the weights of the splits are formed once
+// per row, one split per lane, and shared through LDS.  Every split is multiplied by
+// its weight, be it 0, so an infinity or a NaN among the values gives the unsplit
+// call's.  args: the sequences with more than one split; unit_begin counts their
+// rows.
 constexpr int kAhead = 4;   // splits whose pieces are in flight at once, the first from before the weights are known
 
-template <typename T, int D>
+template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
-  constexpr int Q4 = D / 4, ROWS = 256 / Q4;       // lanes per row, rows per workgroup
+  constexpr int Q4 = D / 4, ROWS = 256 / Q4 / GROUPS;   // lanes of a group, rows per workgroup
   constexpr int PER = (kMaxPartials + Q4 - 1) / Q4;
   __shared__ float wts[ROWS][2][kMaxPartials];
-  const int lr = threadIdx.x / Q4, lq = threadIdx.x % Q4;
+  __shared__ f32x4 part[GROUPS > 1 ? GROUPS : 1][2][Q4];
+  const int lr = threadIdx.x / (Q4 * GROUPS), grp = threadIdx.x / Q4 % GROUPS, lq = threadIdx.x % Q4;
   const int total = a.unit_begin[a.nseq];
   const int idx = blockIdx.x * ROWS + lr;
   const bool live = idx < total;
@@ -643,11 +646,15 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
   auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (s0 + i < nsplit)
+      if (s0 + i * GROUPS < nsplit)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) v[i][x] = load4(po + ((s0 + i) * rows * 2 + x) * D);
+        for (int x = 0; x < 2; ++x) v[i][x] = load4(po + ((s0 + i * GROUPS) * rows * 2 + x) * D);
   };
-  load(0);
+  load(grp);
+  const int token = sd.row_off + local / a.num_q_heads, head = local % a.num_q_heads;
+  const float lam = a.lambda[(int64_t)token * a.lambda_stride + head];
+  f32x4 w = {1.f, 1.f, 1.f, 1.f};
+  if (a.norm_weight != nullptr) w = load4(a.norm_weight + lq * 4);
   float m[2][PER], l[2][PER], top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
@@ -667,37 +674,43 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int s = lq + k * Q4;
-      const float w = (m[x][k] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m[x][k] - top[x]);
-      sum[x] += w * l[x][k];
-      if (s < nsplit) wts[lr][x][s] = w;
+      const float ws = (m[x][k] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m[x][k] - top[x]);
+      sum[x] += ws * l[x][k];
+      if (s < nsplit && grp == 0) wts[lr][x][s] = ws;
     }
 #pragma unroll
     for (int d = Q4 / 2; d > 0; d >>= 1) sum[x] += __shfl_xor(sum[x], d);
   }
   __syncthreads();
   f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  for (int s0 = 0; s0 < nsplit; s0 += kAhead) {
-    if (s0 > 0) load(s0);
+  for (int s0 = grp; s0 < nsplit; s0 += kAhead * GROUPS) {
+    if (s0 >= GROUPS) load(s0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (s0 + i < nsplit)
+      if (s0 + i * GROUPS < nsplit)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) acc[x] += wts[lr][x][s0 + i] * v[i][x];
+        for (int x = 0; x < 2; ++x) acc[x] += wts[lr][x][s0 + i * GROUPS] * v[i][x];
   }
-  const int token = sd.row_off + local / a.num_q_heads, head = local % a.num_q_heads;
-  const float lam = a.lambda[(int64_t)token * a.lambda_stride + head];
+  if constexpr (GROUPS > 1) {   // one row: the groups' shares, in order
+#pragma unroll
+    for (int x = 0; x < 2; ++x) part[grp][x][lq] = acc[x];
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) acc[x] += part[i][x][lq];
+  }
   const float inv0 = 1.0f / sum[0], inv1 = 1.0f / sum[1];
   f32x4 y;
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = map_difference(acc[0][i], inv0, acc[1][i], inv1, lam);
   float scale = a.out_scale;
-  f32x4 w = {1.f, 1.f, 1.f, 1.f};
   if (a.norm_weight != nullptr) {
     float sq = y[0] * y[0] + y[1] * y[1] + y[2] * y[2] + y[3] * y[3];
 #pragma unroll
     for (int d = Q4 / 2; d > 0; d >>= 1) sq += __shfl_xor(sq, d);
     scale *= 1.0f / __builtin_sqrtf(sq * (1.0f / D) + a.eps);
-    w = load4(a.norm_weight + lq * 4);
   }
   if (!live) return;
   y *= scale;
@@ -707,9 +720,15 @@ __global__ __launch_bounds__(256) void diff_combine_kernel(const DiffArgs a) {
 
 template <typename T, int D>
 void combine_as(const DiffArgs& a, hipStream_t stream) {
-  const int64_t per = 256 / (D / 4);
-  hipLaunchKernelGGL((diff_combine_kernel<T, D>), dim3((unsigned)((a.unit_begin[a.nseq] + per - 1) / per)), dim3(256), 0,
-                     stream, a);
+  constexpr int kGroups = 256 / (D / 4);
+  const int rows = a.unit_begin[a.nseq], splits = *std::max_element(a.nsplit, a.nsplit + a.nseq);
+  // a whole workgroup per row pays where a chain of loads is what a row waits for:
+  // decode, 96 rows of 22 splits 90.2 us a call with a group per row, 87.5 so; 32 of
+  // 22 17.5 and 15.1; extend, 512 rows of 32 34.2 and 33.0; but 1024 rows of 8 29.6 and
+  // 30.3, 2144 of 11 81.1 and 84.7
+  const bool wide = splits > 2 * kAhead && rows <= 1024;
+  if (wide) hipLaunchKernelGGL((diff_combine_kernel<T, D, kGroups>), dim3(rows), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((diff_combine_kernel<T, D, 1>), dim3((rows + kGroups - 1) / kGroups), dim3(256), 0, stream, a);
 }
 
 }  // namespace
