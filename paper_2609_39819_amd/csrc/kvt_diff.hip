@@ -442,8 +442,9 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   // ---- main loop: step t takes tile t.  K of tile t+3 and V of tile t+2 start to
   // stream in, each into the slot that the step before was done with (past the
   // last tile the gather reads clamped, in-bounds pages into slots no one reads).
-  // The barrier at the end waits for them too: a step is longer than a load takes,
-  // and a barrier that left them in flight measured the same.
+  // They are waited for before the barrier at the end (each wave counts its own loads
+  // only): a step is longer than a load takes, and a barrier that left them in flight
+  // measured the same.
   // bf16: the scores of a tile's first half come from the step before, and the
   // value product of its second half is left to the step after.
   uint32_t id2 = page_id(j0 + 2), id3 = page_id(j0 + 3);   // pages of tiles t+2, t+3
@@ -464,6 +465,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
 #pragma unroll
     for (int i = 0; i < VPIECES; ++i) reinterpret_cast<u32x4*>(v3.e)[tid + kThreads * i] = (u32x4){0u, 0u, 0u, 0u};
   }
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   __syncthreads();
   if (S::kBf16 && n > 0 && !idle) {
     score_block(k0, 0, s0);
@@ -511,6 +513,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
         value_block(v_cur, 0, p0, std::false_type());
       }
     }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __syncthreads();
   };
   for (int t = 0; t < n; t += 4) {
