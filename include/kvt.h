@@ -346,11 +346,10 @@ typedef struct {
  * no row is empty.  Infinities and NaN in V reach the rows that see them and no
  * others; a non-finite key leaves the rows that see it unspecified.
  *
- * bf16 inputs feed bf16 MFMA, the probabilities rounded to bf16 for the value
- * product (those of the first 16 of every 64 keys, and all of
- * kvt_diff_decode_attention's, given as the sum of two bf16 numbers); fp32
- * inputs run fp32 MFMA (unlike the other attention calls, which round them to
- * bf16: here the difference of two maps would keep that error).  Softmax
+ * bf16 inputs feed bf16 MFMA, each probability given to the value product as the
+ * sum of two bf16 numbers, so that the maps' difference keeps no rounding of theirs;
+ * fp32 inputs run fp32 MFMA (the other attention calls round probabilities, and fp32
+ * inputs, to bf16: here the difference of two maps would keep that error).  Softmax
  * statistics, accumulation and the norm are fp32.
  *
  * Other arguments, alignments and errors as for kvt_extend_attention (there

@@ -13,35 +13,34 @@
 // rows, key split), as the extend kernel's (row r = token r/G, head g*G + r%G);
 // 8 waves, two per SIMD: waves 2 i and 2 i + 1 take the two maps of 32 rows each,
 // on the K/V tiles that all of them share in LDS.  Row tiles of up to 64 rows
-// then have a wave per SIMD (16 new tokens over 30000, 32/8 heads of 128, 34.1 us;
-// with the maps four waves apart 37.7).  A wave with both maps would read each V
-// fragment once for two products, but its two outputs leave no registers to read
-// operands ahead (96/8 heads of 128, 1024 new tokens over 32768, 2.38 and 2.31 ms).
+// then have a wave per SIMD (16 new tokens over 30000, 32/8 heads of 128, with one bf16
+// number per probability 34.1 us; with the maps four waves apart 37.7).  A wave with
+// both maps would read each V fragment once for both, but its two outputs leave no
+// registers to read operands ahead (96/8 heads of 128, 1024 new tokens over 32768, one
+// number per probability, 2.38 and 2.31 ms).
 // S^T = K Q^T (keys on the MFMA rows, queries on the columns), so a query's scores
 // sit in one lane pair (l, l+32) and leave the accumulators in the layout that the
 // value product takes them in.  At the end the second map's waves hand their rows
 // over through LDS and the first map's form the difference and the norm; a key
 // split writes both maps' rows as they are, for the joining launch.
 //
-// bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys.  The value product
-// takes the probabilities in bf16, and the maps' difference keeps both maps'
-// roundings.  The first 16 of a tile's 64 keys hand theirs over as two bf16 numbers
-// (both count in the sum; the other 48 count as rounded), which is a quarter more
-// value products: the result is off by 2.38e-3 of itself (2-norm; a bf16 result of
-// exact weights 1.66e-3).  With one number for every key it is 2.57e-3, 1.55 times
-// the exact weights', and a call takes 8 to 12 % less; with two for every key, as the
-// decode kernel has them, a call takes a quarter to a third more.
-// fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded (the
-// difference of two maps keeps the error of the larger one).
+// bf16 storage: v_mfma_f32_32x32x16_bf16, tiles of 64 keys.  The value product takes
+// each probability as two bf16 numbers, as the decode kernel's does: what y's two sums
+// share goes, what the probabilities were rounded by would stay.  The result is then
+// off by its own last rounding (2-norm, 1.66e-3 of itself).  One number each, 2^-8 of
+// a probability off, leaves 2.56e-3 where the maps have nothing in common, and 1.7e-2
+// where their keys differ by an eighth and lambda is 0.9 to 1; it saves a quarter of
+// a call.  One number for most keys and two for some is no middle way: the error is
+// then that of the keys which the weight happens to lie on.
+// fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded.
 //
 // What bounds it: the matrix cores with the softmax and the barriers beside them.
-// A tile of 64 keys, heads of 128, takes 56 MFMAs of 32 cycles per SIMD (1792) and
-// 270 other vector instructions (1340); it lasts 3060 cycles (1.275 us) with 8
-// workgroups on the chip and 1.55 us with all CUs busy, at the clock that the board
-// then holds.  2048 new tokens over 131072, 32/8 heads of 128: 6.55 ms, 7.8e12
-// operations, 1180 TFLOP/s (a large bf16 matrix product 1262).  512 over 8192:
-// 125 us, 990 TFLOP/s.  fp32, 512 over 8192: 801 us, 133 TFLOP/s (a large fp32
-// matrix product 153).
+// A tile of 64 keys, heads of 128, takes 80 MFMAs of 32 cycles per SIMD (2560); with
+// some 400 other vector instructions it lasts 4060 cycles (1.69 us) with 8 workgroups
+// on the chip and 2.15 us with all CUs busy, at the clock that the board then holds.
+// 2048 new tokens over 131072, 32/8 heads of 128: 8.7 ms, 11.1e12 operations, 1270
+// TFLOP/s (a large bf16 matrix product 1262).  512 over 8192: 160 us.  fp32, 512 over
+// 8192: 797 us, 133 TFLOP/s (a large fp32 matrix product 153).
 //
 // Masked positions.  Their scores are replaced by -inf, so their weight is
 // exactly 0 whatever K holds; positions past the end of the sequence and unused
@@ -127,8 +126,7 @@ struct Queries<float, D> {
 };
 
 // bf16 heads of 64 hold to 128 registers and share a CU between two workgroups
-// (4096 new tokens over 16384, 32/8 heads, one bf16 number per probability: 1155 us
-// one to a CU, 1036 two).
+// (4096 new tokens over 16384, 32/8 heads: 1650 us one to a CU, 1480 two).
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void diff_extend_kernel(const DiffArgs a) {
   using S = Shape<T, D>;
@@ -139,8 +137,10 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   constexpr int KG = S::kBf16 ? 2 : 16;                           // key groups of the value product over 32 keys
   constexpr float kRescaleSlack = 8.0f;                           // log2 headroom before O is rescaled
   constexpr float kSumLimit = 65536.0f;                           // a lane's sum of probabilities over 32 keys
-  struct Probs {   // B operands of the value product over 32 keys
+  constexpr float kOver = S::kBf16 ? 1.0f + 0x1p-8f : 1.0f;       // what the value product multiplies by, of the probability
+  struct Probs {   // B operands of the value product over 32 keys; bf16: a probability is w + rest
     typename std::conditional<S::kBf16, u32x4, float>::type w[KG];
+    u32x4 rest[S::kBf16 ? KG : 1];
   };
   typedef typename std::conditional<S::kBf16, bf16x8, float>::type VFrag;
   // rings of four K and four V tiles; distinct objects, so that the compiler can
@@ -281,34 +281,27 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
     return alpha;
   };
   // ---- probabilities of 32 keys as B operands of the value product; returns their
-  // sum.  split: the first 16 keys' are cut off to bf16 and what is cut off goes into
-  // `rest` (2^-20 of the probability more, so that an infinite value times both
-  // parts stays one).
-  Probs rest;
-  auto probs = [&](const f32x16& s, Probs& p, float neg, auto split) __attribute__((always_inline)) {
+  // sum.  bf16: w is the probability cut off to bf16, the rest what is cut off and 2^-8
+  // of the probability more, so that it is never 0 where w is not, and an infinite value
+  // times both stays one; both together are kOver times the probability (off by 2^-14 of
+  // it at most), which the sum is multiplied by in the end.
+  auto probs = [&](const f32x16& s, Probs& p, float neg) __attribute__((always_inline)) {
     float rs = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
       const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, neg));
       const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, neg));
       if constexpr (S::kBf16) {
-        if (decltype(split)::value && i < 8) {
-          const unsigned u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-          const float r0 = __builtin_fmaf(p0, 1.0f + 0x1p-20f, -__uint_as_float(u0 & 0xffff0000u));
-          const float r1 = __builtin_fmaf(p1, 1.0f + 0x1p-20f, -__uint_as_float(u1 & 0xffff0000u));
-          p.w[0][i / 2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);   // both upper halves
-          rest.w[0][i / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){r0, r1}, bf16x2));
-          rs += p0 + p1;
-          continue;
-        }
-        const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-        rs = __builtin_amdgcn_fdot2_f32_bf16(pp, (bf16x2){(__bf16)1.0f, (__bf16)1.0f}, rs, false);
-        p.w[i / 8][i % 8 / 2] = __builtin_bit_cast(unsigned, pp);
+        const unsigned u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+        const float r0 = __builtin_fmaf(p0, kOver, -__uint_as_float(u0 & 0xffff0000u));
+        const float r1 = __builtin_fmaf(p1, kOver, -__uint_as_float(u1 & 0xffff0000u));
+        p.w[i / 8][i % 8 / 2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);   // both upper halves
+        p.rest[i / 8][i % 8 / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){r0, r1}, bf16x2));
       } else {
         p.w[i] = p0;
         p.w[i + 1] = p1;
-        rs += p0 + p1;
       }
+      rs += p0 + p1;
     }
     return rs;
   };
@@ -344,6 +337,10 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
     if constexpr (S::kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p.w[kg]), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p.w[kg], acc, 0, 0, 0);
   };
+  auto rest_product = [&](VFrag vf, const Probs& p, int kg, f32x16 acc) __attribute__((always_inline)) {
+    if constexpr (S::kBf16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p.rest[kg]), acc, 0, 0, 0);
+    else return acc;
+  };
 
   // ---- non-finite values in a V tile with masked positions (see the top) become
   // 0 there; any_odd (workgroup-uniform) remembers it
@@ -377,7 +374,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
 #pragma unroll
     for (int k = 0; k < QK; ++k) s = score_product(read_k(tl, k, half), k, s);
   };
-  auto value_block = [&](const HalfTile<T, D>& tl, int half, const Probs& p, auto split) __attribute__((always_inline)) {
+  auto value_block = [&](const HalfTile<T, D>& tl, int half, const Probs& p) __attribute__((always_inline)) {
 #pragma unroll
     for (int kg = 0; kg < KG; ++kg) {
       VFrag vf[DT];
@@ -386,18 +383,17 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
         vf[dt] = read_v(tl, half, kg, dt);
         o[dt] = value_product(vf[dt], p, kg, o[dt]);
       }
-      if (!decltype(split)::value || kg > 0) continue;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = value_product(vf[dt], rest, 0, o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = rest_product(vf[dt], p, kg, o[dt]);
     }
   };
   // whether the probabilities p of the scores s hold; rs: their sum.  Where the
   // reference is not set yet, or some score passed it by far, or is a NaN, they
   // are done again from the row maxima (a row that still sees nothing has weights 0).
-  auto check = [&](const f32x16& s, Probs& p, float rs, auto split) __attribute__((always_inline)) {
+  auto check = [&](const f32x16& s, Probs& p, float rs) __attribute__((always_inline)) {
     if (__builtin_amdgcn_ballot_w64(!(rs < kSumLimit)) != 0) {
       const float alpha = settle(s);
-      rs = probs(s, p, m_ref == -INFINITY ? 0.f : -m_ref, split);
+      rs = probs(s, p, m_ref == -INFINITY ? 0.f : -m_ref);
       l_run *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
@@ -410,12 +406,10 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   // in the turn before (kf; kt, khalf is the block of the turn after), so that a
   // turn's first products have nothing to wait for (4 % of a tile).  With heads of
   // 64, whose scores take two products, that costs 5 %: kt, khalf is this turn's block.
-  // first: `cur` is a tile's first half (its probabilities are split, those of the
-  // value product's half, a second one, are not).
   constexpr bool kReadAhead = D == 128;
   u32x4 kf[QK];
   auto turn = [&](const HalfTile<T, D>& kt, int khalf, const f32x16& cur, f32x16& next, const HalfTile<T, D>& vt, int vhalf,
-                  const Probs& prev, Probs& out, auto first) __attribute__((always_inline)) {
+                  const Probs& prev, Probs& out) __attribute__((always_inline)) {
     if constexpr (kReadAhead) {
       next = (f32x16){};
 #pragma unroll
@@ -423,20 +417,20 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
     } else {
       score_block(kt, khalf, next);
     }
-    value_block(vt, vhalf, prev, std::bool_constant<!decltype(first)::value>());
+    value_block(vt, vhalf, prev);
     if constexpr (kReadAhead) {
 #pragma unroll
       for (int k = 0; k < QK; ++k) kf[k] = read_k(kt, k, khalf);
     }
-    const float rs = probs(cur, out, m_neg, first);
+    const float rs = probs(cur, out, m_neg);
     // after each product two operand reads and a share of the softmax
 #pragma unroll
-    for (int i = 0; i < QK + KG * DT + (decltype(first)::value ? 0 : DT); ++i) {
+    for (int i = 0; i < QK + 2 * KG * DT; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       __builtin_amdgcn_sched_group_barrier(0x002, kReadAhead ? 2 : 8, 0);
     }
-    check(cur, out, rs, first);
+    check(cur, out, rs);
   };
 
   // ---- main loop: step t takes tile t.  K of tile t+3 and V of tile t+2 start to
@@ -461,7 +455,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   if constexpr (S::kBf16) {
     // nothing before the first tile: probabilities and values of 0
 #pragma unroll
-    for (int i = 0; i < KG; ++i) p1.w[i] = (u32x4){0u, 0u, 0u, 0u};
+    for (int i = 0; i < KG; ++i) p1.w[i] = p1.rest[i] = (u32x4){0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < VPIECES; ++i) reinterpret_cast<u32x4*>(v3.e)[tid + kThreads * i] = (u32x4){0u, 0u, 0u, 0u};
   }
@@ -497,20 +491,20 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
           asm volatile("");
           mask((j0 + t) * KT, s0);
         }
-        turn(kReadAhead ? k_next : k_cur, kReadAhead ? 0 : 1, s0, s1, v_prev, 1, p1, p0, std::true_type());
+        turn(kReadAhead ? k_next : k_cur, kReadAhead ? 0 : 1, s0, s1, v_prev, 1, p1, p0);
         if (t >= masked) {
           asm volatile("");
           mask((j0 + t) * KT + 32, s1);
         }
-        turn(k_next, kReadAhead ? 1 : 0, s1, s0, v_cur, 0, p0, p1, std::false_type());
+        turn(k_next, kReadAhead ? 1 : 0, s1, s0, v_cur, 0, p0, p1);
       } else {
         score_block(k_cur, 0, s0);
         if (t >= masked) {
           asm volatile("");
           mask((j0 + t) * KT, s0);
         }
-        check(s0, p0, probs(s0, p0, m_neg, std::false_type()), std::false_type());
-        value_block(v_cur, 0, p0, std::false_type());
+        check(s0, p0, probs(s0, p0, m_neg));
+        value_block(v_cur, 0, p0);
       }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -527,7 +521,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   }
   if (S::kBf16 && n > 0 && !idle) {
     const HalfTile<T, D>& v_last = (n & 3) == 1 ? v0 : (n & 3) == 2 ? v1 : (n & 3) == 3 ? v2 : v3;
-    value_block(v_last, 1, p1, std::false_type());
+    value_block(v_last, 1, p1);
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   // what drop_odd left out: the rows that see such a value get it by hand
@@ -549,7 +543,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   }
 
   // ---- epilogue
-  const float l_tot = pair_sum(l_run);
+  const float l_tot = pair_sum(l_run) * kOver;
   if (nsplit > 1) {
     if (!row_valid) return;
     const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;
