@@ -137,7 +137,6 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   constexpr int KG = S::kBf16 ? 2 : 16;                           // key groups of the value product over 32 keys
   constexpr float kRescaleSlack = 8.0f;                           // log2 headroom before O is rescaled
   constexpr float kSumLimit = 65536.0f;                           // a lane's sum of probabilities over 32 keys
-  constexpr float kOver = S::kBf16 ? 1.0f + 0x1p-8f : 1.0f;       // what the value product multiplies by, of the probability
   struct Probs {   // B operands of the value product over 32 keys; bf16: a probability is w + rest
     typename std::conditional<S::kBf16, u32x4, float>::type w[KG];
     u32x4 rest[S::kBf16 ? KG : 1];
@@ -281,10 +280,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
     return alpha;
   };
   // ---- probabilities of 32 keys as B operands of the value product; returns their
-  // sum.  bf16: w is the probability cut off to bf16, the rest what is cut off and 2^-8
-  // of the probability more, so that it is never 0 where w is not, and an infinite value
-  // times both stays one; both together are kOver times the probability (off by 2^-14 of
-  // it at most), which the sum is multiplied by in the end.
+  // sum
   auto probs = [&](const f32x16& s, Probs& p, float neg) __attribute__((always_inline)) {
     float rs = 0.f;
 #pragma unroll
@@ -292,11 +288,10 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
       const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, neg));
       const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], c, neg));
       if constexpr (S::kBf16) {
-        const unsigned u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-        const float r0 = __builtin_fmaf(p0, kOver, -__uint_as_float(u0 & 0xffff0000u));
-        const float r1 = __builtin_fmaf(p1, kOver, -__uint_as_float(u1 & 0xffff0000u));
-        p.w[i / 8][i % 8 / 2] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);   // both upper halves
-        p.rest[i / 8][i % 8 / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){r0, r1}, bf16x2));
+        unsigned w, rest;
+        two_numbers(p0, p1, w, rest);
+        p.w[i / 8][i % 8 / 2] = w;
+        p.rest[i / 8][i % 8 / 2] = rest;
       } else {
         p.w[i] = p0;
         p.w[i + 1] = p1;
@@ -543,7 +538,7 @@ __global__ __launch_bounds__(kThreads, (D == 64 && sizeof(T) == 2) ? 4 : 2) void
   }
 
   // ---- epilogue
-  const float l_tot = pair_sum(l_run) * kOver;
+  const float l_tot = pair_sum(l_run) * (S::kBf16 ? kOver : 1.0f);
   if (nsplit > 1) {
     if (!row_valid) return;
     const int64_t rows = (int64_t)sd.suffix * a.num_q_heads;

@@ -13,10 +13,8 @@
 //   * at the end the four waves' (m, l, O) merge through LDS; the merged row is
 //     either turned into the output there (difference of the maps, norm) or a
 //     partial of its key split.
-// bf16 storage hands the value product each probability as two bf16 numbers, the
-// rounded one and the rest rounded, so nothing of it is lost (the difference of
-// two maps would keep the error of one rounding: 2.56e-3 of the result against
-// 1.66e-3, which is the result's own rounding); beside a stream bound by HBM the
+// bf16 storage hands the value product each probability as two bf16 numbers, as the
+// extend kernel's and for its reason; beside a stream bound by HBM the
 // second product costs at most 1.5 % of a step (64 contexts of 1024..16384 keys,
 // heads of 128, 247.4 -> 248.5 us, of 64 124.1 -> 126.0).  fp32 storage runs fp32
 // matrix products throughout; at 25 GB/s a workgroup they bound it (5.4 TB/s on a
@@ -167,8 +165,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
   const int rsel = (lane & 15) >> 2;
 
   // ---- one 32-key tile starting at key kb: scores, softmax, value product
-  // (FINE: with the rests of the probabilities)
-  auto tile = [&](const DecSlot<T, D>& sl, int kb, auto FINE) __attribute__((always_inline)) {
+  auto tile = [&](const DecSlot<T, D>& sl, int kb) __attribute__((always_inline)) {
     f32x16 s = (f32x16){};
 #pragma unroll
     for (int kk = 0; kk < KF; ++kk) {
@@ -208,12 +205,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
         for (int q2 = 0; q2 < 4; ++q2) {
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kg * 8 + 2 * q2], c, -m_use));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kg * 8 + 2 * q2 + 1], c, -m_use));
-          const bf16x2 pp = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-          const unsigned w = __builtin_bit_cast(unsigned, pp);
-          const float l0 = p0 - __builtin_bit_cast(float, w << 16), l1 = p1 - __builtin_bit_cast(float, w & 0xffff0000u);
-          lv[q2] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){l0, l1}, bf16x2));
-          rs += p0 + p1;
+          unsigned w, rest;
+          two_numbers(p0, p1, w, rest);
           wv[q2] = w;
+          lv[q2] = rest;
+          rs += p0 + p1;
         }
         const bf16x8 pb = __builtin_bit_cast(bf16x8, wv), pl = __builtin_bit_cast(bf16x8, lv);
 #pragma unroll
@@ -228,7 +224,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
           }
           const bf16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
-          if constexpr (FINE) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl, o[dt], 0, 0, 0);
         }
       }
     } else {
@@ -255,36 +251,23 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
   // stores follow the reads of the tile before).
   DecSlot<T, D>& mine = ring[wave];
   auto jt = [&](int i) { return j0 + wave + kWaves * i; };
-  auto stream = [&](auto FINE) __attribute__((always_inline)) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16){};
-    m_ref = -INFINITY, l_run = 0.f;
-    Stage st;
-    uint32_t ids[2];
-    if (nt > 0) {
-      page_ids(jt(0), ids);
-      load_tile(jt(0), ids, st);
-      page_ids(jt(1), ids);
+  for (int dt = 0; dt < DT; ++dt) o[dt] = (f32x16){};
+  m_ref = -INFINITY, l_run = 0.f;
+  Stage st;
+  uint32_t ids[2];
+  if (nt > 0) {
+    page_ids(jt(0), ids);
+    load_tile(jt(0), ids, st);
+    page_ids(jt(1), ids);
+  }
+  for (int i = 0; i < nt; ++i) {
+    stash(jt(i), st, mine);
+    if (i + 1 < nt) {
+      load_tile(jt(i + 1), ids, st);
+      page_ids(jt(i + 2), ids);
     }
-    for (int i = 0; i < nt; ++i) {
-      stash(jt(i), st, mine);
-      if (i + 1 < nt) {
-        load_tile(jt(i + 1), ids, st);
-        page_ids(jt(i + 2), ids);
-      }
-      tile(mine, jt(i) * kTK, FINE);
-    }
-  };
-  stream(std::true_type{});
-  if constexpr (kBf16) {
-    // a rest can be 0 or negative, and such a multiple of an infinite value is not
-    // what its probability makes of it: a NaN is looked at again without the rests
-    bool odd = false;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) odd = odd || o[dt][e] != o[dt][e];
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) != 0, 0)) stream(std::false_type{});
+    tile(mine, jt(i) * kTK);
   }
 
   // ---- merge the four waves.  Each wave parks its O rows in its own slot (its
@@ -292,7 +275,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) * D > 256 ? 1 : 2) void diff
   // order), four columns a piece, the pieces of a row XOR-swizzled by the row.
   static_assert(sizeof(DecSlot<T, D>) >= 32 * D * sizeof(float), "merge buffer");
   constexpr int Q4 = D / 4;
-  const float l_tot = pair_sum(l_run);
+  const float l_tot = pair_sum(l_run) * (kBf16 ? kOver : 1.0f);
   f32x4* ow = reinterpret_cast<f32x4*>(&mine);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)

@@ -102,6 +102,32 @@ def test_the_error_is_the_last_rounding(form, kind, d):
         assert got <= 1.05 * e0
 
 
+@pytest.mark.timeout(120)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("form", ["extend", "decode"])
+def test_a_non_finite_value_costs_the_other_columns_nothing(form, bad, d):
+    """Column 5 of one position that every row sees: the other columns are as exact as without it."""
+    b = case("maps nearly alike", [1437], [24 if form == "extend" else 1], d)
+    b.norm_host = b.norm = None      # a norm would take the column into every other
+    want, e0, _ = errors(b)
+    cols = torch.arange(d) != 5
+    want = want[..., cols]
+    e0 = float((want.bfloat16().double() - want).norm() / want.norm())
+    b.v_pool[int(b.table[0, 2]), :, 9, 5] = bad
+    for ws in (True, False):
+        if form == "extend":
+            out = kvt.diff_extend_attention(b.q, b.k_pool, b.v_pool, b.table, b.prefix, b.suffix, b.lam, b.scale,
+                                            **b.kw(), use_workspace=ws)
+        else:
+            out = kvt.diff_decode_attention(b.q, b.k_pool, b.v_pool, b.table, b.prefix, b.lam, b.scale, **b.kw(),
+                                            use_workspace=ws)
+        assert not torch.isfinite(out[..., 5]).any()
+        got = float((out[..., cols.cuda()].double().cpu() - want).norm() / want.norm())
+        say(f"{form} {bad} d={d}{'' if ws else ' unsplit'}: {got:.3e}, last rounding {e0:.3e}")
+        assert got <= 1.05 * e0
+
+
 @pytest.mark.timeout(60)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("form", ["extend", "decode"])
