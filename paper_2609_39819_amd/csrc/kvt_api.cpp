@@ -908,13 +908,15 @@ int diff_row_tiles(int32_t suffix, int group) {
 // first, one XCD's eighth of the units on its CUs; with many sequences the work
 // spread over the CUs and half a unit) and the merge: its partials at 4.5 TB/s and
 // a launch.  The best k is taken if it beats no split by more than 5 %.  Times are
-// in tiles of 64 keys: 1.28 us each with a few busy CUs, 1.55 with all (heads of
-// 128, bf16; of 64 1.1), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run two units
-// to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8 heads:
-// unsplit 309 us, 2 splits 279; 512 over 8192: 2 splits 90.7 us, 4 84.0).
+// in tiles of 64 keys: 1.69 us each with a few busy CUs, 2.15 with all (heads of
+// 128, bf16; of 64 1.36 and 1.45), 11 us in fp32 (of 64 5.5).  bf16 heads of 64 run
+// two units to a CU, together at 1.15 of one's rate (1024 new tokens over 16384, 32/8
+// heads: unsplit 415 us, 2 splits 377; 512 over 8192: 2 splits 115 us, 4 110).
 //
-// A last row tile of up to 64 rows has a wave per SIMD and takes 0.76 of a tile's
-// time (fp32 0.53); beside full ones it gets as many splits less.
+// A last row tile of up to 64 rows has a wave per SIMD and takes 0.63 (few busy CUs)
+// to 0.65 (all) of a tile's time (fp32 0.53); beside full ones it gets as many splits
+// less (67 over 30011, 32/8 heads of 128, charged with 0.66 of it 99.0 us, with 0.76
+// 101.4).
 DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   DiffPlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads, H = pool->num_kv_heads;
@@ -923,8 +925,8 @@ DiffPlan diff_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t nu
   p.nsplit.assign(B, 1);
   const bool pairs = pool->dtype == KVT_DTYPE_BF16 && pool->head_dim == 64;
   const double both = pairs ? 1.15 : 1.0;   // rate of a CU with two units
-  const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.1 : 1.4;
-  const double light = pool->dtype == KVT_DTYPE_BF16 ? 0.76 : 0.53;
+  const double tile_us = pool->dtype != KVT_DTYPE_BF16 ? 11.0 * pool->head_dim / 128 : pool->head_dim == 64 ? 1.4 : 1.9;
+  const double light = pool->dtype == KVT_DTYPE_BF16 ? 0.66 : 0.53;
   std::vector<int64_t> jobs(B), kt(B);   // jobs: full row tiles of all kv-heads
   std::vector<uint8_t> rest(B);          // whether a light one follows
   for (int i = 0; i < B; ++i) {
