@@ -408,6 +408,15 @@ def _on_device(t):
     return torch.cuda.device(t.device)
 
 
+def _on_stream(stream, t):
+    """Makes the stream that a call was given the current one.  One of another GPU than the call's tensors is refused:
+    the launches would go to whichever stream is current on the tensors' GPU."""
+    import torch
+    if stream.device != t.device:
+        raise ValueError(f"stream is on {stream.device}, the call's tensors are on {t.device}")
+    return torch.cuda.stream(stream)
+
+
 def rotate(x, positions, inv_freq, *, axis=None, interleaved: bool = False, parts: int = 1, out=None, stream=None):
     """Rotary positions of the rows of ``x`` [T][H][D] (``kvt_rotate``).
 
@@ -420,7 +429,7 @@ def rotate(x, positions, inv_freq, *, axis=None, interleaved: bool = False, part
     """
     import torch
     if stream is not None:   # out is allocated for the stream that it is written on
-        with torch.cuda.stream(stream):
+        with _on_stream(stream, x):
             return rotate(x, positions, inv_freq, axis=axis, interleaved=interleaved, parts=parts, out=out)
     if x.dim() != 3:
         raise ValueError("x must be [T][H][D]")
@@ -457,7 +466,7 @@ def append_kv_rotary(k_pool, v_pool, block_table, prefix_len: Sequence[int], suf
     """
     import torch
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on_stream(stream, k_pool):
             return append_kv_rotary(k_pool, v_pool, block_table, prefix_len, suffix_len, k_new, v_new, inv_freq,
                                     axis=axis, interleaved=interleaved, parts=parts, positions=positions, q=q,
                                     q_out=q_out, checked=checked)
@@ -700,7 +709,7 @@ def _diff_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, p
                     norm_weight, eps, out_scale, out, workspace, use_workspace, stream, checked):
     import torch
     if stream is not None:   # what is allocated here belongs to the stream that the kernels run on
-        with torch.cuda.stream(stream):
+        with _on_stream(stream, k_pool):
             return _diff_attention(entry, ws_entry, q, k_pool, v_pool, block_table, prefix_len, suffix_len, lam, scale,
                                    norm_weight, eps, out_scale, out, workspace, use_workspace, None, checked)
     native = _native()
