@@ -106,8 +106,9 @@ kvt_status kvt_append_kv(const kvt_pool* pool, const kvt_seqs* seqs,
 /* Rotary positions: pairs of columns (a, b) of a row turn by theta,
  *   a' = a cos theta - b sin theta,   b' = b cos theta + a sin theta,
  * with theta = positions[axis[j]][row] * inv_freq[j] for pair j of rot_dim/2.
- * theta is taken as that product of exact values, reduced in fp64, so far
- * positions lose nothing; the rotation is fp32, rounded once. */
+ * theta is formed and reduced in fp64 and off by at most 2^-23 + 2^-51 |theta|
+ * radians (positions up to 2^27 at one radian each lose nothing to fp32); the
+ * rotation is fp32, rounded once. */
 typedef struct {
   const float*   inv_freq;    /* HOST [rot_dim/2], finite: radians per position */
   const int32_t* axis;        /* HOST [rot_dim/2], each in [0,num_axes), or NULL: all on axis 0 */

@@ -11,10 +11,10 @@
 // Angles.  theta is needed modulo one turn, and far positions make it large:
 // 131071 * 1 rad in fp32 is off by up to 2^-8 rad.  The host turns each
 // frequency into turns per position in fp64, the kernel multiplies by the
-// position, takes off the whole turns in fp64 (off by at most 2^-53 of the
-// turns, 2^-22 turns at the largest position there is) and only the rest
-// becomes fp32; sine and cosine of it are those of sincospif.  The rotation is
-// fp32, rounded once to the storage type.
+// position and takes off the whole turns in fp64 (three roundings of 2^-53 of the
+// turns: under 2^-23 turns at one radian per position and the largest position
+// there is); only the rest becomes fp32 (2^-26 turns), and its sine and cosine are
+// those of sincospif.  The rotation is fp32, rounded once to the storage type.
 //
 // One launch moves q, K and V of a token.  The lanes of a token form its sines and
 // cosines between them, share them through LDS, keep those of their own columns in
