@@ -148,3 +148,21 @@ def test_an_infinite_value_of_any_weight_stays_one(form, d):
             out = kvt.diff_decode_attention(q, k, v, table, [n - 1], lam, math.log(2))
         assert float(out[0, 0, 3]) == math.inf, f"2^-{x}"
         assert torch.isfinite(out[0, 0, 4:]).all()
+
+
+@pytest.mark.timeout(60)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", ["extend", "decode"])
+def test_the_largest_value_stays_finite(form, d):
+    """One visible position whose values are the largest bf16 numbers: out is (1 - lambda) of them, rounded."""
+    top = float(torch.finfo(torch.bfloat16).max)
+    v = torch.full((1, 1, 16, d), top, device="cuda", dtype=torch.bfloat16)
+    v[..., ::3] = -top
+    q, k = torch.randn((1, 2, d), device="cuda").bfloat16(), torch.randn((1, 1, 16, d), device="cuda").bfloat16()
+    table, lam = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([0.25, 0.5], device="cuda")
+    if form == "extend":
+        out = kvt.diff_extend_attention(q, k, v, table, [0], [1], lam)
+    else:
+        out = kvt.diff_decode_attention(q, k, v, table, [0], lam)
+    want = v[0, 0, :1].double().cpu() * (1 - lam.double().cpu()[:, None])
+    assert bool(((out[0].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs()).all())
