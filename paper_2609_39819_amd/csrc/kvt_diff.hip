@@ -7,7 +7,7 @@
 //   out = out_scale * w * y / sqrt(mean(y^2) + eps)      (w given), else out_scale * y.
 // The sums of both softmaxes are known only after the last key, so one pass
 // over the keys keeps an output per map: 2 D flops per (head, key) for the
-// scores and 2 x 2 D for the values.
+// scores and 2 x 2 D for the values, in bf16 4 x 2 D (see below).
 //
 // Work decomposition: one workgroup per (sequence, kv-head, 128 packed query
 // rows, key split), as the extend kernel's (row r = token r/G, head g*G + r%G);
@@ -29,8 +29,8 @@
 // share goes, what the probabilities were rounded by would stay.  The result is then
 // off by its own last rounding (2-norm, 1.66e-3 of itself).  One number each, 2^-8 of
 // a probability off, leaves 2.56e-3 where the maps have nothing in common, and 1.7e-2
-// where their keys differ by an eighth and lambda is 0.9 to 1; it saves a quarter of
-// a call.  One number for most keys and two for some is no middle way: the error is
+// where their keys differ by an eighth and lambda is 0.9 to 1; it saves a quarter to
+// a third of a call.  One number for most keys and two for some is no middle way: the error is
 // then that of the keys which the weight happens to lie on.
 // fp32 storage: v_mfma_f32_32x32x2_f32, tiles of 32 keys, nothing rounded.
 //
@@ -38,9 +38,9 @@
 // A tile of 64 keys, heads of 128, takes 80 MFMAs of 32 cycles per SIMD (2560); with
 // some 400 other vector instructions it lasts 4060 cycles (1.69 us) with 8 workgroups
 // on the chip and 2.15 us with all CUs busy, at the clock that the board then holds.
-// 2048 new tokens over 131072, 32/8 heads of 128: 8.7 ms, 11.1e12 operations, 1270
+// 2048 new tokens over 131072, 32/8 heads of 128: 8.6 ms, 11.1e12 operations, 1290
 // TFLOP/s (a large bf16 matrix product 1262).  512 over 8192: 160 us.  fp32, 512 over
-// 8192: 797 us, 133 TFLOP/s (a large fp32 matrix product 153).
+// 8192: 800 us, 133 TFLOP/s (a large fp32 matrix product 153).
 //
 // Masked positions.  Their scores are replaced by -inf, so their weight is
 // exactly 0 whatever K holds; positions past the end of the sequence and unused
