@@ -198,8 +198,8 @@ def _run_own(s):
     case = s["case"]
     op = case["op"]
     if op == "append4":
-        kvt.append_kv4(s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"], s["k_new"], s["v_new"])
-        return kvt.read_kv4(s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"], DTYPES[case["dtype"]])
+        kvt.mx_append_kv(s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"], s["k_new"], s["v_new"])
+        return kvt.mx_read_kv(s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"], DTYPES[case["dtype"]])
     if op == "evict":
         length = [p + n for p, n in zip(s["prefix"], s["suffix"])]
         positions, weights = kvt.evict(s["k_pool"], s["v_pool"], s["table"], length, [case["keep"]] * len(length),
@@ -210,8 +210,8 @@ def _run_own(s):
                               s["weights"])
         return s["weights"]
     if op == "decode4":
-        return kvt.decode_attention4(s["q"], s["k_pool"], s["v_pool"], s["table"], s["prefix"], return_lse=True)
-    return kvt.extend_attention4(s["q"], s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"],
+        return kvt.mx_decode_attention(s["q"], s["k_pool"], s["v_pool"], s["table"], s["prefix"], return_lse=True)
+    return kvt.mx_extend_attention(s["q"], s["k_pool"], s["v_pool"], s["table"], s["prefix"], s["suffix"],
                                  return_lse=True)
 
 
