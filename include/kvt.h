@@ -386,6 +386,146 @@ kvt_status kvt_diff_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
  * invalid.  Host-only; enqueues nothing. */
 size_t kvt_diff_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
 
+/* ------------------------------------------------------------------------
+ * 4-bit pages (mx: groups of values under one scale): the same cache in 4.25 bits a value.
+ *
+ * The kvt_mx_ calls take a kvt_pool whose k and v are
+ * [num_blocks][num_kv_heads] records of KVT_MX_PAGE_BYTES(head_dim) bytes (1088
+ * for head_dim 128, 544 for 64), 16-byte aligned; dtype is that of the
+ * per-token tensors.  A record holds 16 tokens' codes, [16][D/2] bytes, the even
+ * column of a byte in its low half, then their scales, [16][D/32] bytes.
+ *
+ * A group of 32 columns of one token and kv-head shares the scale 2^(s - 127) of
+ * its byte s; a code is a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6.  The scale
+ * is the least power of two with which the group's largest magnitude is at most
+ * 7, within 2^-125 .. 2^96 (larger values saturate at 6 * 2^96), and codes are
+ * nearest, ties to the even code.  Every such value is exact in bf16.  A token
+ * whose K or V row of a kv-head holds an infinity or a NaN is no number for that
+ * kv-head: its scale bytes are 255 and its values read as NaN.
+ *
+ * Block tables, sequences, checked mode, ordering and asynchrony are those of
+ * the other calls.  A page moves, is shared and is freed as any other page.
+ * ---------------------------------------------------------------------- */
+#define KVT_MX_PAGE_BYTES(head_dim) (KVT_BLOCK_SIZE * ((head_dim) / 2 + (head_dim) / 32))
+
+/*
+ * kvt_mx_append_kv -- the new tokens' K/V into their 4-bit pages.
+ *
+ * k_new, v_new: rows of Hkv heads of `dtype` (their tokens may lie apart), apart
+ * from the pools.  The pages' other tokens keep their bytes.  K and V pools may
+ * not overlap.
+ */
+kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_new, const kvt_rows* v_new,
+                          void* stream);
+
+/*
+ * kvt_mx_read_kv -- the values that 4-bit pages hold at positions P_b .. P_b+S_b-1
+ * (any part of a sequence that is in the pool), as rows of Hkv heads of `dtype`.
+ * k_out and v_out may touch neither each other nor the pools.  Without a host
+ * mirror of the table an id outside the pool gives unspecified values.
+ */
+kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_out, const kvt_rows* v_out,
+                        void* stream);
+
+/*
+ * kvt_mx_extend_attention -- kvt_extend_attention over 4-bit pages.
+ *
+ * The same operation on the values that the pages stand for, which enter every
+ * product exactly.  bf16 queries feed bf16 MFMA, probabilities rounded to bf16;
+ * fp32 queries and their probabilities are three bf16 terms each, so that out
+ * keeps fp32's precision.  lse is summed in fp32 from unrounded probabilities.
+ * A token that is no number makes the rows that see it NaN, and no others.
+ *
+ * Arguments, workspace rules and errors as for kvt_extend_attention, with
+ * kvt_mx_extend_workspace_bytes; the workspace of a call that is split may not
+ * overlap q, out, lse or the pools (KVT_ERR_INVALID_ARG).  Results are
+ * bit-reproducible for given arguments.
+ */
+kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs,
+                                 const void* q, int32_t num_q_heads, float scale,
+                                 void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
+
+/*
+ * kvt_mx_decode_attention -- one decoding step over 4-bit pages: the same
+ * operation with S_b = 1 for every b (else KVT_ERR_INVALID_ARG), built for
+ * batches whose cost is streaming every sequence's K/V once from HBM.  Any
+ * Hq/Hkv.  workspace: NULL/0 runs unsplit, otherwise at least
+ * kvt_mx_decode_workspace_bytes() for the same arguments, 16-byte aligned and
+ * apart from q, out, lse and the pools (else KVT_ERR_WORKSPACE,
+ * KVT_ERR_INVALID_ARG; any workspace will do where that is 0).
+ */
+kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
+                                 const void* q, int32_t num_q_heads, float scale,
+                                 void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
+
+/*
+ * kvt_attention_weights -- what the attention of a call's new tokens gave every
+ * position, summed per kv-head over the tokens and the query heads that share
+ * it, onto what earlier calls gave (kvt_mx_attention_weights: over 4-bit pages).
+ *
+ * For every b, kv-head g, position j < P_b + S_b:
+ *   a = sum_{i < S_b, P_b + i >= j} sum_{h of g} exp(scale <q[off_b+i][h], K_b[j]> - lse[off_b+i][h])
+ *   weights[b][g][j] = (j < P_b ? weights[b][g][j] : 0) + a
+ * with the q, scale and lse of that attention call (extend, cascade or decode,
+ * after it on the stream).  The new positions are set, so a row needs no
+ * clearing; entries from P_b + S_b on are left as they were.
+ *
+ * weights: device float [B][Hkv], rows weights_stride elements apart (at least
+ * the longest sequence), 4-byte aligned, apart from q, lse and the pools; row b
+ * belongs to sequence b, a forked sequence has a row of its own.  Scores keep
+ * fp32's precision in every dtype (fp32 inputs are not rounded to bf16 here).
+ * Each weight is summed in one fixed order: results are bit-reproducible.  A
+ * non-finite key leaves its own weight unspecified, and no other.
+ */
+kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
+                                 const void* q, int32_t num_q_heads, float scale, const float* lse,
+                                 float* weights, int64_t weights_stride, void* stream);
+kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
+                                  const void* q, int32_t num_q_heads, float scale, const float* lse,
+                                  float* weights, int64_t weights_stride, void* stream);
+
+/* What an eviction keeps, and where it goes. */
+typedef struct {
+  const int32_t* keep;           /* HOST [B], >= 1: positions that sequence b keeps at most */
+  int32_t        sinks;          /* >= 0: first positions that stay in any case ... */
+  int32_t        recent;         /* >= 0: ... and last ones; sinks + recent <= keep[b] where b is longer than that */
+  const float*   weights;        /* DEVICE [B][Hkv], rows weights_stride apart (at least the longest sequence) */
+  int64_t        weights_stride;
+  const int32_t* to_table;       /* DEVICE [B][to_max_blocks]: the pages that the kept positions go to */
+  const int32_t* to_table_host;  /* HOST copy of to_table, or NULL; non-NULL checks the targets */
+  int32_t        to_max_blocks;  /* ceil(n_b/16) <= to_max_blocks for every b */
+  int32_t*       positions;      /* DEVICE [B][Hkv][out_stride]: the kept positions, ascending; -1 past n_b */
+  float*         weights_out;    /* DEVICE, the same shape: their weights, 0 past n_b; NULL: not wanted; may be
+                                    weights itself with out_stride = weights_stride */
+  int64_t        out_stride;     /* at least the largest n_b, at most INT32_MAX */
+} kvt_eviction;
+
+/*
+ * kvt_evict -- keep the positions that carry most weight, per sequence and
+ * kv-head (kvt_mx_evict: in 4-bit pages).
+ *
+ * Sequence b has L_b = P_b + S_b positions and keeps n_b = min(L_b, keep[b]): all
+ * of them if that is L_b, else the first `sinks`, the last `recent` and the
+ * heaviest of the others, the lower position of two that weigh the same (a NaN
+ * is heavier than anything).  With p the i-th of them in ascending order,
+ *   row i of to_table's pages = row p of block_table's pages   (K and V, bit copy, i < n_b)
+ * per kv-head, so that the n_b rows are the cache of a sequence of that length:
+ * attention does not depend on the order of the positions that all rows see.
+ * Other rows of the target pages keep their bytes.
+ *
+ * The pages of to_table may not be among those that the call reads, and none may
+ * be named twice (checked where both host mirrors are given:
+ * KVT_ERR_OUT_OF_RANGE; otherwise the result is unspecified).  A target id
+ * outside the pool is skipped, a source id outside is clamped to the last page.
+ * Source pages are read only: shared ones stay as they are for the others.
+ */
+kvt_status kvt_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream);
+kvt_status kvt_mx_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream);
+
 /* Direction of kvt_copy_blocks. */
 typedef enum {
   KVT_COPY_TO_HOST = 0,     /* pool pages -> host buffer (offload)  */

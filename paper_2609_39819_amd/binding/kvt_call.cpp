@@ -337,6 +337,87 @@ PyObject* diff_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+// mx_rows(head..., k, stride, v, stride, stream) -> status: an append into 4-bit
+// pages or a read of them
+PyObject* mx_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  kvt_rows k, v;
+  void* stream;
+  if (!count_is(n, kHead + 5) || !head(a, &h) || !rows(a + kHead, &k) || !rows(a + kHead + 2, &v) ||
+      !address(a[kHead + 4], &stream))
+    return nullptr;
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_mx_append_kv)>(h.fn)(&h.pool, &h.seqs, &k, &v, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// weights(head..., q, num_q_heads, scale, lse, weights, stride, stream) -> status
+PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  void *q, *lse, *w, *stream;
+  int32_t hq;
+  long long stride;
+  if (!count_is(n, kHead + 7) || !head(a, &h) || !address(a[kHead], &q) || !int32(a[kHead + 1], &hq)) return nullptr;
+  const double scale = PyFloat_AsDouble(a[kHead + 2]);
+  if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+  if (!address(a[kHead + 3], &lse) || !address(a[kHead + 4], &w) || !integer(a[kHead + 5], &stride) ||
+      !address(a[kHead + 6], &stream))
+    return nullptr;
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_attention_weights)>(h.fn)(&h.pool, &h.seqs, q, hq, (float)scale,
+                                                                reinterpret_cast<const float*>(lse),
+                                                                reinterpret_cast<float*>(w), stride, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// evict(head..., keep (packed, as the lengths), sinks, recent, weights, stride,
+// to_table, columns, host copy or None, positions, weights_out or None,
+// out_stride, stream) -> status
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  kvt_eviction ev;
+  void *w, *to, *positions, *out, *stream;
+  long long stride, out_stride;
+  if (!count_is(n, kHead + 12) || !head(a, &h) || !int32(a[kHead + 1], &ev.sinks) ||
+      !int32(a[kHead + 2], &ev.recent) || !address(a[kHead + 3], &w) || !integer(a[kHead + 4], &stride) ||
+      !address(a[kHead + 5], &to) || !int32(a[kHead + 6], &ev.to_max_blocks) || !address(a[kHead + 8], &positions) ||
+      !address(a[kHead + 9], &out) || !integer(a[kHead + 10], &out_stride) || !address(a[kHead + 11], &stream))
+    return nullptr;
+  if (!PyBytes_CheckExact(a[kHead]) || PyBytes_GET_SIZE(a[kHead]) < (Py_ssize_t)h.seqs.num_seqs * 4) {
+    PyErr_SetString(PyExc_TypeError, "bad packed counts");
+    return nullptr;
+  }
+  ev.keep = reinterpret_cast<const int32_t*>(PyBytes_AS_STRING(a[kHead]));
+  ev.weights = reinterpret_cast<const float*>(w);
+  ev.weights_stride = stride;
+  ev.to_table = reinterpret_cast<const int32_t*>(to);
+  ev.to_table_host = nullptr;
+  ev.positions = reinterpret_cast<int32_t*>(positions);
+  ev.weights_out = reinterpret_cast<float*>(out);
+  ev.out_stride = out_stride;
+  Py_buffer host;
+  const bool checked = a[kHead + 7] != Py_None;
+  if (checked) {
+    if (PyObject_GetBuffer(a[kHead + 7], &host, PyBUF_C_CONTIGUOUS) != 0) return nullptr;
+    if (host.itemsize != 4 || (long long)(host.len / 4) < h.seqs.num_seqs * (long long)ev.to_max_blocks) {
+      PyBuffer_Release(&host);
+      PyErr_SetString(PyExc_ValueError, "the target table's host copy is too small");
+      return nullptr;
+    }
+    ev.to_table_host = reinterpret_cast<const int32_t*>(host.buf);
+  }
+  kvt_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = reinterpret_cast<decltype(&kvt_evict)>(h.fn)(&h.pool, &h.seqs, &ev, stream);
+  Py_END_ALLOW_THREADS
+  if (checked) PyBuffer_Release(&host);
+  return PyLong_FromLong(st);
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f))
 PyMethodDef methods[] = {{"pack", FAST(pack), METH_FASTCALL, nullptr},
                          {"append", FAST(append), METH_FASTCALL, nullptr},
@@ -345,6 +426,9 @@ PyMethodDef methods[] = {{"pack", FAST(pack), METH_FASTCALL, nullptr},
                          {"workspace", FAST(workspace), METH_FASTCALL, nullptr},
                          {"attend", FAST(attend), METH_FASTCALL, nullptr},
                          {"diff_attend", FAST(diff_attend), METH_FASTCALL, nullptr},
+                         {"mx_rows", FAST(mx_rows), METH_FASTCALL, nullptr},
+                         {"weights", FAST(weights), METH_FASTCALL, nullptr},
+                         {"evict", FAST(evict), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvt_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -20,6 +20,7 @@
 
 #include "kvt.h"
 #include "kvt_diff.h"
+#include "kvt_mx.h"
 #include "kvt_internal.h"
 #include "kvt_rotary.h"
 
@@ -118,6 +119,13 @@ kvt_status check_append_targets(const kvt_seqs* seqs, int64_t T) {
     }
   }
   return KVT_OK;
+}
+
+// Bytes of one of a pool's two tensors; `mx`: of 4-bit pages.
+size_t pool_tensor_bytes(const kvt_pool* pool, bool mx) {
+  const size_t page = mx ? (size_t)kvt::mx_page_bytes(pool->head_dim)
+                          : (size_t)kvt::kBlock * pool->head_dim * elem_bytes(pool->dtype);
+  return (size_t)pool->num_blocks * pool->num_kv_heads * page;
 }
 
 bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
@@ -698,11 +706,11 @@ bool mode_ok(int32_t mode) {
 
 // out must not overlap q or a pool; lse must not overlap out.
 kvt_status check_outputs(const kvt_pool* pool, const void* q, int32_t num_q_heads, const void* out,
-                         const float* lse, int64_t T) {
+                         const float* lse, int64_t T, bool mx = false) {
   if (!aligned16(q) || !aligned16(out) || ((uintptr_t)lse & 3) != 0) return KVT_ERR_INVALID_ARG;
   const size_t es = elem_bytes(pool->dtype);
   const size_t tok_bytes = (size_t)T * num_q_heads * pool->head_dim * es;
-  const size_t pool_bytes = (size_t)pool->num_blocks * pool->num_kv_heads * kvt::kBlock * pool->head_dim * es;
+  const size_t pool_bytes = pool_tensor_bytes(pool, mx);
   if (overlaps(out, tok_bytes, q, tok_bytes) || overlaps(out, tok_bytes, pool->k, pool_bytes) ||
       overlaps(out, tok_bytes, pool->v, pool_bytes))
     return KVT_ERR_INVALID_ARG;
@@ -818,7 +826,7 @@ kvt_status check_rotary(const kvt_rotary* r, int32_t head_dim, kvt::RotaryArgs* 
 // The argument checks of kvt_extend_attention (and its no-alloc variant);
 // fills the total token count.
 kvt_status check_extend(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
-                        const void* out, const float* lse, int64_t* T) {
+                        const void* out, const float* lse, int64_t* T, bool mx = false) {
   kvt_status st = check_pool(pool);
   if (st != KVT_OK) return st;
   if ((st = check_seqs(seqs, T)) != KVT_OK) return st;
@@ -826,13 +834,14 @@ kvt_status check_extend(const kvt_pool* pool, const kvt_seqs* seqs, const void* 
   if (!heads_ok(pool, num_q_heads, *T)) return KVT_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale)) return KVT_ERR_INVALID_ARG;
   if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
-  return check_outputs(pool, q, num_q_heads, out, lse, *T);
+  return check_outputs(pool, q, num_q_heads, out, lse, *T, mx);
 }
 
-// Launches of one extend call under `plan` (partials in `workspace` when split).
+// Launches of one extend call under `plan` (partials in `workspace` when split);
+// `mx`: over 4-bit pages.
 kvt_status launch_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
                               float scale, void* out, float* lse, int64_t T, const ExtendPlan& plan,
-                              void* workspace, void* stream) {
+                              void* workspace, void* stream, bool mx = false) {
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int G = num_q_heads / pool->num_kv_heads;
   std::vector<int32_t> row_off(seqs->num_seqs + 1, 0);
@@ -854,7 +863,8 @@ kvt_status launch_extend_plan(const kvt_pool* pool, const kvt_seqs* seqs, const 
     a.unit_begin[n] = units;
     const int64_t grid = (int64_t)units * pool->num_kv_heads;
     if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
-    const hipError_t e = kvt::launch_extend(a, pool->dtype, pool->head_dim, (int)grid, s);
+    const hipError_t e = mx ? kvt::launch_mx_extend(a, pool->dtype, pool->head_dim, (int)grid, s)
+                             : kvt::launch_extend(a, pool->dtype, pool->head_dim, (int)grid, s);
     if (e != hipSuccess) return device_error(e);
   }
   return plan.nsplit > 1 ? combine(a, pool, out, lse, T, num_q_heads, plan.nsplit, plan.heaviest > 0.0, s) : KVT_OK;
@@ -1153,6 +1163,305 @@ kvt_status launch_diff(const kvt_pool* pool, const kvt_seqs* seqs, const void* q
     a.nseq = n;
     a.unit_begin[n] = (int32_t)rows;
     const hipError_t e = kvt::launch_diff_combine(a, pool->dtype, pool->head_dim, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
+}
+
+// ---- 4-bit pages and eviction
+
+// The workspace of a call may not hold anything that the call reads or writes
+// otherwise.
+bool workspace_apart(const kvt_pool* pool, const void* q, const void* out, const float* lse, int32_t num_q_heads,
+                     int64_t T, const void* workspace, size_t bytes) {
+  const size_t io = (size_t)T * num_q_heads * pool->head_dim * elem_bytes(pool->dtype);
+  const size_t held = pool_tensor_bytes(pool, true);
+  return !overlaps(workspace, bytes, q, io) && !overlaps(workspace, bytes, out, io) &&
+         !overlaps(workspace, bytes, pool->k, held) && !overlaps(workspace, bytes, pool->v, held) &&
+         (lse == nullptr || !overlaps(workspace, bytes, lse, (size_t)T * num_q_heads * sizeof(float)));
+}
+
+// Key splits of a decoding step over 4-bit pages: every sequence has its own
+// count, the partial sets being those of the largest.
+struct MxDecodePlan {
+  std::vector<int> order;        // sequences, longest key range first
+  std::vector<int32_t> nsplit;   // by sequence
+  int sets = 1;                  // the largest count
+  int chunks = 1;                // workgroups that share a kv-head's query heads
+  size_t ws_bytes = 0;
+};
+
+MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
+  MxDecodePlan p;
+  const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
+  p.chunks = (G + kvt::kMxDecMaxRows - 1) / kvt::kMxDecMaxRows;
+  const int64_t heads = (int64_t)pool->num_kv_heads * p.chunks;
+  p.order = longest_first(seqs);
+  p.nsplit.assign(B, 1);
+  const int64_t longest = (int64_t)seqs->prefix_len[p.order.front()] + 1;
+  const int64_t cus = device_cus(), all = total_keys(seqs) * heads;
+  auto splits = [&](int b, int64_t chunk) {
+    const int64_t n = ((int64_t)seqs->prefix_len[b] + 1 + chunk / 2) / chunk;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kvt::kMaxPartials, n));
+  };
+  const double key_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) / kvt::kBlock;
+  const double one = 25e3, every = 5.5e6;   // bytes per us
+  auto cost = [&](int64_t c) {
+    FreeTimes cu(0.0, cus, 0.0, 0);
+    int sets = 1;
+    for (int i = 0; i < B; ++i) {
+      const int b = p.order[i], n = splits(b, c);
+      cu.run(n * heads, std::ceil((double)(seqs->prefix_len[b] + 1) / n) * key_bytes + 60e3);
+      sets = std::max(sets, n);
+    }
+    return cu.drain(one, every) +
+           (sets > 1 ? 4.0 + 2.0 * (double)part_bytes(pool, sets, (int64_t)B * num_q_heads) / 4.5e6 : 0.0);
+  };
+  int64_t chunk = 2 * longest;   // unsplit
+  double best = 0.97 * cost(chunk);
+  for (double f : {0.7, 1.0, 1.5, 2.0, 3.0, 4.0}) {   // units per CU
+    if (B > 32 && f != 1.0 && f != 2.0 && f != 4.0) continue;   // large batches: fewer, for the host's sake
+    const int64_t c = std::max<int64_t>(128, (int64_t)((double)all / (f * (double)cus)));
+    if (splits(p.order.front(), c) == 1) continue;
+    const double t = cost(c);
+    if (t < best) best = t, chunk = c;
+  }
+  for (int b = 0; b < B; ++b) {
+    p.nsplit[b] = splits(b, chunk);
+    p.sets = std::max(p.sets, (int)p.nsplit[b]);
+  }
+  if (p.sets > 1) p.ws_bytes = part_bytes(pool, p.sets, (int64_t)B * num_q_heads);
+  return p;
+}
+
+// Token rows of a 4-bit append or read; fills the launch arguments.
+kvt_status check_mx_rows(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k, const kvt_rows* v, bool writes,
+                       int64_t* T, kvt::MxRowsArgs* a) {
+  kvt_status st = check_pool(pool);
+  if (st != KVT_OK) return st;
+  if ((st = check_seqs(seqs, T)) != KVT_OK) return st;
+  if (k == nullptr || v == nullptr) return KVT_ERR_INVALID_ARG;
+  const int es = elem_bytes(pool->dtype);
+  const int64_t width = (int64_t)pool->num_kv_heads * pool->head_dim;
+  Rows kr, vr;
+  if ((st = check_rows(k, *T, width, es, &kr)) != KVT_OK) return st;
+  if ((st = check_rows(v, *T, width, es, &vr)) != KVT_OK) return st;
+  const size_t held = pool_tensor_bytes(pool, true);
+  for (const Rows* r : {&kr, &vr})
+    for (const void* p : {(const void*)pool->k, (const void*)pool->v})
+      if (overlaps((const void*)r->first, r->extent(), p, held)) return KVT_ERR_INVALID_ARG;
+  if (writes ? rows_touch(kr, vr) : overlaps(pool->k, held, pool->v, held)) return KVT_ERR_INVALID_ARG;
+  if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
+  a->k = k->data;
+  a->v = v->data;
+  a->k_stride = k->stride;
+  a->v_stride = v->stride;
+  a->k_pool = pool->k;
+  a->v_pool = pool->v;
+  a->block_table = seqs->block_table;
+  a->num_blocks = pool->num_blocks;
+  a->max_blocks = seqs->max_blocks;
+  a->num_kv_heads = pool->num_kv_heads;
+  return KVT_OK;
+}
+
+kvt_status launch_mx_rows(kvt::MxRowsArgs& a, const kvt_pool* pool, const kvt_seqs* seqs, bool writes, void* stream) {
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  int32_t row = 0;
+  for (int b0 = 0; b0 < seqs->num_seqs; b0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - b0);
+    a.nseq = n;
+    a.row_begin = row;
+    for (int i = 0; i < n; ++i) {
+      const int b = b0 + i;
+      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row};
+      row += seqs->suffix_len[b];
+    }
+    a.rows = row - a.row_begin;
+    const hipError_t e = writes ? kvt::launch_mx_read(a, pool->dtype, pool->head_dim, s)
+                                : kvt::launch_mx_append(a, pool->dtype, pool->head_dim, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
+}
+
+// Extent of rows [B][Hkv] of `used` values each, `stride` apart; 0: too large.
+size_t head_rows_bytes(const kvt_pool* pool, int num_seqs, int64_t stride, int64_t used) {
+  const int64_t rows = (int64_t)num_seqs * pool->num_kv_heads;
+  if (stride > INT64_MAX / 8 / rows) return 0;
+  return (size_t)((rows - 1) * stride + used) * 4;
+}
+
+int64_t longest_sequence(const kvt_seqs* seqs) {
+  int64_t most = 0;
+  for (int b = 0; b < seqs->num_seqs; ++b)
+    most = std::max(most, (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b]);
+  return most;
+}
+
+kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                             float scale, const float* lse, float* weights, int64_t stride, void* stream, bool mx) {
+  kvt_status st = check_pool(pool);
+  if (st != KVT_OK) return st;
+  int64_t T = 0;
+  if ((st = check_seqs(seqs, &T)) != KVT_OK) return st;
+  if (q == nullptr || lse == nullptr || weights == nullptr || !aligned16(q) || ((uintptr_t)lse & 3) != 0 ||
+      ((uintptr_t)weights & 3) != 0)
+    return KVT_ERR_INVALID_ARG;
+  if (!heads_ok(pool, num_q_heads, T)) return KVT_ERR_INVALID_ARG;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return KVT_ERR_INVALID_ARG;
+  const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
+  const int64_t most = longest_sequence(seqs);
+  const size_t bytes = stride < most ? 0 : head_rows_bytes(pool, B, stride, most);
+  if (bytes == 0) return KVT_ERR_INVALID_ARG;
+  const size_t rows = (size_t)T * num_q_heads, held = pool_tensor_bytes(pool, mx);
+  if (overlaps(weights, bytes, q, rows * pool->head_dim * elem_bytes(pool->dtype)) ||
+      overlaps(weights, bytes, lse, rows * sizeof(float)) || overlaps(weights, bytes, pool->k, held) ||
+      overlaps(weights, bytes, pool->v, held))
+    return KVT_ERR_INVALID_ARG;
+  if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
+
+  kvt::WeightsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k_pool = pool->k;
+  a.lse = lse;
+  a.weights = weights;
+  a.stride = stride;
+  a.block_table = seqs->block_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.group = G;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const int format = mx ? kvt::kMx : pool->dtype;
+  const std::vector<int> order = longest_first(seqs);
+  int64_t most_rows = 0;
+  std::vector<int32_t> row_off(B + 1, 0);
+  for (int b = 0; b < B; ++b) {
+    row_off[b + 1] = row_off[b] + seqs->suffix_len[b];
+    most_rows = std::max(most_rows, (int64_t)seqs->suffix_len[b] * G);
+  }
+  const bool step = most_rows <= 32;
+  const int keys = kvt::weights_keys_per_unit(format);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
+    a.nseq = n;
+    int64_t units = 0, longest = 0;
+    for (int i = 0; i < n; ++i) {
+      const int b = order[c0 + i];
+      const int64_t len = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
+      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
+      a.unit_begin[i] = (int32_t)units;
+      units += (len + keys - 1) / keys;
+      longest = std::max(longest, len);
+      if (units * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    }
+    a.unit_begin[n] = (int32_t)units;
+    hipError_t e;
+    if (step) {
+      // workgroups of at least 512 keys, about four to a CU
+      const int64_t want = (4 * (int64_t)device_cus() + (int64_t)n * pool->num_kv_heads - 1) /
+                           ((int64_t)n * pool->num_kv_heads);
+      a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(want, (longest + 511) / 512));
+      e = kvt::launch_weights_step(a, format, pool->dtype, pool->head_dim, n * a.nsplit * pool->num_kv_heads, s);
+    } else {
+      const int waves = (int)std::min<int64_t>(8, (most_rows + 31) / 32);
+      e = kvt::launch_weights_turn(a, format, pool->dtype, pool->head_dim, waves, (int)units * pool->num_kv_heads, s);
+    }
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
+}
+
+kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* ev, void* stream, bool mx) {
+  kvt_status st = check_pool(pool);
+  if (st != KVT_OK) return st;
+  int64_t T = 0;
+  if ((st = check_seqs(seqs, &T)) != KVT_OK) return st;
+  if (ev == nullptr || ev->keep == nullptr || ev->weights == nullptr || ev->to_table == nullptr ||
+      ev->positions == nullptr || ev->sinks < 0 || ev->recent < 0 || ev->to_max_blocks < 1)
+    return KVT_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)ev->weights, (const void*)ev->positions, (const void*)ev->weights_out})
+    if (((uintptr_t)p & 3) != 0) return KVT_ERR_INVALID_ARG;
+  const int B = seqs->num_seqs;
+  std::vector<int32_t> kept(B);
+  int64_t most_kept = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t L = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
+    if (ev->keep[b] < 1) return KVT_ERR_INVALID_ARG;
+    if (L > ev->keep[b] && (int64_t)ev->sinks + ev->recent > ev->keep[b]) return KVT_ERR_INVALID_ARG;
+    kept[b] = (int32_t)std::min<int64_t>(L, ev->keep[b]);
+    if ((kept[b] + kvt::kBlock - 1) / kvt::kBlock > ev->to_max_blocks) return KVT_ERR_INVALID_ARG;
+    most_kept = std::max<int64_t>(most_kept, kept[b]);
+  }
+  const int64_t most = longest_sequence(seqs);
+  const size_t in_bytes = ev->weights_stride < most ? 0 : head_rows_bytes(pool, B, ev->weights_stride, most);
+  const size_t out_bytes =
+      ev->out_stride < most_kept || ev->out_stride > INT32_MAX ? 0 : head_rows_bytes(pool, B, ev->out_stride, ev->out_stride);
+  if (in_bytes == 0 || out_bytes == 0) return KVT_ERR_INVALID_ARG;
+  const size_t held = pool_tensor_bytes(pool, mx);
+  const bool in_place = ev->weights_out == ev->weights && ev->out_stride == ev->weights_stride;
+  auto in_pool = [&](const void* p, size_t n) { return overlaps(p, n, pool->k, held) || overlaps(p, n, pool->v, held); };
+  if (overlaps(ev->positions, out_bytes, ev->weights, in_bytes) || in_pool(ev->positions, out_bytes) ||
+      in_pool(ev->weights, in_bytes) || overlaps(pool->k, held, pool->v, held))
+    return KVT_ERR_INVALID_ARG;
+  if (ev->weights_out != nullptr &&
+      ((!in_place && overlaps(ev->weights_out, out_bytes, ev->weights, in_bytes)) ||
+       overlaps(ev->weights_out, out_bytes, ev->positions, out_bytes) || in_pool(ev->weights_out, out_bytes)))
+    return KVT_ERR_INVALID_ARG;
+  if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
+  if (ev->to_table_host != nullptr) {
+    // targets: inside the pool, each page once, and none that the call reads
+    std::unordered_set<int32_t> seen;
+    for (int b = 0; b < B; ++b)
+      for (int i = 0; i < (kept[b] + kvt::kBlock - 1) / kvt::kBlock; ++i) {
+        const int32_t id = ev->to_table_host[(int64_t)b * ev->to_max_blocks + i];
+        if (id < 0 || id >= pool->num_blocks || !seen.insert(id).second) return KVT_ERR_OUT_OF_RANGE;
+      }
+    for (int b = 0; b < B && seqs->block_table_host != nullptr; ++b) {
+      const int64_t L = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
+      for (int64_t i = 0; i < (L + kvt::kBlock - 1) / kvt::kBlock; ++i)
+        if (seen.count(seqs->block_table_host[(int64_t)b * seqs->max_blocks + i])) return KVT_ERR_OUT_OF_RANGE;
+    }
+  }
+
+  kvt::EvictArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.weights = ev->weights;
+  a.stride = ev->weights_stride;
+  a.positions = ev->positions;
+  a.weights_out = ev->weights_out;
+  a.out_stride = ev->out_stride;
+  a.block_table = seqs->block_table;
+  a.to_table = ev->to_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.to_max_blocks = ev->to_max_blocks;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.sinks = ev->sinks;
+  a.recent = ev->recent;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const std::vector<int> order = longest_first(seqs);
+  for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
+    int64_t pages = 0;
+    a.nseq = n;
+    for (int i = 0; i < n; ++i) {
+      const int b = order[c0 + i];
+      a.seq[i] = kvt::EvictDesc{b, seqs->prefix_len[b] + seqs->suffix_len[b], kept[b]};
+      a.unit_begin[i] = (int32_t)pages;
+      pages += (kept[b] + kvt::kBlock - 1) / kvt::kBlock;
+      if (pages * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    }
+    a.unit_begin[n] = (int32_t)pages;
+    hipError_t e = kvt::launch_evict_select(a, s);
+    if (e != hipSuccess) return device_error(e);
+    e = kvt::launch_evict_move(a, mx ? kvt::kMx : pool->dtype, pool->head_dim, (int)(pages * pool->num_kv_heads), s);
     if (e != hipSuccess) return device_error(e);
   }
   return KVT_OK;
@@ -1602,6 +1911,136 @@ kvt_status kvt_diff_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
   if (T != seqs->num_seqs) return KVT_ERR_INVALID_ARG;   // one new token per sequence
   DiffPlan plan = diff_decode_plan(pool, seqs, num_q_heads);
   return launch_diff(pool, seqs, q, num_q_heads, scale, diff, out, T, plan, true, workspace, workspace_bytes, stream);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_new, const kvt_rows* v_new,
+                          void* stream) try {
+  kvt::MxRowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  int64_t T = 0;
+  kvt_status st = check_mx_rows(pool, seqs, k_new, v_new, false, &T, &a);
+  if (st != KVT_OK) return st;
+  if ((st = check_append_targets(seqs, T)) != KVT_OK) return st;
+  return launch_mx_rows(a, pool, seqs, false, stream);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_out, const kvt_rows* v_out,
+                        void* stream) try {
+  kvt::MxRowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  int64_t T = 0;
+  const kvt_status st = check_mx_rows(pool, seqs, k_out, v_out, true, &T, &a);
+  if (st != KVT_OK) return st;
+  return launch_mx_rows(a, pool, seqs, true, stream);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) try {
+  return kvt_extend_workspace_bytes(pool, seqs, num_q_heads);
+} catch (const std::bad_alloc&) {
+  return 0;
+}
+
+kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                 float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream) try {
+  int64_t T = 0;
+  const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
+  if (st != KVT_OK) return st;
+  ExtendPlan plan = extend_plan(pool, seqs, num_q_heads, T);
+  const kvt_status fit = fit_workspace(&plan, pool, T * num_q_heads, workspace, workspace_bytes);
+  if (fit != KVT_OK) return fit;
+  if (plan.nsplit > 1 && !workspace_apart(pool, q, out, lse, num_q_heads, T, workspace, plan.ws_bytes))
+    return KVT_ERR_INVALID_ARG;
+  return launch_extend_plan(pool, seqs, q, num_q_heads, scale, out, lse, T, plan, workspace, stream, true);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) try {
+  if (check_pool(pool) != KVT_OK) return 0;
+  int64_t T = 0;
+  if (check_seqs(seqs, &T) != KVT_OK || T != seqs->num_seqs || !heads_ok(pool, num_q_heads, T)) return 0;
+  return mx_decode_plan(pool, seqs, num_q_heads).ws_bytes;
+} catch (const std::bad_alloc&) {
+  return 0;
+}
+
+kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                 float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream) try {
+  int64_t T = 0;
+  const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
+  if (st != KVT_OK) return st;
+  if (T != seqs->num_seqs) return KVT_ERR_INVALID_ARG;   // one new token per sequence
+  MxDecodePlan plan = mx_decode_plan(pool, seqs, num_q_heads);
+  if (plan.sets > 1) {
+    if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
+      plan.nsplit.assign(seqs->num_seqs, 1);
+      plan.sets = 1;
+    } else {
+      if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
+      if (!aligned16(workspace) || !workspace_apart(pool, q, out, lse, num_q_heads, T, workspace, plan.ws_bytes))
+        return KVT_ERR_INVALID_ARG;
+    }
+  }
+  ExtendPlan sets;
+  sets.nsplit = plan.sets;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  kvt::ExtendArgs a = base_args(pool, seqs, q, num_q_heads, scale, out, lse, T, sets, workspace);
+  bool gaps = false;
+  for (int c0 = 0; c0 < seqs->num_seqs; c0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - c0);
+    a.nseq = n;
+    int32_t units = 0;
+    for (int i = 0; i < n; ++i) {
+      const int b = plan.order[c0 + i];
+      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], 1, b};   // row of sequence b is b
+      a.last[i] = (uint8_t)plan.nsplit[b];
+      a.unit_begin[i] = units;
+      units += plan.nsplit[b];
+      gaps = gaps || plan.nsplit[b] < plan.sets;
+    }
+    a.unit_begin[n] = units;
+    const int64_t grid = (int64_t)units * pool->num_kv_heads * plan.chunks;
+    if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    const hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, plan.chunks, (int)grid, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  return plan.sets > 1 ? combine(a, pool, out, lse, T, num_q_heads, plan.sets, gaps, s) : KVT_OK;
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                 float scale, const float* lse, float* weights, int64_t weights_stride,
+                                 void* stream) try {
+  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, stream, false);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                  float scale, const float* lse, float* weights, int64_t weights_stride,
+                                  void* stream) try {
+  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, stream, true);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream) try {
+  return evict(pool, seqs, eviction, stream, false);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_mx_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream) try {
+  return evict(pool, seqs, eviction, stream, true);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }

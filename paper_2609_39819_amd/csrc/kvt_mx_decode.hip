@@ -1,0 +1,335 @@
+// Decode attention over 4-bit pages, gfx950: one new token per sequence.
+//
+// The formula is kvt_decode.hip's; the cost is streaming each sequence's 4-bit
+// K/V once from HBM (2 * 17/32 D bytes a key and kv-head).  Work decomposition:
+//   * one workgroup per (sequence, kv-head, key split, up to 32 of the kv-head's
+//     query heads), 4 waves; wave w takes the split's 32-key tiles w, w+4, ...
+//     and keeps two of them in flight in registers; no barrier in the loop;
+//   * v_mfma_f32_16x16x32_bf16 with 16 rows (NB = 1) or 32 (NB = 2): S^T = K Q^T.
+//     A lane's K operand is 8 columns of one key, in any order of the columns
+//     that Q's shares, so each lane takes D/4 neighbouring columns of its key:
+//     16 bytes of codes under one scale (D = 128), converted straight into the
+//     operand.  K never goes through LDS;
+//   * V does, as bf16 [key][D], because its operand runs along the keys: the
+//     lane that loaded 32 columns of a key writes them, and transposed reads
+//     bring them back; the rows are swizzled so that neither has a conflict;
+//   * fp32 queries are three bf16 terms, and so are the probabilities: every
+//     product then keeps fp32's 24 bits (the 4-bit values are exact in bf16);
+//   * at the end the four waves' (m, l, O) merge through LDS into the output or
+//     a partial of the key split.
+#include "kvt_mx_device.h"
+
+namespace kvt {
+namespace {
+
+using namespace dev;
+
+constexpr int kWaves = kDecWaves;
+constexpr int kTK = kDecKeysPerTile;   // keys per tile = 2 pages
+
+template <int D, int NB>
+struct alignas(1024) MxDecSlot {
+  // V of one tile; at the end O, [row][D] fp32
+  char bytes[kTK * D * 2 > NB * 16 * D * 4 ? kTK * D * 2 : NB * 16 * D * 4];
+};
+
+// XOR swizzle of the 16-byte chunks of a V row in LDS.  A write takes 16 keys at
+// one chunk, a transposed read 8 keys at two neighbouring chunks (the first an
+// even one): both get 16 distinct bank groups of the 256 bytes of a cycle.
+template <int D>
+__device__ __forceinline__ int swz_mx(int key) {
+  if constexpr (D == 128) return ((key & 7) << 1) | ((key >> 3) & 1);
+  else return (((key >> 1) & 3) << 1) | ((key >> 3) & 1);
+}
+
+template <typename T, int D, int NB>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 ? 1 : 2) void mx_decode_kernel(const ExtendArgs a, const int chunks) {
+  constexpr int NT = kTerms<T>;
+  constexpr int KS = D / 32;                     // score steps = words of a lane's codes
+  constexpr int CT = D / 16;                     // 16-column tiles of the output
+  constexpr int64_t kPage = mx_page_bytes(D);
+  constexpr float kRescaleSlack = 8.0f;
+  __shared__ MxDecSlot<D, NB> ring[kWaves];
+  __shared__ float ml[kWaves][NB * 16][2];       // per wave and row: m (log2 units), l
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15;
+  const int qd = lane >> 4;
+
+  // ---- which (sequence, kv-head, key split, head chunk) this workgroup owns
+  const int hkv = a.num_kv_heads;
+  const int G = a.group;
+  const int g = blockIdx.x % hkv;
+  const int rest = blockIdx.x / hkv;
+  const int unit = chunks == 1 ? rest : rest / chunks;
+  const int per_chunk = (G + chunks - 1) / chunks;
+  const int head0 = (rest - unit * chunks) * per_chunk;
+  const int heads = min(per_chunk, G - head0);
+  const int si = find_seq(a.unit_begin, a.nseq, unit);
+  const SeqDesc sd = a.seq[si];
+  const int nsplit = a.last[si];
+  const int split = unit - a.unit_begin[si];
+  const int L = sd.prefix + 1;                   // keys 0..P_b
+  const int nblk = (L + kBlock - 1) / kBlock;
+  const int ntk = (L + kTK - 1) / kTK;
+  const int per_split = (ntk + nsplit - 1) / nsplit;
+  const int j0 = split * per_split;
+  const int j1 = min(ntk, j0 + per_split);
+  const int nt = j1 - j0 > wave ? (j1 - j0 - wave + kWaves - 1) / kWaves : 0;   // this wave's tiles
+
+  // ---- this lane's query rows (rows past the last head repeat it and are
+  // dropped): columns qd * D/4 ..
+  const int64_t first_row = (int64_t)sd.row_off * a.num_q_heads + g * G + head0;
+  bf16x8 qreg[NB][KS][NT];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const T* qp = reinterpret_cast<const T*>(a.q) + (first_row + min(b * 16 + l16, heads - 1)) * D + qd * (D / 4);
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) load_terms(qp + kk * 8, qreg[b][kk]);
+  }
+
+  const char* kpool = reinterpret_cast<const char*>(a.k_pool);
+  const char* vpool = reinterpret_cast<const char*>(a.v_pool);
+  const __attribute__((address_space(4))) int32_t* bt =
+      (const __attribute__((address_space(4))) int32_t*)(a.block_table + (int64_t)sd.seq * a.max_blocks);
+  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
+
+  auto page_ids = [&](int j, uint32_t (&ids)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int page = __builtin_amdgcn_readfirstlane(min(j * 2 + p, nblk - 1));
+      const uint32_t raw = (uint32_t)bt[page];
+      ids[p] = __builtin_amdgcn_readfirstlane(raw > nb_max ? nb_max : raw);
+    }
+  };
+  // one tile in flight: per page, the lane's codes and scales of key l16
+  struct Stage {
+    unsigned k[2][KS], v[2][KS];
+    unsigned char sk[2], sv[2];
+  };
+  // positions past the end read the last real position (weight 0)
+  auto load_tile = [&](int j, const uint32_t (&ids)[2], Stage& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int page = min(j * 2 + p, nblk - 1);
+      const int slot = min(l16, L - 1 - page * kBlock);
+      const int64_t at = ((int64_t)ids[p] * hkv + g) * kPage;
+      const int code = slot * (D / 2) + qd * (D / 8);
+      const int scale = mx_code_bytes(D) + slot * (D / 32) + (D == 128 ? qd : qd >> 1);
+      const char* ks = kpool + at;
+      const char* vs = vpool + at;
+      if constexpr (KS == 4) {
+        const u32x4 k4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ks + code));
+        const u32x4 v4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vs + code));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.k[p][i] = k4[i], st.v[p][i] = v4[i];
+      } else {
+        const u32x2 k2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(ks + code));
+        const u32x2 v2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vs + code));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) st.k[p][i] = k2[i], st.v[p][i] = v2[i];
+      }
+      st.sk[p] = (unsigned char)ks[scale];
+      st.sv[p] = (unsigned char)vs[scale];
+    }
+  };
+
+  f32x4 o[NB][CT];
+  float m_ref[NB], l_run[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    m_ref[b] = -INFINITY, l_run[b] = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) o[b][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  const float c = a.scale_log2;
+  __bf16* vs = reinterpret_cast<__bf16*>(ring[wave].bytes);
+  const lds_bf16* vl = (const lds_bf16*)vs;
+  const int vkey = 4 * qd + (l16 >> 2);          // key of this lane's transposed reads
+  const int vrow = vkey * D + (l16 & 1) * 4, vsub = (l16 >> 1) & 1, vswz = swz_mx<D>(vkey);
+
+  // ---- tile i from its stage; `next` refills the stage when it is free
+  auto tile = [&](Stage& st, int kb, auto&& next) __attribute__((always_inline)) {
+    // V into LDS.  A token that is not a number counts through K (its score is
+    // one for the rows that see it); its V becomes 0, so that no other row
+    // takes it in with a weight of 0.
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const float sv = mx_scale(st.sv[p] == kMxNan ? 0u : st.sv[p]);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int chunk = qd * KS + i;           // 8 columns
+        *reinterpret_cast<u32x4*>(vs + (p * 16 + l16) * D + ((chunk ^ swz_mx<D>(l16)) << 3)) =
+            __builtin_bit_cast(u32x4, mx_values(st.v[p][i], sv));
+      }
+    }
+    f32x4 s[NB][2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const float sk = mx_scale(st.sk[p]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][p] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const bf16x8 kf = mx_values(st.k[p][kk], sk);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            s[b][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[b][kk][t], s[b][p], 0, 0, 0);
+      }
+    }
+    next();
+    if (kb + kTK > L) {   // the sequence ends inside this tile
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (kb + 16 * p + 4 * qd + e >= L) s[b][p][e] = -INFINITY;
+    }
+    bf16x8 pb[NB][NT];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float mx = s[b][0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[b][e >> 2][e & 3]);
+      const float mxc = quad_max(mx) * c;
+      const float m_new = (mxc > m_ref[b] + kRescaleSlack) ? mxc : m_ref[b];
+      const float alpha = (m_new == -INFINITY) ? 1.0f : __builtin_amdgcn_exp2f(m_ref[b] - m_new);
+      m_ref[b] = m_new;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[b][ct] *= alpha;
+      }
+      const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
+      float pr[8], rs = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        pr[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e >> 2][e & 3], c, -m_use));
+        rs += pr[e];
+      }
+      l_run[b] = l_run[b] * alpha + rs;
+      prob_terms(pr, pb[b]);
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      bf16x4 v[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        v[p] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+            (lds_bf16x4*)(vl + p * 16 * D + vrow + (((2 * ct + vsub) ^ vswz) << 3)));
+      const bf16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          o[b][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[b][t], o[b][ct], 0, 0, 0);
+    }
+  };
+
+  // ---- this wave's tiles j0 + wave + kWaves*i, two in flight
+  auto jt = [&](int i) { return j0 + wave + kWaves * i; };
+  Stage st[2];
+  uint32_t ids[2];
+  if (nt > 0) {
+    page_ids(jt(0), ids);
+    load_tile(jt(0), ids, st[0]);
+    page_ids(jt(1), ids);
+    if (nt > 1) load_tile(jt(1), ids, st[1]);
+    page_ids(jt(2), ids);
+  }
+  auto step = [&](int i, Stage& s) __attribute__((always_inline)) {
+    tile(s, jt(i) * kTK, [&]() __attribute__((always_inline)) {
+      if (i + 2 < nt) {
+        load_tile(jt(i + 2), ids, s);
+        page_ids(jt(i + 3), ids);
+      }
+    });
+  };
+  int i = 0;
+  for (; i + 2 <= nt; i += 2) {
+    step(i, st[0]);
+    step(i + 1, st[1]);
+  }
+  if (i < nt) step(i, st[0]);
+
+  // ---- merge the four waves.  Each parks its O rows in its own slot (its reads
+  // of V precede these writes in LDS order), four columns a piece, the pieces of
+  // a row XOR-swizzled by the row.
+  constexpr int Q4 = D / 4;
+  f32x4* ow = reinterpret_cast<f32x4*>(ring[wave].bytes);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const float l_tot = quad_sum(l_run[b]);
+    const int row = b * 16 + l16;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) ow[row * Q4 + ((ct * 4 + qd) ^ l16)] = o[b][ct];
+    if (qd == 0) {
+      ml[wave][row][0] = m_ref[b];
+      ml[wave][row][1] = l_tot;
+    }
+  }
+  __syncthreads();
+  const int64_t set_rows = (int64_t)a.total_rows * a.num_q_heads;
+  for (int idx = tid; idx < heads * Q4; idx += kWaves * 64) {
+    const int r = idx / Q4, q = idx - r * Q4;
+    float mstar = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mstar = fmaxf(mstar, ml[w][r][0]);
+    float lsum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float mw = ml[w][r][0];
+      // a wave without tiles has m = -inf, l = 0 and O = 0; one whose scores
+      // are all NaN has m = -inf too, and its l is NaN
+      const float wt = (mw == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mw - mstar);
+      lsum += wt * ml[w][r][1];
+      acc += wt * reinterpret_cast<const f32x4*>(ring[w].bytes)[r * Q4 + (q ^ (r & 15))];
+    }
+    const int64_t row = first_row + r;
+    if (a.direct) {
+      const float inv = 1.0f / lsum;
+      store4(reinterpret_cast<T*>(a.out) + row * D + q * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      if (a.lse != nullptr && q == 0) a.lse[row] = (mstar + __builtin_log2f(lsum)) * kLn2;
+    } else {
+      const int64_t prow = split * set_rows + row;
+      *reinterpret_cast<f32x4*>(a.part_o + prow * D + q * 4) = acc;
+      if (q == 0) {
+        a.part_ml[prow * 2] = mstar;
+        a.part_ml[prow * 2 + 1] = lsum;
+        if (split == nsplit - 1) {   // the sets that this sequence has no splits for
+          for (int s = split + 1; s < a.nsplit; ++s) {
+            a.part_ml[(s * set_rows + row) * 2] = -INFINITY;
+            a.part_ml[(s * set_rows + row) * 2 + 1] = -1.f;
+          }
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int D>
+void launch_as(const ExtendArgs& a, int chunks, int grid, hipStream_t stream) {
+  const int per_chunk = (a.group + chunks - 1) / chunks;
+  if (per_chunk <= 16)
+    hipLaunchKernelGGL((mx_decode_kernel<T, D, 1>), dim3(grid), dim3(kWaves * 64), 0, stream, a, chunks);
+  else
+    hipLaunchKernelGGL((mx_decode_kernel<T, D, 2>), dim3(grid), dim3(kWaves * 64), 0, stream, a, chunks);
+}
+
+}  // namespace
+
+hipError_t launch_mx_decode(const ExtendArgs& a, int dtype, int head_dim, int chunks, int grid, hipStream_t stream) {
+  if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, chunks, grid, stream);
+  else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, chunks, grid, stream);
+  else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, chunks, grid, stream);
+  else launch_as<float, 64>(a, chunks, grid, stream);
+  return hipGetLastError();
+}
+
+}  // namespace kvt

@@ -39,13 +39,16 @@ MGR_EXPORTED = ("kvt_mgr_append", "kvt_mgr_begin_request", "kvt_mgr_create", "kv
                 "kvt_mgr_start_prefill", "kvt_mgr_terminate", "kvt_mgr_unpin")
 MGR_OPS = ("spawn", "fork", "append", "one_off", "pin", "unpin", "replace", "remove", "terminate", "begin_request",
            "start_prefill", "prefill_done", "end_request")   # KVT_MGR_OP_* in this order
-EXPORTED = ("kvt_append_kv", "kvt_append_kv_rotary", "kvt_cascade_extend_attention", "kvt_cascade_extend_attention_ex",
-            "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
+EXPORTED = ("kvt_append_kv", "kvt_mx_append_kv", "kvt_append_kv_rotary", "kvt_attention_weights",
+            "kvt_mx_attention_weights", "kvt_cascade_extend_attention",
+            "kvt_cascade_extend_attention_ex", "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
             "kvt_copy_blocks",
-            "kvt_decode_attention", "kvt_decode_workspace_bytes", "kvt_diff_decode_attention",
+            "kvt_decode_attention", "kvt_mx_decode_attention", "kvt_decode_workspace_bytes",
+            "kvt_mx_decode_workspace_bytes", "kvt_diff_decode_attention",
             "kvt_diff_decode_workspace_bytes", "kvt_diff_extend_attention", "kvt_diff_extend_workspace_bytes",
-            "kvt_extend_attention",
-            "kvt_extend_attention_noalloc", "kvt_extend_workspace_bytes", "kvt_last_hip_error", "kvt_rotate",
+            "kvt_evict", "kvt_mx_evict", "kvt_extend_attention", "kvt_mx_extend_attention",
+            "kvt_extend_attention_noalloc", "kvt_extend_workspace_bytes", "kvt_mx_extend_workspace_bytes",
+            "kvt_last_hip_error", "kvt_mx_read_kv", "kvt_rotate",
             "kvt_status_str") + MGR_EXPORTED
 CASCADE_AUTO, CASCADE_SHARED_PASS, CASCADE_PLAIN = 0, 1, 2    # kvt_cascade_mode
 KVT_COPY_TO_HOST = 0
@@ -78,6 +81,13 @@ class KvtRows(ctypes.Structure):
 class KvtDiff(ctypes.Structure):
     _fields_ = [("lambda_", ctypes.c_void_p), ("lambda_stride", ctypes.c_int64), ("norm_weight", ctypes.c_void_p),
                 ("eps", ctypes.c_float), ("out_scale", ctypes.c_float)]
+
+
+class KvtEviction(ctypes.Structure):
+    _fields_ = [("keep", ctypes.POINTER(ctypes.c_int32)), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("weights", ctypes.c_void_p), ("weights_stride", ctypes.c_int64), ("to_table", ctypes.c_void_p),
+                ("to_table_host", ctypes.POINTER(ctypes.c_int32)), ("to_max_blocks", ctypes.c_int32),
+                ("positions", ctypes.c_void_p), ("weights_out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
 
 
 class KvtMgrReport(ctypes.Structure):
@@ -158,6 +168,22 @@ def lib():
         L.kvt_diff_decode_attention.restype = ctypes.c_int
         L.kvt_diff_decode_workspace_bytes.argtypes = L.kvt_extend_workspace_bytes.argtypes
         L.kvt_diff_decode_workspace_bytes.restype = ctypes.c_size_t
+        for name in ("kvt_mx_append_kv", "kvt_mx_read_kv"):
+            getattr(L, name).argtypes = [P(KvtPool), P(KvtSeqs), P(KvtRows), P(KvtRows), ctypes.c_void_p]
+            getattr(L, name).restype = ctypes.c_int
+        for name in ("kvt_mx_extend_attention", "kvt_mx_decode_attention"):
+            getattr(L, name).argtypes = L.kvt_extend_attention.argtypes
+            getattr(L, name).restype = ctypes.c_int
+        for name in ("kvt_mx_extend_workspace_bytes", "kvt_mx_decode_workspace_bytes"):
+            getattr(L, name).argtypes = L.kvt_extend_workspace_bytes.argtypes
+            getattr(L, name).restype = ctypes.c_size_t
+        for name in ("kvt_attention_weights", "kvt_mx_attention_weights"):
+            getattr(L, name).argtypes = [P(KvtPool), P(KvtSeqs), ctypes.c_void_p, ctypes.c_int32, ctypes.c_float,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+            getattr(L, name).restype = ctypes.c_int
+        for name in ("kvt_evict", "kvt_mx_evict"):
+            getattr(L, name).argtypes = [P(KvtPool), P(KvtSeqs), P(KvtEviction), ctypes.c_void_p]
+            getattr(L, name).restype = ctypes.c_int
         M, I64, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
         L.kvt_mgr_create.argtypes, L.kvt_mgr_create.restype = [I64], M
         L.kvt_mgr_destroy.argtypes, L.kvt_mgr_destroy.restype = [M], None
@@ -752,6 +778,265 @@ def _diff_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, p
     if st != KVT_OK:
         raise KvtError(st, entry)
     return out
+
+
+# ---------------------------------------------------------------------------
+# 4-bit pages, attention weights, eviction
+# ---------------------------------------------------------------------------
+
+def mx_page_bytes(head_dim: int) -> int:
+    """Bytes of one kv-head's 4-bit page (``KVT_MX_PAGE_BYTES``): a 4-bit pool is a
+    uint8 tensor [num_blocks][num_kv_heads][mx_page_bytes(head_dim)]."""
+    if head_dim not in (64, 128):
+        raise ValueError("head_dim must be 64 or 128")
+    return BLOCK_SIZE * (head_dim // 2 + head_dim // 32)
+
+
+_MX_HEAD_DIM = {544: 64, 1088: 128}   # by the bytes of a page
+
+
+def _mx_pool_args(k_pool, v_pool, dtype) -> tuple:
+    """(k, v, num_blocks, num_kv_heads, head_dim, dtype code of the per-token tensors) of a checked 4-bit pool."""
+    import torch
+    shape = k_pool.shape
+    if (shape != v_pool.shape or k_pool.dtype != torch.uint8 or v_pool.dtype != torch.uint8 or len(shape) != 3
+            or shape[2] not in _MX_HEAD_DIM):
+        raise ValueError("4-bit pools must both be uint8 [num_blocks][num_kv_heads][mx_page_bytes(head_dim)]")
+    if not (k_pool.is_contiguous() and v_pool.is_contiguous()):
+        raise ValueError("pools must be contiguous")
+    if dtype == torch.bfloat16:
+        code = KVT_DTYPE_BF16
+    elif dtype == torch.float32:
+        code = KVT_DTYPE_F32
+    else:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return k_pool.data_ptr(), v_pool.data_ptr(), shape[0], shape[1], _MX_HEAD_DIM[shape[2]], code
+
+
+def mx_append_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], k_new, v_new, *,
+               stream=None, checked: bool = False) -> None:
+    """The new tokens' K/V ([T][Hkv][D], bf16 or fp32, whose tokens may lie apart)
+    into their 4-bit pages (``kvt_mx_append_kv``)."""
+    if stream is not None:
+        with _on_stream(stream, k_pool):
+            return mx_append_kv(k_pool, v_pool, block_table, prefix_len, suffix_len, k_new, v_new, checked=checked)
+    pool = _mx_pool_args(k_pool, v_pool, k_new.dtype)
+    device = k_pool.get_device()
+    head, T = _head("kvt_mx_append_kv", pool, prefix_len, suffix_len, block_table, checked)
+    _check_table(block_table, head[8], device, v_pool)
+    k_rows = _rows_of(k_new, "k_new", T, pool[3], pool[4], k_new.dtype, device)
+    v_rows = _rows_of(v_new, "v_new", T, pool[3], pool[4], k_new.dtype, device)
+    with _on_device(k_pool):
+        st = _native().mx_rows(*head, *k_rows, *v_rows, _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, "kvt_mx_append_kv")
+
+
+def mx_read_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], dtype, *, k_out=None,
+             v_out=None, stream=None, checked: bool = False):
+    """The values that 4-bit pages hold at positions ``prefix_len[b]`` ..
+    ``prefix_len[b] + suffix_len[b] - 1`` (``kvt_mx_read_kv``): (k, v), each
+    [T][Hkv][D] of ``dtype``.  The tokens of ``k_out`` and ``v_out`` may lie apart."""
+    import torch
+    if stream is not None:   # what is allocated here belongs to the stream that it is written on
+        with _on_stream(stream, k_pool):
+            return mx_read_kv(k_pool, v_pool, block_table, prefix_len, suffix_len, dtype, k_out=k_out, v_out=v_out,
+                            checked=checked)
+    pool = _mx_pool_args(k_pool, v_pool, dtype)
+    hkv, d, device = pool[3], pool[4], k_pool.get_device()
+    head, T = _head("kvt_mx_read_kv", pool, prefix_len, suffix_len, block_table, checked)
+    _check_table(block_table, head[8], device, v_pool)
+    with _on_device(k_pool):
+        rows, outs = [], []
+        for name, x in (("k_out", k_out), ("v_out", v_out)):
+            if x is None:
+                x = torch.empty((T, hkv, d), dtype=dtype, device=k_pool.device)
+                rows.append((x.data_ptr(), hkv * d))
+            else:
+                rows.append(_rows_of(x, name, T, hkv, d, dtype, device))
+            outs.append(x)
+        st = _native().mx_rows(*head, *rows[0], *rows[1], _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, "kvt_mx_read_kv")
+    return tuple(outs)
+
+
+def mx_extend_workspace_bytes(k_pool, v_pool, block_table, prefix_len, suffix_len, num_q_heads: int, dtype) -> int:
+    head, _ = _head("kvt_mx_extend_workspace_bytes", _mx_pool_args(k_pool, v_pool, dtype), prefix_len, suffix_len,
+                    block_table, False)
+    return _native().workspace(*head, int(num_q_heads))
+
+
+def mx_extend_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int],
+                      scale: Optional[float] = None, *, out=None, lse=None, return_lse: bool = False,
+                      workspace=None, use_workspace: bool = True, stream=None, checked: bool = False):
+    """``extend_attention`` over 4-bit pages (``kvt_mx_extend_attention``): ``q`` is
+    bf16 or fp32, and so is the result.  Other arguments as there."""
+    return _mx_attention("kvt_mx_extend_attention", "kvt_mx_extend_workspace_bytes", q, k_pool, v_pool, block_table,
+                       prefix_len, suffix_len, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
+
+
+def mx_decode_workspace_bytes(k_pool, v_pool, block_table, prefix_len, num_q_heads: int, dtype) -> int:
+    head, _ = _head("kvt_mx_decode_workspace_bytes", _mx_pool_args(k_pool, v_pool, dtype), prefix_len, None, block_table,
+                    False)
+    return _native().workspace(*head, int(num_q_heads))
+
+
+def mx_decode_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], scale: Optional[float] = None, *,
+                      out=None, lse=None, return_lse: bool = False, workspace=None, use_workspace: bool = True,
+                      stream=None, checked: bool = False):
+    """``decode_attention`` over 4-bit pages (``kvt_mx_decode_attention``): row b of
+    ``q`` ([B][Hq][D], bf16 or fp32) is the new token of sequence b at position
+    ``prefix_len[b]``, whose K/V was appended first."""
+    return _mx_attention("kvt_mx_decode_attention", "kvt_mx_decode_workspace_bytes", q, k_pool, v_pool, block_table,
+                       prefix_len, None, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
+
+
+def _mx_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, prefix_len, suffix_len, scale, out, lse,
+                return_lse, workspace, use_workspace, stream, checked):
+    import torch
+    if stream is not None:   # what is allocated here belongs to the stream that the kernels run on
+        with _on_stream(stream, k_pool):
+            return _mx_attention(entry, ws_entry, q, k_pool, v_pool, block_table, prefix_len, suffix_len, scale, out,
+                               lse, return_lse, workspace, use_workspace, None, checked)
+    native = _native()
+    pool = _mx_pool_args(k_pool, v_pool, q.dtype)
+    head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
+    Hq, d, device = int(q.shape[1]), pool[4], k_pool.get_device()
+    _check_tokens(q, "q", T, Hq, d, q.dtype)
+    given = [v_pool, q]
+    if out is not None:
+        _check_tokens(out, "out", T, Hq, d, q.dtype)
+        given.append(out)
+    want_lse = return_lse or lse is not None
+    if lse is not None:
+        _check_lse(lse, T, Hq)
+        given.append(lse)
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        given.append(workspace)
+    _check_table(block_table, head[8], device, *given)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    with _on_device(k_pool):
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=k_pool.device)
+        ws_ptr, ws_bytes = None, 0
+        if workspace is not None:
+            ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        elif use_workspace:
+            ws_bytes = native.workspace(lib().address[ws_entry], *head[1:], Hq)
+            if ws_bytes:
+                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=k_pool.device)
+                ws_ptr = workspace.data_ptr()
+        st = native.attend(*head, q.data_ptr(), Hq, float(scale), out.data_ptr(), lse.data_ptr() if want_lse else None,
+                           ws_ptr, ws_bytes, _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, entry)
+    return (out, lse) if want_lse else out
+
+
+def _head_rows(t, name: str, seqs: int, hkv: int, least: int, dtype, device: int) -> int:
+    """The row stride of a contiguous [B][Hkv][>= least] tensor."""
+    shape = t.shape
+    if (t.dtype != dtype or len(shape) != 3 or shape[0] != seqs or shape[1] != hkv or shape[2] < least
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} [{seqs}][{hkv}][>= {least}] tensor, got {tuple(shape)} "
+                         f"{t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on the call's GPU {device}")
+    return shape[2]
+
+
+def attention_weights(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Optional[Sequence[int]],
+                      lse, weights, scale: Optional[float] = None, *, stream=None, checked: bool = False):
+    """What the attention of the new tokens gave every position, summed per
+    kv-head onto ``weights`` (``kvt_attention_weights``, over 4-bit pools
+    ``kvt_mx_attention_weights``).
+
+    ``q`` and ``lse`` are those of an ``extend_attention`` or (``suffix_len``
+    None) ``decode_attention`` call with the same pools, table, lengths and
+    scale.  ``weights``: float32 [B][Hkv][>= longest sequence]; reused positions
+    are added to, new ones set, the entries past a sequence are left alone.
+    Returns ``weights``.
+    """
+    import torch
+    if stream is not None:
+        with _on_stream(stream, k_pool):
+            return attention_weights(q, k_pool, v_pool, block_table, prefix_len, suffix_len, lse, weights, scale,
+                                     checked=checked)
+    four = k_pool.dtype == torch.uint8
+    pool = _mx_pool_args(k_pool, v_pool, q.dtype) if four else _pool_args(k_pool, v_pool)
+    entry = "kvt_mx_attention_weights" if four else "kvt_attention_weights"
+    head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
+    Hq, d, device = int(q.shape[1]), pool[4], k_pool.get_device()
+    _check_tokens(q, "q", T, Hq, d, q.dtype if four else k_pool.dtype)
+    _check_lse(lse, T, Hq)
+    _check_table(block_table, head[8], device, v_pool, q, lse)
+    stride = _head_rows(weights, "weights", head[8], pool[3], 1, torch.float32, device)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    with _on_device(k_pool):
+        st = _native().weights(*head, q.data_ptr(), Hq, float(scale), lse.data_ptr(), weights.data_ptr(), stride,
+                               _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, entry)
+    return weights
+
+
+def evict(k_pool, v_pool, block_table, length: Sequence[int], keep: Sequence[int], weights, to_table, *,
+          sinks: int = 0, recent: int = 0, positions=None, weights_out=None, stream=None, checked: bool = False):
+    """Keep the positions that carry most weight, per sequence and kv-head
+    (``kvt_evict``, in 4-bit pools ``kvt_mx_evict``).
+
+    Of the ``length[b]`` positions of sequence b, n_b = min(length[b], keep[b])
+    stay: the first ``sinks``, the last ``recent`` and the heaviest of the others
+    by ``weights`` (float32 [B][Hkv][>= longest length]), of equal ones the lower
+    position.  Their K/V rows go to rows 0 .. n_b - 1 of the pages of
+    ``to_table``, in ascending order; none of those pages may be among the
+    sequences' own.  Returns (positions, weights_out): int32 and float32
+    [B][Hkv][>= largest n_b], -1 and 0 past n_b; allocated here with that width
+    unless given (both of one width; ``weights_out`` may be ``weights``).
+    """
+    import torch
+    if stream is not None:   # what is allocated here belongs to the stream that it is written on
+        with _on_stream(stream, k_pool):
+            return evict(k_pool, v_pool, block_table, length, keep, weights, to_table, sinks=sinks, recent=recent,
+                         positions=positions, weights_out=weights_out, checked=checked)
+    four = k_pool.dtype == torch.uint8
+    pool = _mx_pool_args(k_pool, v_pool, torch.bfloat16) if four else _pool_args(k_pool, v_pool)
+    entry = "kvt_mx_evict" if four else "kvt_evict"
+    length, keep = [int(x) for x in length], [int(x) for x in keep]
+    if len(keep) != len(length) or not length:
+        raise ValueError("keep must hold one count for each sequence")
+    head, _ = _head(entry, pool, [x - 1 for x in length], None, block_table, checked)
+    kept, n, _ = _native().pack(keep, None, _i32_array)
+    hkv, device = pool[3], k_pool.get_device()
+    if to_table.dtype != torch.int32 or to_table.dim() != 2 or not to_table.is_contiguous():
+        raise ValueError("to_table must be a contiguous int32 [num_seqs][max_blocks] device tensor")
+    _check_table(block_table, n, device, v_pool, to_table)
+    _check_table(to_table, n, device)
+    stride = _head_rows(weights, "weights", n, hkv, max(length), torch.float32, device)
+    width = max(1, max(min(a, b) for a, b in zip(length, keep)))
+    with _on_device(k_pool):
+        if positions is None:
+            cols = width if weights_out is None else weights_out.shape[-1]
+            positions = torch.empty((n, hkv, cols), dtype=torch.int32, device=k_pool.device)
+        out_stride = _head_rows(positions, "positions", n, hkv, width, torch.int32, device)
+        if weights_out is None:
+            weights_out = torch.empty((n, hkv, out_stride), dtype=torch.float32, device=k_pool.device)
+        if _head_rows(weights_out, "weights_out", n, hkv, width, torch.float32, device) != out_stride:
+            raise ValueError("positions and weights_out must have one width")
+        host = to_table.cpu().numpy() if checked else None
+        st = _native().evict(*head, kept, int(sinks), int(recent), weights.data_ptr(), stride, to_table.data_ptr(),
+                             to_table.shape[1], host, positions.data_ptr(), weights_out.data_ptr(), out_stride,
+                             _stream_handle(k_pool))
+    if st != KVT_OK:
+        raise KvtError(st, entry)
+    return positions, weights_out
 
 
 # ---------------------------------------------------------------------------
