@@ -499,8 +499,7 @@ typedef struct {
   const int32_t* to_table_host;  /* HOST copy of to_table, or NULL; non-NULL checks the targets */
   int32_t        to_max_blocks;  /* ceil(n_b/16) <= to_max_blocks for every b */
   int32_t*       positions;      /* DEVICE [B][Hkv][out_stride]: the kept positions, ascending; -1 past n_b */
-  float*         weights_out;    /* DEVICE, the same shape: their weights, 0 past n_b; NULL: not wanted; may be
-                                    weights itself with out_stride = weights_stride */
+  float*         weights_out;    /* DEVICE, the same shape: their weights, 0 past n_b; NULL: not wanted */
   int64_t        out_stride;     /* at least the largest n_b, at most INT32_MAX */
 } kvt_eviction;
 
@@ -522,6 +521,7 @@ typedef struct {
  * KVT_ERR_OUT_OF_RANGE; otherwise the result is unspecified).  A target id
  * outside the pool is skipped, a source id outside is clamped to the last page.
  * Source pages are read only: shared ones stay as they are for the others.
+ * weights, positions, weights_out and the pools may not overlap.
  */
 kvt_status kvt_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream);
 kvt_status kvt_mx_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream);

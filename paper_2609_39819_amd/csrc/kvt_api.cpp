@@ -1181,56 +1181,58 @@ bool workspace_apart(const kvt_pool* pool, const void* q, const void* out, const
          (lse == nullptr || !overlaps(workspace, bytes, lse, (size_t)T * num_q_heads * sizeof(float)));
 }
 
-// Key splits of a decoding step over 4-bit pages: every sequence has its own
-// count, the partial sets being those of the largest.
+// A decoding step over 4-bit pages, launch by launch: see MxDecodeArgs.
 struct MxDecodePlan {
-  std::vector<int> order;        // sequences, longest key range first
-  std::vector<int32_t> nsplit;   // by sequence
-  int sets = 1;                  // the largest count
-  int chunks = 1;                // workgroups that share a kv-head's query heads
+  std::vector<int> order;          // sequences, longest key range first
+  std::vector<int32_t> share;      // by launch: tiles of a slot, 0: slot x is sequence x
+  std::vector<int32_t> parts;      // by place in `order`: slots that hold a part of the sequence
+  int chunks = 1;                  // workgroups that share a kv-head's query heads
+  int64_t part_rows = 0;
   size_t ws_bytes = 0;
 };
+
+int64_t mx_tiles(const kvt_seqs* seqs, int b) {
+  return ((int64_t)seqs->prefix_len[b] + kvt::kDecKeysPerTile) / kvt::kDecKeysPerTile;
+}
+size_t mx_part_o_bytes(const kvt_pool* pool, int64_t part_rows) {
+  return ((size_t)part_rows * pool->head_dim * sizeof(float) + 255) / 256 * 256;
+}
 
 MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   MxDecodePlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
   p.chunks = (G + kvt::kMxDecMaxRows - 1) / kvt::kMxDecMaxRows;
-  const int64_t heads = (int64_t)pool->num_kv_heads * p.chunks;
   p.order = longest_first(seqs);
-  p.nsplit.assign(B, 1);
-  const int64_t longest = (int64_t)seqs->prefix_len[p.order.front()] + 1;
-  const int64_t cus = device_cus(), all = total_keys(seqs) * heads;
-  auto splits = [&](int b, int64_t chunk) {
-    const int64_t n = ((int64_t)seqs->prefix_len[b] + 1 + chunk / 2) / chunk;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(kvt::kMaxPartials, n));
-  };
-  const double key_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) / kvt::kBlock;
-  const double one = 25e3, every = 5.5e6;   // bytes per us
-  auto cost = [&](int64_t c) {
-    FreeTimes cu(0.0, cus, 0.0, 0);
-    int sets = 1;
-    for (int i = 0; i < B; ++i) {
-      const int b = p.order[i], n = splits(b, c);
-      cu.run(n * heads, std::ceil((double)(seqs->prefix_len[b] + 1) / n) * key_bytes + 60e3);
-      sets = std::max(sets, n);
+  p.parts.assign(B, 1);
+  const int64_t heads = (int64_t)pool->num_kv_heads * p.chunks;
+  for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) total += mx_tiles(seqs, p.order[c0 + i]);
+    const int64_t longest = mx_tiles(seqs, p.order[c0]);
+    // two workgroups to a CU, of at least 16 tiles (four for each wave)
+    const int64_t slots = std::max<int64_t>(1, 2 * device_cus() / heads);
+    int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
+    // a sequence lies in at most one slot more than its tiles fill
+    share = std::max(share, (longest + kvt::kMaxPartials - 2) / (kvt::kMaxPartials - 1));
+    bool split = false;
+    int64_t begin = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t end = begin + mx_tiles(seqs, p.order[c0 + i]);
+      const int parts = (int)((end - 1) / share - begin / share + 1);
+      split = split || parts > 1;
+      p.parts[c0 + i] = parts;
+      if (parts > 1) p.part_rows += (int64_t)parts * num_q_heads;
+      begin = end;
     }
-    return cu.drain(one, every) +
-           (sets > 1 ? 4.0 + 2.0 * (double)part_bytes(pool, sets, (int64_t)B * num_q_heads) / 4.5e6 : 0.0);
-  };
-  int64_t chunk = 2 * longest;   // unsplit
-  double best = 0.97 * cost(chunk);
-  for (double f : {0.7, 1.0, 1.5, 2.0, 3.0, 4.0}) {   // units per CU
-    if (B > 32 && f != 1.0 && f != 2.0 && f != 4.0) continue;   // large batches: fewer, for the host's sake
-    const int64_t c = std::max<int64_t>(128, (int64_t)((double)all / (f * (double)cus)));
-    if (splits(p.order.front(), c) == 1) continue;
-    const double t = cost(c);
-    if (t < best) best = t, chunk = c;
+    p.share.push_back(split ? (int32_t)share : 0);
   }
-  for (int b = 0; b < B; ++b) {
-    p.nsplit[b] = splits(b, chunk);
-    p.sets = std::max(p.sets, (int)p.nsplit[b]);
+  if (p.part_rows > INT32_MAX) {
+    p.parts.assign(B, 1);
+    p.share.assign(p.share.size(), 0);
+    p.part_rows = 0;
   }
-  if (p.sets > 1) p.ws_bytes = part_bytes(pool, p.sets, (int64_t)B * num_q_heads);
+  if (p.part_rows > 0) p.ws_bytes = mx_part_o_bytes(pool, p.part_rows) + (size_t)p.part_rows * 2 * sizeof(float);
   return p;
 }
 
@@ -1344,32 +1346,51 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     most_rows = std::max(most_rows, (int64_t)seqs->suffix_len[b] * G);
   }
   const bool step = most_rows <= 32;
-  const int keys = kvt::weights_keys_per_unit(format);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
     const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
     a.nseq = n;
-    int64_t units = 0, longest = 0;
+    int64_t units = 0, narrow = 0;
+    const int keys = step ? kvt::kWeightsStepKeys : kvt::kWeightsWideKeys;
     for (int i = 0; i < n; ++i) {
       const int b = order[c0 + i];
       const int64_t len = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
       a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
+      units += step ? (len + keys - 1) / keys : len / keys;
+    }
+    // turn: wide workgroups in whole rounds of the CUs, and what a last, mostly
+    // empty round would hold as narrow ones (a narrow one of 32 keys takes a third
+    // of a wide one's time instead of an eighth: it loads as many rows)
+    int64_t drop = 0;   // wide workgroups of each kv-head that become narrow ones
+    if (!step) {
+      const int64_t excess = units * pool->num_kv_heads % device_cus();
+      const int64_t thin = (excess * 8 + device_cus() - 1) / device_cus();   // rounds of narrow ones
+      if (thin < 3) drop = (excess + pool->num_kv_heads - 1) / pool->num_kv_heads;
+    }
+    units = 0;
+    for (int i = 0; i < n; ++i) {
+      const int64_t len = (int64_t)a.seq[i].prefix + a.seq[i].suffix;
       a.unit_begin[i] = (int32_t)units;
-      units += (len + keys - 1) / keys;
-      longest = std::max(longest, len);
-      if (units * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
+      a.narrow_begin[i] = (int32_t)narrow;
+      int64_t wide = step ? (len + keys - 1) / keys : len / keys;
+      const int64_t fewer = std::min(wide, drop);
+      wide -= fewer;
+      drop -= fewer;
+      units += wide;
+      if (!step) narrow += (len - wide * keys + 31) / 32;
+      if ((units + narrow) * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
     }
     a.unit_begin[n] = (int32_t)units;
+    a.narrow_begin[n] = (int32_t)narrow;
     hipError_t e;
     if (step) {
-      // workgroups of at least 512 keys, about four to a CU
-      const int64_t want = (4 * (int64_t)device_cus() + (int64_t)n * pool->num_kv_heads - 1) /
-                           ((int64_t)n * pool->num_kv_heads);
-      a.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(want, (longest + 511) / 512));
-      e = kvt::launch_weights_step(a, format, pool->dtype, pool->head_dim, n * a.nsplit * pool->num_kv_heads, s);
+      const int64_t slots = std::max<int64_t>(1, 4 * (int64_t)device_cus() / pool->num_kv_heads);   // four to a CU
+      a.share = (int32_t)std::max<int64_t>(4, (units + slots - 1) / slots);
+      e = kvt::launch_weights_step(a, format, pool->dtype, pool->head_dim,
+                                   (int)((units + a.share - 1) / a.share) * pool->num_kv_heads, s);
     } else {
-      const int waves = (int)std::min<int64_t>(8, (most_rows + 31) / 32);
-      e = kvt::launch_weights_turn(a, format, pool->dtype, pool->head_dim, waves, (int)units * pool->num_kv_heads, s);
+      e = kvt::launch_weights_turn(a, format, pool->dtype, pool->head_dim, (int)(units + narrow) * pool->num_kv_heads,
+                                   s);
     }
     if (e != hipSuccess) return device_error(e);
   }
@@ -1403,13 +1424,12 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
       ev->out_stride < most_kept || ev->out_stride > INT32_MAX ? 0 : head_rows_bytes(pool, B, ev->out_stride, ev->out_stride);
   if (in_bytes == 0 || out_bytes == 0) return KVT_ERR_INVALID_ARG;
   const size_t held = pool_tensor_bytes(pool, mx);
-  const bool in_place = ev->weights_out == ev->weights && ev->out_stride == ev->weights_stride;
   auto in_pool = [&](const void* p, size_t n) { return overlaps(p, n, pool->k, held) || overlaps(p, n, pool->v, held); };
   if (overlaps(ev->positions, out_bytes, ev->weights, in_bytes) || in_pool(ev->positions, out_bytes) ||
       in_pool(ev->weights, in_bytes) || overlaps(pool->k, held, pool->v, held))
     return KVT_ERR_INVALID_ARG;
   if (ev->weights_out != nullptr &&
-      ((!in_place && overlaps(ev->weights_out, out_bytes, ev->weights, in_bytes)) ||
+      (overlaps(ev->weights_out, out_bytes, ev->weights, in_bytes) ||
        overlaps(ev->weights_out, out_bytes, ev->positions, out_bytes) || in_pool(ev->weights_out, out_bytes)))
     return KVT_ERR_INVALID_ARG;
   if ((st = check_table_ids(pool, seqs)) != KVT_OK) return st;
@@ -1979,40 +1999,73 @@ kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, c
   if (st != KVT_OK) return st;
   if (T != seqs->num_seqs) return KVT_ERR_INVALID_ARG;   // one new token per sequence
   MxDecodePlan plan = mx_decode_plan(pool, seqs, num_q_heads);
-  if (plan.sets > 1) {
+  if (plan.ws_bytes > 0) {
     if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
-      plan.nsplit.assign(seqs->num_seqs, 1);
-      plan.sets = 1;
+      plan.parts.assign(seqs->num_seqs, 1);
+      plan.share.assign(plan.share.size(), 0);
+      plan.ws_bytes = 0;
     } else {
       if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
       if (!aligned16(workspace) || !workspace_apart(pool, q, out, lse, num_q_heads, T, workspace, plan.ws_bytes))
         return KVT_ERR_INVALID_ARG;
     }
   }
-  ExtendPlan sets;
-  sets.nsplit = plan.sets;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  kvt::ExtendArgs a = base_args(pool, seqs, q, num_q_heads, scale, out, lse, T, sets, workspace);
-  bool gaps = false;
-  for (int c0 = 0; c0 < seqs->num_seqs; c0 += kvt::kSeqsPerLaunch) {
+  kvt::MxDecodeArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.out = out;
+  a.lse = lse;
+  a.block_table = seqs->block_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.group = num_q_heads / pool->num_kv_heads;
+  a.chunks = plan.chunks;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  if (plan.ws_bytes > 0) {
+    a.part_o = reinterpret_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + mx_part_o_bytes(pool, plan.part_rows));
+  }
+  kvt::MxJoinArgs join;
+  join.part_o = a.part_o;
+  join.part_ml = a.part_ml;
+  join.out = out;
+  join.lse = lse;
+  join.num_q_heads = num_q_heads;
+  int64_t part_row = 0;
+  for (int c0 = 0, launch = 0; c0 < seqs->num_seqs; c0 += kvt::kSeqsPerLaunch, ++launch) {
     const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - c0);
     a.nseq = n;
-    int32_t units = 0;
+    a.share = plan.share[launch];
+    join.nseq = 0;
+    int64_t tiles = 0;
     for (int i = 0; i < n; ++i) {
-      const int b = plan.order[c0 + i];
+      const int b = plan.order[c0 + i], parts = plan.parts[c0 + i];
       a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], 1, b};   // row of sequence b is b
-      a.last[i] = (uint8_t)plan.nsplit[b];
-      a.unit_begin[i] = units;
-      units += plan.nsplit[b];
-      gaps = gaps || plan.nsplit[b] < plan.sets;
+      a.tile_begin[i] = (int32_t)tiles;
+      a.part_row[i] = (int32_t)part_row;
+      tiles += mx_tiles(seqs, b);
+      if (parts > 1) {
+        join.part_row[join.nseq] = (int32_t)part_row;
+        join.row[join.nseq] = b * num_q_heads;
+        join.parts[join.nseq++] = (uint8_t)parts;
+        part_row += (int64_t)parts * num_q_heads;
+      }
     }
-    a.unit_begin[n] = units;
-    const int64_t grid = (int64_t)units * pool->num_kv_heads * plan.chunks;
+    if (tiles > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    a.tile_begin[n] = (int32_t)tiles;
+    const int64_t slots = a.share > 0 ? (tiles + a.share - 1) / a.share : n;
+    const int64_t grid = slots * pool->num_kv_heads * plan.chunks;
     if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
-    const hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, plan.chunks, (int)grid, s);
+    hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, (int)grid, s);
+    if (e == hipSuccess && join.nseq > 0) e = kvt::launch_mx_join(join, pool->dtype, pool->head_dim, s);
     if (e != hipSuccess) return device_error(e);
   }
-  return plan.sets > 1 ? combine(a, pool, out, lse, T, num_q_heads, plan.sets, gaps, s) : KVT_OK;
+  return KVT_OK;
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }

@@ -3,14 +3,15 @@
 // Per sequence and kv-head, of L positions n = min(L, keep) stay: the first
 // `sinks`, the last `recent`, and of those between them the heaviest, of equal
 // ones the lowest positions.  Two launches:
-//   * select: one workgroup per (sequence, kv-head).  The k-th largest weight is
-//     found as a 32-bit key, 8 bits at a time from the top: a histogram of the
-//     keys that agree so far (integer counts in LDS, so their order does not
-//     matter), then the bin that holds the k-th.  Then the positions are taken in
-//     order: a scan counts those that stay, and gives each its place.
+//   * select: one workgroup per (sequence, kv-head).  The weights become 32-bit
+//     keys in the same order.  The k-th largest is found 11, 11 and 10 bits at a
+//     time from the top: a histogram of the keys that agree so far (integer
+//     counts in LDS, so their order does not matter), then the bin that holds the
+//     k-th.  Every wave owns a sixteenth of the positions, in order, so that its
+//     ballots count what stays before a position, and the waves' totals the rest.
 //   * move: the kept rows into the other pages, 16 bytes a lane in the order of
 //     the targets; reads are whole rows.  HBM-bound: 2 rows read, 2 written per
-//     kept position and kv-head.
+//     kept position and kv-head.  It brings their weights, too.
 #include "kvt_mx_device.h"
 
 namespace kvt {
@@ -20,116 +21,137 @@ using namespace dev;
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kPer = 4;                            // neighbouring positions of one thread
+constexpr int kSelBins = 2048, kSelCopies = 2;     // histograms: fewer waves on one counter
 
-// Unsigned keys in the order of the weights; -0 is 0, and a NaN, of either sign,
-// comes after +infinity.
+// Unsigned keys in the order of the weights, between 0, for places past the
+// end, and kForced: -0 is 0, and a NaN, of either sign, comes after +infinity.
+constexpr unsigned kForced = 0xffffffffu;
 __device__ __forceinline__ unsigned order_key(float w) {
   const unsigned u = __builtin_bit_cast(unsigned, w + 0.0f);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const unsigned key = u ^ ((unsigned)((int)u >> 31) | 0x80000000u);   // negative ones inverted, the others above them
+  return w != w ? kForced - 1 : key;
 }
 
+// BY: weights of a lane that are taken at a time.  2 for short sequences, whose
+// waves would pass over 8 where they have one (1000 positions: 8.1 us, with 8
+// 10.4; 16 contexts of 8192..65536 positions, 8 kv-heads: 72 and 47.5).
+template <int BY>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
-  __shared__ unsigned hist[kSelWaves][256];        // one per wave: fewer lanes on one counter
-  __shared__ unsigned pick[2];                     // bin, counts above it
+  __shared__ unsigned hist[kSelCopies][kSelBins];
+  __shared__ unsigned pick[2];                     // bin, count above it
   __shared__ unsigned totals[2][kSelWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % a.num_kv_heads, i = blockIdx.x / a.num_kv_heads;
   const EvictDesc sd = a.seq[i];
   const int L = sd.length, n = sd.keep;
   const int64_t row = (int64_t)sd.seq * a.num_kv_heads + g;
   const float* w = a.weights + row * a.stride;
   int32_t* out = a.positions + row * a.out_stride;
-  float* wout = a.weights_out != nullptr ? a.weights_out + row * a.out_stride : nullptr;
-  const int lo = L > n ? a.sinks : L, hi = L > n ? L - a.recent : L;   // positions that compete
-
-  // ---- the border: keys above `edge` stay, and the first `even` equal to it
-  unsigned edge = 0, even = 0;
-  int k = n - (L - (hi - lo));                     // how many of them stay
-  if (L > n && k > 0) {
-    unsigned want = (unsigned)k;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int b = tid; b < kSelWaves * 256; b += kSelThreads) (&hist[0][0])[b] = 0;
-      __syncthreads();
-      for (int p = lo + tid; p < hi; p += kSelThreads) {
-        const unsigned u = order_key(w[p]);
-        if (shift == 24 || (u >> (shift + 8)) == (edge >> (shift + 8))) atomicAdd(&hist[wave][(u >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      // counts from the largest bin down; thread t holds bin 255 - t
-      unsigned count = 0;
-      if (tid < 256) {
-#pragma unroll
-        for (int x = 0; x < kSelWaves; ++x) count += hist[x][255 - tid];
-      }
-      unsigned upto = count;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const unsigned below = __shfl_up(upto, d);
-        if (lane >= d) upto += below;
-      }
-      if (tid < 256 && lane == 63) totals[0][wave] = upto;
-      __syncthreads();
-      if (tid < 256) {
-        for (int x = 0; x < wave; ++x) upto += totals[0][x];
-        if (upto >= want && upto - count < want) pick[0] = 255 - tid, pick[1] = upto - count;
-      }
-      __syncthreads();
-      edge |= pick[0] << shift;
-      want -= pick[1];
-    }
-    even = want;
-  }
-
-  // ---- the positions in order.  A thread's count packs what stays for certain
-  // and what equals the edge; the latter stay while they are among the first.
-  unsigned sure_before = 0, equal_before = 0;      // of the tiles before
-  for (int p0 = 0; p0 < L; p0 += kSelThreads * kPer) {
-    unsigned sure = 0, equal = 0, mask_sure = 0, mask_equal = 0;
-    float val[kPer];
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int p = p0 + tid * kPer + x;
-      if (p >= L) break;
-      val[x] = w[p];
-      const unsigned u = order_key(val[x]);
-      if (p < lo || p >= hi || (k > 0 && u > edge)) ++sure, mask_sure |= 1u << x;
-      else if (k > 0 && u == edge) ++equal, mask_equal |= 1u << x;
-    }
-    unsigned s = sure, e = equal;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const unsigned ps = __shfl_up(s, d), pe = __shfl_up(e, d);
-      if (lane >= d) s += ps, e += pe;
-    }
-    if (lane == 63) totals[0][wave] = s, totals[1][wave] = e;
-    __syncthreads();
-    unsigned all_s = 0, all_e = 0;
-#pragma unroll
-    for (int x = 0; x < kSelWaves; ++x) {
-      const unsigned ts = totals[0][x], te = totals[1][x];
-      if (x < wave) s += ts, e += te;
-      all_s += ts, all_e += te;
-    }
-    __syncthreads();
-    s += sure_before - sure, e += equal_before - equal;   // before this thread's first position
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const bool is_sure = mask_sure >> x & 1, is_equal = mask_equal >> x & 1;
-      if (is_sure || (is_equal && e < even)) {
-        const int64_t at = (int64_t)s + min(e, even);
-        out[at] = p0 + tid * kPer + x;
-        if (wout != nullptr) wout[at] = val[x];
-      }
-      s += is_sure, e += is_equal;
-    }
-    sure_before += all_s, equal_before += all_e;
-  }
+  float* wout = a.weights_out != nullptr ? a.weights_out + row * a.out_stride : nullptr;   // its first n: by move
   for (int64_t x = n + tid; x < a.out_stride; x += kSelThreads) {
     out[x] = -1;
     if (wout != nullptr) wout[x] = 0.f;
   }
+  if (L == n) {                                    // everything stays
+    for (int p = tid; p < n; p += kSelThreads) out[p] = p;
+    return;
+  }
+
+  // ---- this wave's positions from, from + 64, ..: `steps` of one each lane
+  const int steps = (L + kSelThreads - 1) / kSelThreads;
+  const int from = wave * steps * 64 + lane;
+  const int end = min(L, (wave + 1) * steps * 64);
+  const int lo = a.sinks, hi = L - a.recent;       // positions that compete
+  // f(key, position) of all positions of this wave, 64 at a time, in order (past
+  // its end with keys 0).  The weights come from the L2 each time (a read of 65536
+  // is 2 us; held in registers they spill); what takes time is the instructions for
+  // each, so groups that compete as a whole skip the tests for the rest.
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    for (int j0 = 0; j0 < steps; j0 += BY) {
+      const int p0 = from + j0 * 64;
+      const int g0 = __builtin_amdgcn_readfirstlane(p0 - lane), g1 = g0 + BY * 64;   // of the group
+      if (g0 >= end) break;
+      float raw[BY];                               // loads without a branch between them: all in flight
+#pragma unroll
+      for (int j = 0; j < BY; ++j) raw[j] = w[min(p0 + j * 64, L - 1)];
+      if (g0 >= lo && g1 <= hi && g1 <= end) {
+#pragma unroll
+        for (int j = 0; j < BY; ++j) f(order_key(raw[j]), p0 + j * 64);
+      } else {
+#pragma unroll
+        for (int j = 0; j < BY; ++j) {
+          const int p = p0 + j * 64;
+          f(p >= end ? 0u : p < lo || p >= hi ? kForced : order_key(raw[j]), p);
+        }
+      }
+    }
+  };
+
+  // ---- the n-th largest key: larger ones stay, and the first `even` equal to it
+  unsigned edge = 0, even = (unsigned)n;
+  for (int b = tid; b < kSelCopies * kSelBins; b += kSelThreads) (&hist[0][0])[b] = 0;
+  __syncthreads();
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+    unsigned* mine = hist[wave % kSelCopies];
+    if (pass == 0) {
+      each([&](unsigned u, int) __attribute__((always_inline)) {
+        if (u != 0) atomicAdd(&mine[u >> 21], 1u);
+      });
+    } else {
+      const int top = pass == 1 ? 21 : 10;
+      const unsigned agreed = edge >> top;
+      each([&](unsigned u, int) __attribute__((always_inline)) {
+        if ((u >> top) == agreed) atomicAdd(&mine[u >> shift & (bins - 1)], 1u);
+      });
+    }
+    __syncthreads();
+    // counts from the largest bin down; thread t holds bins 2047 - 2t and 2046 - 2t,
+    // and clears them for the next pass
+    unsigned c0 = 0, c1 = 0;
+#pragma unroll
+    for (int x = 0; x < kSelCopies; ++x) {
+      c0 += hist[x][kSelBins - 1 - 2 * tid], c1 += hist[x][kSelBins - 2 - 2 * tid];
+      hist[x][kSelBins - 1 - 2 * tid] = hist[x][kSelBins - 2 - 2 * tid] = 0;
+    }
+    unsigned upto = c0 + c1;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned below = __shfl_up(upto, d);
+      if (lane >= d) upto += below;
+    }
+    if (lane == 63) totals[0][wave] = upto;
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) upto += totals[0][x];
+    const unsigned before = upto - c0 - c1;
+    if (before < even && before + c0 >= even) pick[0] = kSelBins - 1 - 2 * tid, pick[1] = before;
+    else if (before + c0 < even && upto >= even) pick[0] = kSelBins - 2 - 2 * tid, pick[1] = before + c0;
+    __syncthreads();
+    edge |= pick[0] << shift;
+    even -= pick[1];
+  }
+
+  // ---- the places of what stays: what the waves before this one keep, then ballots
+  unsigned s = 0, e = 0;
+  each([&](unsigned u, int) __attribute__((always_inline)) {
+    s += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u > edge));
+    e += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == edge));
+  });
+  __syncthreads();                                 // totals are read
+  if (lane == 0) totals[0][wave] = s, totals[1][wave] = e;
+  __syncthreads();
+  s = e = 0;
+  for (int x = 0; x < wave; ++x) s += totals[0][x], e += totals[1][x];
+  each([&](unsigned u, int p) __attribute__((always_inline)) {
+    const uint64_t sure = __builtin_amdgcn_ballot_w64(u > edge), equal = __builtin_amdgcn_ballot_w64(u == edge);
+    if ((sure | equal) == 0) return;
+    const unsigned sb = __builtin_amdgcn_mbcnt_hi((unsigned)(sure >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)sure, s));
+    const unsigned eb =
+        __builtin_amdgcn_mbcnt_hi((unsigned)(equal >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)equal, e));
+    if (u > edge || (u == edge && eb < even)) out[sb + min(eb, even)] = p;
+    s += __builtin_popcountll(sure), e += __builtin_popcountll(equal);
+  });
 }
 
 // A page of targets per workgroup and kv-head.  Rows are ROW bytes of 16-byte
@@ -145,11 +167,15 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a) {
   const EvictDesc sd = a.seq[si];
   const int page = unit - a.unit_begin[si];
   const int32_t to = a.to_table[(int64_t)sd.seq * a.to_max_blocks + page];
-  if (to < 0 || (int64_t)to >= a.num_blocks) return;   // skipped, as an append's
   const int32_t* from = a.positions + ((int64_t)sd.seq * hkv + g) * a.out_stride + page * kBlock;
   const int32_t* bt = a.block_table + (int64_t)sd.seq * a.max_blocks;
   const int rows = min(kBlock, sd.keep - page * kBlock);
   const int64_t dst = ((int64_t)to * hkv + g) * kPage;
+  if (a.weights_out != nullptr && threadIdx.x < rows) {
+    const int64_t row = (int64_t)sd.seq * hkv + g;
+    a.weights_out[row * a.out_stride + page * kBlock + threadIdx.x] = a.weights[row * a.stride + from[threadIdx.x]];
+  }
+  if (to < 0 || (int64_t)to >= a.num_blocks) return;   // skipped, as an append's
   auto source = [&](int i, int& slot) __attribute__((always_inline)) {
     const int pos = from[i];
     const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
@@ -183,7 +209,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a) {
 }  // namespace
 
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)a.nseq * a.num_kv_heads), dim3(kSelThreads), 0, stream, a);
+  const dim3 grid((unsigned)a.nseq * a.num_kv_heads), block(kSelThreads);
+  if (a.seq[0].length <= 4 * kSelThreads) hipLaunchKernelGGL((evict_select_kernel<2>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((evict_select_kernel<8>), grid, block, 0, stream, a);   // longest first
   return hipGetLastError();
 }
 

@@ -1,6 +1,6 @@
 // Launch descriptors of the calls over 4-bit pages and of eviction
 // (kvt_mx_append.hip, kvt_mx_extend.hip, kvt_mx_decode.hip, kvt_weights.hip,
-// kvt_evict.hip); the attention calls over 4-bit pages take ExtendArgs.
+// kvt_evict.hip); the extend call over 4-bit pages takes ExtendArgs.
 #pragma once
 
 #include "kvt_internal.h"
@@ -30,8 +30,49 @@ struct MxRowsArgs {
   SeqDesc seq[kSeqsPerLaunch];  // in packed-row order
 };
 
-// Query heads of one kv-head that one decode4 workgroup serves.
+// Decoding: query heads of one kv-head that one workgroup serves.
 constexpr int kMxDecMaxRows = 32;
+
+// Decoding: the tiles of kDecKeysPerTile keys of a launch's sequences lie one
+// after the other, and slot x of a kv-head takes tiles x * share .. (x + 1) *
+// share - 1: parts of as many sequences as lie there.  share 0: slot x is
+// sequence x.  A sequence in more than one slot leaves a partial result in each,
+// n of them from row part_row on, [n][Hq].
+struct MxDecodeArgs {
+  const void* q;
+  const void* k_pool;
+  const void* v_pool;
+  void* out;
+  float* lse;           // may be null
+  float* part_o;        // [partial rows][D]
+  float* part_ml;       // [partial rows][2]  (reference max in log2 units, row sum)
+  const int32_t* block_table;
+  int64_t num_blocks;
+  int32_t max_blocks;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;        // Hq / Hkv
+  int32_t chunks;       // workgroups that share a kv-head's query heads
+  float scale_log2;
+  int32_t share;
+  int32_t nseq;
+  int32_t tile_begin[kSeqsPerLaunch + 1];
+  int32_t part_row[kSeqsPerLaunch];
+  SeqDesc seq[kSeqsPerLaunch];
+};
+
+// The join of a step's split sequences.
+struct MxJoinArgs {
+  const float* part_o;
+  const float* part_ml;
+  void* out;
+  float* lse;
+  int32_t num_q_heads;
+  int32_t nseq;
+  int32_t part_row[kSeqsPerLaunch];
+  int32_t row[kSeqsPerLaunch];      // output row of head 0
+  uint8_t parts[kSeqsPerLaunch];
+};
 
 // Attention weights per position.
 struct WeightsArgs {
@@ -47,9 +88,10 @@ struct WeightsArgs {
   int32_t num_kv_heads;
   int32_t group;        // Hq / Hkv
   float scale_log2;
-  int32_t nsplit;       // step kernel: workgroups per (sequence, kv-head)
+  int32_t share;        // step kernel: tiles of a workgroup
   int32_t nseq;
-  int32_t unit_begin[kSeqsPerLaunch + 1];
+  int32_t unit_begin[kSeqsPerLaunch + 1];   // prefix sums of the sequences' tiles (step kernel) or wide workgroups
+  int32_t narrow_begin[kSeqsPerLaunch + 1]; // turn kernel: of the narrow ones, for the keys after those
   SeqDesc seq[kSeqsPerLaunch];
 };
 
@@ -80,21 +122,20 @@ struct EvictArgs {
   EvictDesc seq[kSeqsPerLaunch];
 };
 
-static_assert(sizeof(MxRowsArgs) <= 8192 && sizeof(WeightsArgs) <= 8192 && sizeof(EvictArgs) <= 8192,
+static_assert(sizeof(MxRowsArgs) <= 8192 && sizeof(MxDecodeArgs) <= 8192 && sizeof(MxJoinArgs) <= 8192 && sizeof(WeightsArgs) <= 8192 && sizeof(EvictArgs) <= 8192,
               "kernel argument block too large");
 
 hipError_t launch_mx_append(const MxRowsArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_mx_read(const MxRowsArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_mx_extend(const ExtendArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
-// chunks: workgroups that share a kv-head's query heads.  Every sequence has
-// its own split count (ExtendArgs::last); nsplit is the number of partial sets.
-hipError_t launch_mx_decode(const ExtendArgs& a, int dtype, int head_dim, int chunks, int grid, hipStream_t stream);
+hipError_t launch_mx_decode(const MxDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
+hipError_t launch_mx_join(const MxJoinArgs& a, int dtype, int head_dim, hipStream_t stream);
 // format: a kvt_dtype of the K pool, or kMx for 4-bit pages; dtype is q's.
 constexpr int kMx = 2;
 hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
-hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int waves, int grid,
-                               hipStream_t stream);
-int weights_keys_per_unit(int format);   // turn kernel: keys of one workgroup
+hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
+constexpr int kWeightsStepKeys = 32;      // step kernel: keys of one tile
+constexpr int kWeightsWideKeys = 256;     // turn kernel: keys of a wide workgroup (a narrow one: 32)
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t stream);
 hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int grid, hipStream_t stream);
 

@@ -43,12 +43,13 @@ __device__ __forceinline__ int swz_mx(int key) {
 }
 
 template <typename T, int D, int NB>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 ? 1 : 2) void mx_decode_kernel(const ExtendArgs a, const int chunks) {
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 ? 1 : 2) void mx_decode_kernel(const MxDecodeArgs a) {
   constexpr int NT = kTerms<T>;
   constexpr int KS = D / 32;                     // score steps = words of a lane's codes
   constexpr int CT = D / 16;                     // 16-column tiles of the output
   constexpr int64_t kPage = mx_page_bytes(D);
   constexpr float kRescaleSlack = 8.0f;
+  constexpr int DEPTH = 2;                       // tiles in flight
   __shared__ MxDecSlot<D, NB> ring[kWaves];
   __shared__ float ml[kWaves][NB * 16][2];       // per wave and row: m (log2 units), l
 
@@ -58,25 +59,38 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   const int l16 = lane & 15;
   const int qd = lane >> 4;
 
-  // ---- which (sequence, kv-head, key split, head chunk) this workgroup owns
+  // ---- which kv-head, query heads and tiles this workgroup owns
   const int hkv = a.num_kv_heads;
   const int G = a.group;
+  const int chunks = a.chunks;
   const int g = blockIdx.x % hkv;
   const int rest = blockIdx.x / hkv;
   const int unit = chunks == 1 ? rest : rest / chunks;
   const int per_chunk = (G + chunks - 1) / chunks;
   const int head0 = (rest - unit * chunks) * per_chunk;
   const int heads = min(per_chunk, G - head0);
-  const int si = find_seq(a.unit_begin, a.nseq, unit);
+  const int share = a.share;
+  const char* kpool = reinterpret_cast<const char*>(a.k_pool);
+  const char* vpool = reinterpret_cast<const char*>(a.v_pool);
+  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
+  __bf16* vs = reinterpret_cast<__bf16*>(ring[wave].bytes);
+  const lds_bf16* vl = (const lds_bf16*)vs;
+  const int vkey = 4 * qd + (l16 >> 2);          // key of this lane's transposed reads
+  const int vrow = vkey * D + (l16 & 1) * 4, vsub = (l16 >> 1) & 1, vswz = swz_mx<D>(vkey);
+  const float c = a.scale_log2;
+
+  int si = share == 0 ? unit : find_seq(a.tile_begin, a.nseq, unit * share);
+  int from = share == 0 ? a.tile_begin[si] : unit * share;
+  const int to = share == 0 ? a.tile_begin[si + 1] : min(from + share, a.tile_begin[a.nseq]);
+  for (; from < to; ++si) {   // the sequences of this slot
   const SeqDesc sd = a.seq[si];
-  const int nsplit = a.last[si];
-  const int split = unit - a.unit_begin[si];
+  const int begin = a.tile_begin[si], end = a.tile_begin[si + 1];
+  const int split = share == 0 ? 0 : unit - begin / share;
+  const int nsplit = share == 0 ? 1 : (end - 1) / share - begin / share + 1;
+  const int j0 = from - begin, j1 = min(to, end) - begin;
+  from = begin + j1;
   const int L = sd.prefix + 1;                   // keys 0..P_b
   const int nblk = (L + kBlock - 1) / kBlock;
-  const int ntk = (L + kTK - 1) / kTK;
-  const int per_split = (ntk + nsplit - 1) / nsplit;
-  const int j0 = split * per_split;
-  const int j1 = min(ntk, j0 + per_split);
   const int nt = j1 - j0 > wave ? (j1 - j0 - wave + kWaves - 1) / kWaves : 0;   // this wave's tiles
 
   // ---- this lane's query rows (rows past the last head repeat it and are
@@ -90,18 +104,13 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     for (int kk = 0; kk < KS; ++kk) load_terms(qp + kk * 8, qreg[b][kk]);
   }
 
-  const char* kpool = reinterpret_cast<const char*>(a.k_pool);
-  const char* vpool = reinterpret_cast<const char*>(a.v_pool);
   const __attribute__((address_space(4))) int32_t* bt =
       (const __attribute__((address_space(4))) int32_t*)(a.block_table + (int64_t)sd.seq * a.max_blocks);
-  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
-
   auto page_ids = [&](int j, uint32_t (&ids)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int page = __builtin_amdgcn_readfirstlane(min(j * 2 + p, nblk - 1));
-      const uint32_t raw = (uint32_t)bt[page];
-      ids[p] = __builtin_amdgcn_readfirstlane(raw > nb_max ? nb_max : raw);
+      ids[p] = (uint32_t)bt[page];
     }
   };
   // one tile in flight: per page, the lane's codes and scales of key l16
@@ -115,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     for (int p = 0; p < 2; ++p) {
       const int page = min(j * 2 + p, nblk - 1);
       const int slot = min(l16, L - 1 - page * kBlock);
-      const int64_t at = ((int64_t)ids[p] * hkv + g) * kPage;
+      const int64_t at = ((int64_t)min(ids[p], nb_max) * hkv + g) * kPage;
       const int code = slot * (D / 2) + qd * (D / 8);
       const int scale = mx_code_bytes(D) + slot * (D / 32) + (D == 128 ? qd : qd >> 1);
       const char* ks = kpool + at;
@@ -144,11 +153,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) o[b][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
-  const float c = a.scale_log2;
-  __bf16* vs = reinterpret_cast<__bf16*>(ring[wave].bytes);
-  const lds_bf16* vl = (const lds_bf16*)vs;
-  const int vkey = 4 * qd + (l16 >> 2);          // key of this lane's transposed reads
-  const int vrow = vkey * D + (l16 & 1) * 4, vsub = (l16 >> 1) & 1, vswz = swz_mx<D>(vkey);
 
   // ---- tile i from its stage; `next` refills the stage when it is free
   auto tile = [&](Stage& st, int kb, auto&& next) __attribute__((always_inline)) {
@@ -231,31 +235,34 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     }
   };
 
-  // ---- this wave's tiles j0 + wave + kWaves*i, two in flight
-  auto jt = [&](int i) { return j0 + wave + kWaves * i; };
-  Stage st[2];
+  // ---- this wave's tiles j0 + wave + kWaves*i, two in flight.  Past the last
+  // one the loads bring it again, so that every step issues the same number of
+  // them: with a branch around them the compiler waits for all that are in
+  // flight at every step.
+  auto jt = [&](int i) { return j0 + wave + kWaves * min(i, nt - 1); };
+  Stage st[DEPTH];
   uint32_t ids[2];
   if (nt > 0) {
     page_ids(jt(0), ids);
-    load_tile(jt(0), ids, st[0]);
-    page_ids(jt(1), ids);
-    if (nt > 1) load_tile(jt(1), ids, st[1]);
-    page_ids(jt(2), ids);
+#pragma unroll
+    for (int x = 0; x < DEPTH; ++x) {
+      load_tile(jt(x), ids, st[x]);
+      page_ids(jt(x + 1), ids);
+    }
+    auto step = [&](int i, Stage& s) __attribute__((always_inline)) {
+      tile(s, jt(i) * kTK, [&]() __attribute__((always_inline)) {
+        load_tile(jt(i + DEPTH), ids, s);
+        page_ids(jt(i + DEPTH + 1), ids);
+      });
+    };
+    int i = 0;
+    for (; i + DEPTH <= nt; i += DEPTH)
+#pragma unroll
+      for (int x = 0; x < DEPTH; ++x) step(i + x, st[x]);
+#pragma unroll
+    for (int x = 0; x + 1 < DEPTH; ++x)
+      if (i + x < nt) step(i + x, st[x]);
   }
-  auto step = [&](int i, Stage& s) __attribute__((always_inline)) {
-    tile(s, jt(i) * kTK, [&]() __attribute__((always_inline)) {
-      if (i + 2 < nt) {
-        load_tile(jt(i + 2), ids, s);
-        page_ids(jt(i + 3), ids);
-      }
-    });
-  };
-  int i = 0;
-  for (; i + 2 <= nt; i += 2) {
-    step(i, st[0]);
-    step(i + 1, st[1]);
-  }
-  if (i < nt) step(i, st[0]);
 
   // ---- merge the four waves.  Each parks its O rows in its own slot (its reads
   // of V precede these writes in LDS order), four columns a piece, the pieces of
@@ -274,7 +281,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     }
   }
   __syncthreads();
-  const int64_t set_rows = (int64_t)a.total_rows * a.num_q_heads;
   for (int idx = tid; idx < heads * Q4; idx += kWaves * 64) {
     const int r = idx / Q4, q = idx - r * Q4;
     float mstar = -INFINITY;
@@ -291,44 +297,112 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       lsum += wt * ml[w][r][1];
       acc += wt * reinterpret_cast<const f32x4*>(ring[w].bytes)[r * Q4 + (q ^ (r & 15))];
     }
-    const int64_t row = first_row + r;
-    if (a.direct) {
+    if (nsplit == 1) {
+      const int64_t row = first_row + r;
       const float inv = 1.0f / lsum;
       store4(reinterpret_cast<T*>(a.out) + row * D + q * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
       if (a.lse != nullptr && q == 0) a.lse[row] = (mstar + __builtin_log2f(lsum)) * kLn2;
     } else {
-      const int64_t prow = split * set_rows + row;
+      const int64_t prow = a.part_row[si] + (int64_t)split * a.num_q_heads + g * G + head0 + r;
       *reinterpret_cast<f32x4*>(a.part_o + prow * D + q * 4) = acc;
-      if (q == 0) {
-        a.part_ml[prow * 2] = mstar;
-        a.part_ml[prow * 2 + 1] = lsum;
-        if (split == nsplit - 1) {   // the sets that this sequence has no splits for
-          for (int s = split + 1; s < a.nsplit; ++s) {
-            a.part_ml[(s * set_rows + row) * 2] = -INFINITY;
-            a.part_ml[(s * set_rows + row) * 2 + 1] = -1.f;
-          }
-        }
-      }
+      if (q == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = (f32x2){mstar, lsum};
     }
+  }
+  if (from < to) __syncthreads();   // the slots and ml are free again
   }
 }
 
+// The partial results of a row, in the order of its keys:
+//   m* = max_s m_s,  w_s = 2^(m_s - m*),  out = sum_s w_s O_s / sum_s w_s l_s.
+// D/4 lanes take a row's columns, four each; a workgroup's groups of such lanes
+// share one row's partials (WIDE: a call with few rows and many partials is
+// bound by memory round trips) or have a row each.
+template <typename T, int D, bool WIDE>
+__global__ __launch_bounds__(256) void mx_join_kernel(const MxJoinArgs a) {
+  constexpr int Q4 = D / 4, GROUPS = 256 / Q4, AHEAD = 8;
+  __shared__ f32x4 part[WIDE ? GROUPS : 1][Q4];
+  __shared__ float sums[WIDE ? GROUPS : 1];
+  const int q = threadIdx.x % Q4, group = threadIdx.x / Q4;
+  const int64_t at = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * GROUPS + group;
+  const bool live = at < (int64_t)a.nseq * a.num_q_heads;
+  const int64_t x = live ? at : 0;
+  const int si = (int)(x / a.num_q_heads), h = (int)(x - (int64_t)si * a.num_q_heads);
+  const int n = a.parts[si];
+  const int64_t first = a.part_row[si] + h;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
+  const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + first * D) + q;
+  const int64_t step = a.num_q_heads;
+  float mstar = -INFINITY;
+  for (int s = q; s < n; s += Q4) mstar = fmaxf(mstar, ml[s * step][0]);
+#pragma unroll
+  for (int d = Q4 / 2; d > 0; d >>= 1) mstar = fmaxf(mstar, __shfl_xor(mstar, d));
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float lsum = 0.f;
+  constexpr int BY = WIDE ? GROUPS : 1;
+  for (int s0 = WIDE ? group : 0; s0 < n; s0 += BY * AHEAD) {
+    f32x4 v[AHEAD];
+    f32x2 e[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (s0 + i * BY < n) v[i] = po[(s0 + i * BY) * step * Q4], e[i] = ml[(s0 + i * BY) * step];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (s0 + i * BY < n) {
+        const float w = e[i][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(e[i][0] - mstar);   // -inf: no keys, l and O 0
+        lsum += w * e[i][1];
+        acc += w * v[i];
+      }
+  }
+  if constexpr (WIDE) {
+    part[group][q] = acc;
+    if (q == 0) sums[group] = lsum;
+    __syncthreads();
+    if (group != 0) return;
+    acc = (f32x4){0.f, 0.f, 0.f, 0.f}, lsum = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) acc += part[i][q], lsum += sums[i];
+  }
+  if (!live) return;
+  const int64_t row = (int64_t)a.row[si] + h;
+  const float inv = 1.0f / lsum;
+  store4(reinterpret_cast<T*>(a.out) + row * D + q * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  if (a.lse != nullptr && q == 0) a.lse[row] = (mstar + __builtin_log2f(lsum)) * kLn2;
+}
+
 template <typename T, int D>
-void launch_as(const ExtendArgs& a, int chunks, int grid, hipStream_t stream) {
-  const int per_chunk = (a.group + chunks - 1) / chunks;
-  if (per_chunk <= 16)
-    hipLaunchKernelGGL((mx_decode_kernel<T, D, 1>), dim3(grid), dim3(kWaves * 64), 0, stream, a, chunks);
+void launch_join_as(const MxJoinArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.nseq * a.num_q_heads, groups = 256 / (D / 4);
+  if (rows < 4096)
+    hipLaunchKernelGGL((mx_join_kernel<T, D, true>), dim3((unsigned)rows), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((mx_decode_kernel<T, D, 2>), dim3(grid), dim3(kWaves * 64), 0, stream, a, chunks);
+    hipLaunchKernelGGL((mx_join_kernel<T, D, false>), dim3((unsigned)((rows + groups - 1) / groups)), dim3(256), 0,
+                       stream, a);
+}
+
+template <typename T, int D>
+void launch_as(const MxDecodeArgs& a, int grid, hipStream_t stream) {
+  const int per_chunk = (a.group + a.chunks - 1) / a.chunks;
+  if (per_chunk <= 16)
+    hipLaunchKernelGGL((mx_decode_kernel<T, D, 1>), dim3(grid), dim3(kWaves * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((mx_decode_kernel<T, D, 2>), dim3(grid), dim3(kWaves * 64), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_mx_decode(const ExtendArgs& a, int dtype, int head_dim, int chunks, int grid, hipStream_t stream) {
-  if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, chunks, grid, stream);
-  else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, chunks, grid, stream);
-  else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, chunks, grid, stream);
-  else launch_as<float, 64>(a, chunks, grid, stream);
+hipError_t launch_mx_decode(const MxDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t stream) {
+  if (dtype == 0 && head_dim == 128) launch_as<__bf16, 128>(a, grid, stream);
+  else if (dtype == 0 && head_dim == 64) launch_as<__bf16, 64>(a, grid, stream);
+  else if (dtype == 1 && head_dim == 128) launch_as<float, 128>(a, grid, stream);
+  else launch_as<float, 64>(a, grid, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_join(const MxJoinArgs& a, int dtype, int head_dim, hipStream_t stream) {
+  if (dtype == 0 && head_dim == 128) launch_join_as<__bf16, 128>(a, stream);
+  else if (dtype == 0 && head_dim == 64) launch_join_as<__bf16, 64>(a, stream);
+  else if (dtype == 1 && head_dim == 128) launch_join_as<float, 128>(a, stream);
+  else launch_join_as<float, 64>(a, stream);
   return hipGetLastError();
 }
 

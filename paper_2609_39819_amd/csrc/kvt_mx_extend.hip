@@ -215,7 +215,8 @@ __global__ __launch_bounds__(kThreads) void mx_extend_kernel(const ExtendArgs a)
 
   // ---- main loop.  Step t converts tile t+1, loaded during step t-1, into the
   // other slot, starts loading tile t+2 and computes tile t; the barrier at the
-  // end publishes tile t+1 and frees the slot of tile t.
+  // end publishes tile t+1 and frees the slot of tile t.  Past the last tile the
+  // loads still read pages of the sequence, into a slot no one reads.
   const int n = j1 - j0;
   const bool idle = r0 + wave * 32 >= rows_seq;   // a wave of padding rows only: gathers, no products
   uint32_t id = 0;
@@ -223,16 +224,14 @@ __global__ __launch_bounds__(kThreads) void mx_extend_kernel(const ExtendArgs a)
     load_tile(j0, page_id(j0));
     id = page_id(j0 + 1);
     stash(slot0);
-    if (n > 1) load_tile(j0 + 1, id);
+    load_tile(j0 + 1, id);
     id = page_id(j0 + 2);
   }
   __syncthreads();
   auto step = [&](int t, const MxHalfTile<D> (&cur)[2], MxHalfTile<D> (&fill)[2]) __attribute__((always_inline)) {
-    if (t + 1 < n) {
-      stash(fill);
-      if (t + 2 < n) load_tile(j0 + t + 2, id);
-      id = page_id(j0 + t + 3);
-    }
+    stash(fill);
+    load_tile(j0 + t + 2, id);
+    id = page_id(j0 + t + 3);
     if (!idle) tile(j0 + t, cur);
     __syncthreads();
   };

@@ -11,11 +11,12 @@
 // Two kernels, by the rows that the largest sequence adds:
 //   * step (at most 32 rows, a decoding step): HBM-bound on K.  4 waves stream
 //     32-key tiles from HBM into their operands (no LDS), 16 or 32 rows by
-//     v_mfma_f32_16x16x32_bf16;
-//   * turn: bound by the exponentials (a score costs 16 cycles of a wave's
-//     vector unit for 64 of them and 4 of the matrix unit's).  A workgroup holds 64
-//     keys (fp32: 32) as operands in every wave's registers, the waves take
-//     the row blocks of 32 in turn, their sums meet in LDS at the end.
+//     v_mfma_f32_16x16x32_bf16.  The batch's tiles lie one after the other and every
+//     workgroup takes an equal share, of as many sequences as lie there;
+//   * turn: bound by the exponentials (16 cycles of a wave's vector unit for 64 of
+//     them, 8 more for a score's product and sum).  Every wave holds 32 keys as
+//     operands in registers; the rows pass through LDS, 64 at a time, for all
+//     waves of the workgroup.
 #include <type_traits>
 
 #include "kvt_mx_device.h"
@@ -63,6 +64,23 @@ __device__ __forceinline__ float scatter_sum(float (&v)[N], int lane, int top) {
   return v[0];
 }
 
+// Sum over the 16 lanes of a row, in all of them.
+__device__ __forceinline__ float row_sum(float x) {
+  auto add = [](float v, auto ctrl) __attribute__((always_inline)) {
+    const int u = __builtin_bit_cast(int, v);
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = add(x, std::integral_constant<int, 0xb1>());    // lane ^ 1
+  x = add(x, std::integral_constant<int, 0x4e>());    // lane ^ 2
+  x = add(x, std::integral_constant<int, 0x141>());   // 7 - lane of 8
+  return add(x, std::integral_constant<int, 0x140>());   // 15 - lane of 16
+}
+
+// Four floats at any 4-byte aligned place.
+struct __attribute__((packed, aligned(4))) Four {
+  float x[4];
+};
+
 // Old weights are those of the reused positions; the new ones have none.
 __device__ __forceinline__ void put(float* w, int key, const SeqDesc& sd, float sum) {
   w[key] = key < sd.prefix ? w[key] + sum : sum;
@@ -84,13 +102,16 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
 
   const int hkv = a.num_kv_heads, G = a.group;
   const int g = blockIdx.x % hkv;
-  const int unit = blockIdx.x / hkv;
-  const int si = unit / a.nsplit, split = unit - si * a.nsplit;
+  const char* kpool = reinterpret_cast<const char*>(a.k_pool);
+  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
+  int from = blockIdx.x / hkv * a.share;
+  const int to = min(from + a.share, a.unit_begin[a.nseq]);
+  for (int si = find_seq(a.unit_begin, a.nseq, from); from < to; ++si) {   // the sequences of this slot
   const SeqDesc sd = a.seq[si];
   const int P = sd.prefix, L = P + sd.suffix, rows = sd.suffix * G;
-  const int nblk = (L + kBlock - 1) / kBlock, ntk = (L + kTK - 1) / kTK;
-  const int per_split = (ntk + a.nsplit - 1) / a.nsplit;
-  const int j0 = split * per_split, j1 = min(ntk, j0 + per_split);
+  const int nblk = (L + kBlock - 1) / kBlock;
+  const int j0 = from - a.unit_begin[si], j1 = min(to, a.unit_begin[si + 1]) - a.unit_begin[si];
+  from = a.unit_begin[si] + j1;
   const int nt = j1 - j0 > wave ? (j1 - j0 - wave + 3) / 4 : 0;
 
   // ---- this lane's query rows; rows past the last see nothing
@@ -104,32 +125,37 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
     const T* qp = reinterpret_cast<const T*>(a.q) + row * D;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) load_terms(qp + (kCodes ? qd * (D / 4) + kk * 8 : kk * 32 + qd * 8), qreg[b][kk]);
-    lse2[b] = a.lse[row] * kLog2e;
-    lim[b] = b * 16 + l16 < rows ? P + t : -1;
+    // a row past the last: 2^(s - infinity) = 0 (or NaN for a key that is one
+    // anyway)
+    lse2[b] = b * 16 + l16 < rows ? a.lse[row] * kLog2e : INFINITY;
+    lim[b] = P + t;
   }
   float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
-  const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const __attribute__((address_space(4))) int32_t* bt =
       (const __attribute__((address_space(4))) int32_t*)(a.block_table + (int64_t)sd.seq * a.max_blocks);
-  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
   auto page_ids = [&](int j, uint32_t (&ids)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int page = __builtin_amdgcn_readfirstlane(min(j * 2 + p, nblk - 1));
-      const uint32_t raw = (uint32_t)bt[page];
-      ids[p] = __builtin_amdgcn_readfirstlane(raw > nb_max ? nb_max : raw);
+      ids[p] = (uint32_t)bt[page];
     }
   };
+  // (and the old weights of keys 4 qd .. + 3 of each page, of which there are 4
+  // at least, or else any 16 readable bytes)
+  const float* old = P >= 4 ? w : reinterpret_cast<const float*>(a.q);
   struct Stage {
     u32x4 k[2][kPieces];
     unsigned char scale[2];
+    Four old[2];
   };
   auto load_tile = [&](int j, const uint32_t (&ids)[2], Stage& st) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
+      // (a tile that reaches past the old ones reads them when it stores)
+      st.old[p] = *reinterpret_cast<const Four*>(old + max(0, min(j * kTK + 16 * p + 4 * qd, P - 4)));
       const int page = min(j * 2 + p, nblk - 1);
       const int slot = min(l16, L - 1 - page * kBlock);
-      const char* at = kpool + ((int64_t)ids[p] * hkv + g) * kPage;
+      const char* at = kpool + ((int64_t)min(ids[p], nb_max) * hkv + g) * kPage;
       if constexpr (kCodes) {
         const char* code = at + slot * (D / 2) + qd * (D / 8);
         if constexpr (KS == 4) {
@@ -153,6 +179,7 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
   const float c = a.scale_log2;
   auto tile = [&](Stage& st, int kb, auto&& next) __attribute__((always_inline)) {
     f32x4 s[NB][2];
+    const Four before[2] = {st.old[0], st.old[1]};
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
 #pragma unroll
@@ -170,6 +197,24 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
     }
     next();
     float sum[8];
+    if (kb + kTK <= P) {   // every row sees all of the tile, every key has an old weight
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum[e] = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e >> 2][e & 3], c, -lse2[b]));
+        sum[e] = row_sum(sum[e]);
+      }
+      if (l16 == 0) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          *reinterpret_cast<Four*>(w + kb + 16 * p + 4 * qd) =
+              Four{{before[p].x[0] + sum[4 * p], before[p].x[1] + sum[4 * p + 1], before[p].x[2] + sum[4 * p + 2],
+                    before[p].x[3] + sum[4 * p + 3]}};
+      }
+      return;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int key = kb + 16 * (e >> 2) + 4 * qd + (e & 3);
@@ -179,169 +224,256 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e >> 2][e & 3], c, -lse2[b]));
         sum[e] += key > lim[b] ? 0.f : p;
       }
+      sum[e] = row_sum(sum[e]);
+      if (l16 == 0 && key < L) put(w, key, sd, sum[e]);
     }
-    float total = scatter_sum(sum, lane, 8);     // of element (l16 >> 1), half of it
-    total += __shfl_xor(total, 1);
-    const int e = l16 >> 1, key = kb + 16 * (e >> 2) + 4 * qd + (e & 3);
-    if ((lane & 1) == 0 && key < L) put(w, key, sd, total);
   };
 
-  auto jt = [&](int i) { return j0 + wave + 4 * i; };
+  // past the last tile the loads bring it again: every step issues as many
+  auto jt = [&](int i) { return j0 + wave + 4 * min(i, nt - 1); };
   Stage st[DEPTH];
   uint32_t ids[2];
   if (nt > 0) {
     page_ids(jt(0), ids);
 #pragma unroll
     for (int x = 0; x < DEPTH; ++x) {
-      if (x < nt) load_tile(jt(x), ids, st[x]);
+      load_tile(jt(x), ids, st[x]);
       page_ids(jt(x + 1), ids);
     }
-  }
-  for (int i = 0; i < nt; i += DEPTH)
+    auto step = [&](int i, Stage& s) __attribute__((always_inline)) {
+      tile(s, jt(i) * kTK, [&]() __attribute__((always_inline)) {
+        load_tile(jt(i + DEPTH), ids, s);
+        page_ids(jt(i + DEPTH + 1), ids);
+      });
+    };
+    int i = 0;
+    for (; i + DEPTH <= nt; i += DEPTH)
 #pragma unroll
-    for (int x = 0; x < DEPTH; ++x)
-      if (i + x < nt)
-        tile(st[x], jt(i + x) * kTK, [&]() __attribute__((always_inline)) {
-          if (i + x + DEPTH < nt) {
-            load_tile(jt(i + x + DEPTH), ids, st[x]);
-            page_ids(jt(i + x + DEPTH + 1), ids);
-          }
-        });
+      for (int x = 0; x < DEPTH; ++x) step(i + x, st[x]);
+    if (i < nt) step(i, st[0]);
+  }
+  }
 }
 
-template <int FORMAT>
-constexpr int kTurnBlocks = FORMAT == 1 ? 1 : 2;   // 32-key blocks of a workgroup
+// Rows of queries in LDS at a time, as the operand terms of their type: [term][row][D] bf16,
+// the 16-byte chunks of a row XOR-swizzled as a key tile's in the extend kernel.
+template <typename T>
+constexpr int kTurnRows = sizeof(T) == 2 ? 256 : 64;
+template <typename T, int D>
+struct TurnRows {
+  __bf16 q[kTerms<T>][kTurnRows<T> * D];
+  float lse[kTurnRows<T>];
+  int lim[kTurnRows<T>];
+};
 
 template <typename T, int D, int FORMAT>
 __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) {
   constexpr bool kCodes = FORMAT == kMx;
   constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
-  constexpr int KSTEPS = D / 16;
-  constexpr int KB = kTurnBlocks<FORMAT>, KEYS = KB * 32;
+  constexpr int KSTEPS = D / 16, CHUNKS = D / 8;
+  constexpr int ROWS = kTurnRows<T>, BLOCKS = ROWS / 32;
   constexpr int64_t kPage = kCodes ? mx_page_bytes(D) : (int64_t)kBlock * D * (FORMAT == 0 ? 2 : 4);
-  constexpr int QP = (int)sizeof(T) / 2;         // 16-byte pieces of 8 query columns
-  __shared__ float red[8][KEYS];
+  constexpr int PIECES = ROWS * CHUNKS / 512;    // of 8 columns, per thread and stage
+  extern __shared__ __attribute__((aligned(1024))) char turn_lds[];
+  TurnRows<T, D>* stage = reinterpret_cast<TurnRows<T, D>*>(turn_lds);   // two
   const int tid = threadIdx.x;
-  const int waves = blockDim.x / 64;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, l32 = lane & 31;
 
+  // ---- a wide workgroup has 32 keys per wave and every wave takes all rows, a
+  // narrow one has 32 keys and its waves take the row blocks in turn
   const int hkv = a.num_kv_heads, G = a.group;
   const int g = blockIdx.x % hkv;
   const int unit = blockIdx.x / hkv;
-  const int si = find_seq(a.unit_begin, a.nseq, unit);
+  const bool narrow = unit >= a.unit_begin[a.nseq];
+  const int at = narrow ? unit - a.unit_begin[a.nseq] : unit;
+  const int si = find_seq(narrow ? a.narrow_begin : a.unit_begin, a.nseq, at);
   const SeqDesc sd = a.seq[si];
   const int P = sd.prefix, L = P + sd.suffix, rows = sd.suffix * G;
-  const int kb = (unit - a.unit_begin[si]) * KEYS;
+  const int wide_keys = (a.unit_begin[si + 1] - a.unit_begin[si]) * kWeightsWideKeys;
+  const int kb0 = narrow ? wide_keys + (at - a.narrow_begin[si]) * 32 : (at - a.unit_begin[si]) * kWeightsWideKeys;
+  const int kb = narrow ? kb0 : kb0 + wave * 32;
   const int nblk = (L + kBlock - 1) / kBlock;
-  // row blocks that see one of the keys
-  const int blocks = (rows + 31) / 32;
-  const int first = kb > P ? (int)((int64_t)(kb - P) * G / 32) : 0;
 
-  float acc[KB][16];
-#pragma unroll
-  for (int x = 0; x < KB; ++x)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
-
-  if (first + wave < blocks) {
-    // ---- the keys, as operands
-    const char* kpool = reinterpret_cast<const char*>(a.k_pool);
-    const int32_t* bt = a.block_table + (int64_t)sd.seq * a.max_blocks;
+  // ---- this wave's keys, as operands (past the end the last one: not stored)
+  bf16x8 kf[KSTEPS][KN];
+  {
     const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
-    bf16x8 kf[KB][KSTEPS][KN];
+    const int pos = min(kb + l32, L - 1);
+    const uint32_t id =
+        min((uint32_t)a.block_table[(int64_t)sd.seq * a.max_blocks + min(pos / kBlock, nblk - 1)], nb_max);
+    const int slot = pos % kBlock;
+    const char* page = reinterpret_cast<const char*>(a.k_pool) + ((int64_t)id * hkv + g) * kPage;
+    if constexpr (kCodes) {
 #pragma unroll
-    for (int x = 0; x < KB; ++x) {
-      const int pos = min(kb + x * 32 + l32, L - 1);
-      const uint32_t id = min((uint32_t)bt[min(pos / kBlock, nblk - 1)], nb_max);
-      const int slot = pos % kBlock;
-      const char* at = kpool + ((int64_t)id * hkv + g) * kPage;
-      if constexpr (kCodes) {
+      for (int y = 0; y < D / 64; ++y) {         // 32 columns: four words under one scale
+        const u32x4 c4 = *reinterpret_cast<const u32x4*>(page + slot * (D / 2) + hh * (D / 4) + y * 16);
+        const float scale = mx_scale((unsigned char)page[mx_code_bytes(D) + slot * (D / 32) + hh * (D / 64) + y]);
 #pragma unroll
-        for (int y = 0; y < D / 64; ++y) {       // 32 columns: four words under one scale
-          const u32x4 c4 = *reinterpret_cast<const u32x4*>(at + slot * (D / 2) + hh * (D / 4) + y * 16);
-          const float scale = mx_scale((unsigned char)at[mx_code_bytes(D) + slot * (D / 32) + hh * (D / 64) + y]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) kf[x][y * 4 + i][0] = mx_values(c4[i], scale);
-        }
-      } else {
-        typedef typename std::conditional<FORMAT == 0, __bf16, float>::type K;
-#pragma unroll
-        for (int kk = 0; kk < KSTEPS; ++kk)
-          load_terms(reinterpret_cast<const K*>(at) + slot * D + kk * 16 + hh * 8, kf[x][kk]);
+        for (int i = 0; i < 4; ++i) kf[y * 4 + i][0] = mx_values(c4[i], scale);
       }
-    }
-    // ---- row blocks of 32, the next one's queries in flight
-    struct Rows {
-      u32x4 q[KSTEPS][QP];
-      float lse;
-      int lim;
-    };
-    auto load_rows = [&](int rb, Rows& o) __attribute__((always_inline)) {
-      const int r = min(rb * 32 + l32, rows - 1), t = r / G;
-      const int64_t row = (int64_t)(sd.row_off + t) * a.num_q_heads + g * G + (r - t * G);
-      const char* qp = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.q) + row * D);
+    } else {
+      typedef typename std::conditional<FORMAT == 0, __bf16, float>::type K;
 #pragma unroll
       for (int kk = 0; kk < KSTEPS; ++kk)
-#pragma unroll
-        for (int x = 0; x < QP; ++x)
-          o.q[kk][x] = *reinterpret_cast<const u32x4*>(
-              qp + (kCodes ? hh * (D / 2) + kk * 8 : kk * 16 + hh * 8) * (int)sizeof(T) + 16 * x);
-      o.lse = a.lse[row];
-      o.lim = rb * 32 + l32 < rows ? P + t : -1;   // rows past the last see nothing
-    };
-    const float c = a.scale_log2;
-    Rows cur;
-    load_rows(first + wave, cur);
-    for (int rb = first + wave; rb < blocks; rb += waves) {
-      f32x16 s[KB];
-#pragma unroll
-      for (int x = 0; x < KB; ++x) s[x] = (f32x16){};
-#pragma unroll
-      for (int kk = 0; kk < KSTEPS; ++kk) {
-        bf16x8 qf[QN];
-        if constexpr (QN == 1) qf[0] = __builtin_bit_cast(bf16x8, cur.q[kk][0]);
-        else split3(__builtin_bit_cast(f32x4, cur.q[kk][0]), __builtin_bit_cast(f32x4, cur.q[kk][QP - 1]), qf);
-#pragma unroll
-        for (int x = 0; x < KB; ++x) products32(s[x], kf[x][kk], qf);
-      }
-      const float lse2 = cur.lse * kLog2e;
-      const int lim = cur.lim;
-      if (rb + waves < blocks) load_rows(rb + waves, cur);
-      // the block's first row sees the fewest keys; the last block may end early
-      const bool whole = P + rb * 32 / G >= kb + KEYS - 1 && rb * 32 + 32 <= rows;
-      if (whole) {
-#pragma unroll
-        for (int x = 0; x < KB; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[x][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], c, -lse2));
-      } else {
-        const int thr = lim - kb - 4 * hh;       // keys past lim: offset > thr
-#pragma unroll
-        for (int x = 0; x < KB; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], c, -lse2));
-            acc[x][e] += x * 32 + 8 * (e >> 2) + (e & 3) > thr ? 0.f : p;
-          }
-      }
+        load_terms(reinterpret_cast<const K*>(page) + slot * D + kk * 16 + hh * 8, kf[kk]);
     }
   }
-  // ---- sums over the rows: the lanes of a half, then the waves in order
+
+  // ---- rows in stages, from the first that sees one of the workgroup's keys.
+  // Row r of a stage whose first row is head h0 of token t0 is head x - d * G of
+  // token t0 + d, d = x / G, x = h0 + r (a product with 2^32 / G, rounded up: exact
+  // for these small numbers).
+  const int first = kb0 > P ? (int)((int64_t)(kb0 - P) * G / ROWS) : 0;
+  const int stages = (rows + ROWS - 1) / ROWS;
+  const int adv_t = ROWS / G, adv_h = ROWS - adv_t * G;
+  int t0 = (int)((int64_t)first * ROWS / G), h0 = first * ROWS - t0 * G;    // of the stage that is loaded next
+  const unsigned magic = G == 1 ? 0u : 0xffffffffu / (unsigned)G + 1u;
+  auto place = [&](int r, int& tok, int64_t& row) __attribute__((always_inline)) {
+    const int x = h0 + r;
+    const int d = G == 1 ? x : (int)__umulhi((unsigned)x, magic);
+    tok = t0 + d;
+    const bool past = tok >= sd.suffix;          // past the last row: any row, it sees nothing
+    row = (int64_t)(sd.row_off + (past ? 0 : tok)) * a.num_q_heads + g * G + (x - d * G);
+  };
+  constexpr int QP = (int)sizeof(T) / 2;
+  u32x4 raw[QN == 1 ? 1 : PIECES][QP];
+  float lse_raw = 0.f;
+  int lim_raw = -1;
+  // bf16 rows go straight into LDS: load i of a wave brings 64 pieces, and lane l
+  // lands at piece l of them, so it fetches the chunk that the swizzle puts there;
+  // fp32 rows pass through registers (drop), where they become their terms
+  auto load_stage = [&](TurnRows<T, D>& to) __attribute__((always_inline)) {
 #pragma unroll
-  for (int x = 0; x < KB; ++x) {
-    float sum = scatter_sum(acc[x], lane, 16);   // of element l32 >> 1, half of it
-    sum += __shfl_xor(sum, 1);
-    const int e = l32 >> 1;
-    if ((lane & 1) == 0) red[wave][x * 32 + 8 * (e >> 2) + 4 * hh + (e & 3)] = sum;
+    for (int x = 0; x < PIECES; ++x) {
+      const int p = (QN == 1 ? (wave * PIECES + x) * 64 + lane : tid + x * 512);
+      const int r = p / CHUNKS, chunk = QN == 1 ? (p % CHUNKS) ^ swz<D>(r) : p % CHUNKS;
+      int tok;
+      int64_t row;
+      place(r, tok, row);
+      const char* q = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.q) + row * D + chunk * 8);
+      if constexpr (QN == 1) {
+        __builtin_amdgcn_global_load_lds(
+            (const void*)q, (__attribute__((address_space(3))) void*)((lds_bf16*)to.q[0] + (wave * PIECES + x) * 512), 16,
+            0, 0);
+      } else {
+#pragma unroll
+        for (int y = 0; y < QP; ++y) raw[x][y] = *reinterpret_cast<const u32x4*>(q + 16 * y);
+      }
+    }
+    if (tid < ROWS) {
+      int tok;
+      int64_t row;
+      place(tid, tok, row);
+      lse_raw = a.lse[row];
+      lim_raw = tok >= sd.suffix ? -1 : P + tok;
+    }
+    t0 += adv_t;
+    h0 += adv_h;
+    if (h0 >= G) h0 -= G, ++t0;
+  };
+  auto drop = [&](TurnRows<T, D>& to) __attribute__((always_inline)) {
+    if constexpr (QN == 3) {
+#pragma unroll
+      for (int x = 0; x < PIECES; ++x) {
+        const int p = tid + x * 512, r = p / CHUNKS, piece = r * D + (((p % CHUNKS) ^ swz<D>(r)) << 3);
+        bf16x8 t3[3];
+        split3(__builtin_bit_cast(f32x4, raw[x][0]), __builtin_bit_cast(f32x4, raw[x][1]), t3);
+#pragma unroll
+        for (int y = 0; y < QN; ++y) *reinterpret_cast<u32x4*>(to.q[y] + piece) = __builtin_bit_cast(u32x4, t3[y]);
+      }
+    }
+    if (tid < ROWS) to.lse[tid] = lse_raw, to.lim[tid] = lim_raw;
+  };
+
+  float acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  const float c = a.scale_log2;
+  auto scores = [&](const TurnRows<T, D>& from, int block) __attribute__((always_inline)) {
+    const int row = block * 32 + l32;
+    f32x16 s = (f32x16){};
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; ++kk) {
+      const int chunk = kCodes ? hh * (D / 16) + kk : 2 * kk + hh;
+      bf16x8 qf[QN];
+#pragma unroll
+      for (int y = 0; y < QN; ++y)
+        qf[y] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(from.q[y] + row * D + ((chunk ^ swz<D>(l32)) << 3)));
+      products32(s, kf[kk], qf);
+    }
+    return s;
+  };
+  auto add = [&](const TurnRows<T, D>& from, int block, const f32x16& s, auto masked) __attribute__((always_inline)) {
+    const float lse2 = from.lse[block * 32 + l32] * kLog2e;
+    const int thr = decltype(masked)::value ? from.lim[block * 32 + l32] - kb - 4 * hh : 0;   // keys past lim: offset > thr
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse2));
+      if constexpr (decltype(masked)::value) acc[e] += 8 * (e >> 2) + (e & 3) > thr ? 0.f : p;
+      else acc[e] += p;
+    }
+  };
+  if (first < stages) {
+    int seen = t0, seen_h = h0;                  // first row of the stage that is computed: it sees the fewest keys
+    load_stage(stage[0]);
+    drop(stage[0]);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    for (int i = first; i < stages; ++i) {
+      const TurnRows<T, D>& cur = stage[(i - first) & 1];
+      TurnRows<T, D>& fill = stage[(i + 1 - first) & 1];
+      if (i + 1 < stages) load_stage(fill);
+      const bool whole = P + seen >= kb + 31 && (i + 1) * ROWS <= rows;
+      if (narrow) {
+        if (wave < BLOCKS) add(cur, wave, scores(cur, wave), std::true_type());
+      } else if (whole) {
+        f32x16 s = scores(cur, 0);
+#pragma unroll
+        for (int block = 0; block < BLOCKS; ++block) {
+          f32x16 s1 = s;
+          if (block + 1 < BLOCKS) s1 = scores(cur, block + 1);
+          add(cur, block, s, std::false_type());
+          s = s1;
+          if constexpr (QN == 1 && KN == 1) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < KSTEPS; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x002, 48 / KSTEPS, 0);
+              __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+          }
+        }
+      } else {
+        for (int block = 0; block < BLOCKS; ++block) add(cur, block, scores(cur, block), std::true_type());
+      }
+      seen += adv_t;
+      seen_h += adv_h;
+      if (seen_h >= G) seen_h -= G, ++seen;
+      if (i + 1 < stages) drop(fill);
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      __syncthreads();
+    }
   }
+  // ---- sums over the rows: the lanes of a half, and of a narrow workgroup the
+  // waves, in order
+  float sum = scatter_sum(acc, lane, 16);        // of element l32 >> 1, half of it
+  sum += __shfl_xor(sum, 1);
+  const int e = l32 >> 1, k32 = 8 * (e >> 2) + 4 * hh + (e & 3);
+  float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
+  if (!narrow) {
+    if ((lane & 1) == 0 && kb + k32 < L) put(w, kb + k32, sd, sum);
+    return;
+  }
+  float* red = reinterpret_cast<float*>(turn_lds);   // the stages are done with
+  if ((lane & 1) == 0) red[wave * 32 + k32] = sum;
   __syncthreads();
-  for (int k = tid; k < KEYS; k += blockDim.x) {
-    if (kb + k >= L) break;
-    float sum = 0.f;
-    for (int x = 0; x < waves; ++x) sum += red[x][k];
-    put(a.weights + ((int64_t)sd.seq * hkv + g) * a.stride, kb + k, sd, sum);
+  if (tid < 32 && kb + tid < L) {
+    sum = 0.f;
+    for (int x = 0; x < 8; ++x) sum += red[x * 32 + tid];
+    put(w, kb + tid, sd, sum);
   }
 }
 
@@ -353,13 +485,11 @@ void launch_step_as(const WeightsArgs& a, int grid, hipStream_t stream) {
   else hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 2>), dim3(grid), dim3(256), 0, stream, a);
 }
 template <typename T, int D, int FORMAT>
-void launch_turn_as(const WeightsArgs& a, int waves, int grid, hipStream_t stream) {
-  hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT>), dim3(grid), dim3(64 * waves), 0, stream, a);
+void launch_turn_as(const WeightsArgs& a, int grid, hipStream_t stream) {
+  hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT>), dim3(grid), dim3(512), 2 * sizeof(TurnRows<T, D>), stream, a);
 }
 
 }  // namespace
-
-int weights_keys_per_unit(int format) { return 32 * (format == 1 ? kTurnBlocks<1> : kTurnBlocks<0>); }
 
 hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream) {
   const bool wide = head_dim == 128;
@@ -370,13 +500,12 @@ hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int 
   return hipGetLastError();
 }
 
-hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int waves, int grid,
-                               hipStream_t stream) {
+hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream) {
   const bool wide = head_dim == 128;
-  if (format == 0) wide ? launch_turn_as<__bf16, 128, 0>(a, waves, grid, stream) : launch_turn_as<__bf16, 64, 0>(a, waves, grid, stream);
-  else if (format == 1) wide ? launch_turn_as<float, 128, 1>(a, waves, grid, stream) : launch_turn_as<float, 64, 1>(a, waves, grid, stream);
-  else if (dtype == 0) wide ? launch_turn_as<__bf16, 128, kMx>(a, waves, grid, stream) : launch_turn_as<__bf16, 64, kMx>(a, waves, grid, stream);
-  else wide ? launch_turn_as<float, 128, kMx>(a, waves, grid, stream) : launch_turn_as<float, 64, kMx>(a, waves, grid, stream);
+  if (format == 0) wide ? launch_turn_as<__bf16, 128, 0>(a, grid, stream) : launch_turn_as<__bf16, 64, 0>(a, grid, stream);
+  else if (format == 1) wide ? launch_turn_as<float, 128, 1>(a, grid, stream) : launch_turn_as<float, 64, 1>(a, grid, stream);
+  else if (dtype == 0) wide ? launch_turn_as<__bf16, 128, kMx>(a, grid, stream) : launch_turn_as<__bf16, 64, kMx>(a, grid, stream);
+  else wide ? launch_turn_as<float, 128, kMx>(a, grid, stream) : launch_turn_as<float, 64, kMx>(a, grid, stream);
   return hipGetLastError();
 }
 

@@ -999,7 +999,7 @@ def evict(k_pool, v_pool, block_table, length: Sequence[int], keep: Sequence[int
     ``to_table``, in ascending order; none of those pages may be among the
     sequences' own.  Returns (positions, weights_out): int32 and float32
     [B][Hkv][>= largest n_b], -1 and 0 past n_b; allocated here with that width
-    unless given (both of one width; ``weights_out`` may be ``weights``).
+    unless given (both of one width).
     """
     import torch
     if stream is not None:   # what is allocated here belongs to the stream that it is written on

@@ -58,16 +58,17 @@ class Cache:
         return [pool[page, :, slot * d // 2:(slot + 1) * d // 2],
                 pool[page, :, cut + slot * (d // 32):cut + (slot + 1) * (d // 32)]]
 
-    def check(self, sinks=0, recent=0, in_place=False, checked=True):
+    def check(self, sinks=0, recent=0, wide=False, checked=True):
         on = [p.cuda() for p in self.pools]
         w = self.weights.cuda()
         kw = {}
-        if in_place:
-            kw = dict(weights_out=w)
+        if wide:
+            kw = dict(positions=torch.full(w.shape, 7, dtype=torch.int32, device="cuda"),
+                      weights_out=torch.full(w.shape, 7.0, device="cuda"))
         positions, weights = kvt.evict(*on, self.table.cuda(), self.lengths, self.keep, w, self.to.cuda(), sinks=sinks,
                                        recent=recent, checked=checked, **kw)
         width = max(min(n, k) for n, k in zip(self.lengths, self.keep))
-        assert positions.shape[2] == weights.shape[2] == (w.shape[2] if in_place else width)
+        assert positions.shape[2] == weights.shape[2] == (w.shape[2] if wide else width)
         want = [p.clone() for p in self.pools]
         for b, n in enumerate(self.lengths):
             for h in range(self.hkv):
@@ -105,8 +106,16 @@ def test_evict(kind, hkv, d, lengths, keep, sinks, recent):
     Cache(lengths, keep, hkv, d, kind).check(sinks, recent)
 
 
-def test_a_long_context():
-    Cache([70001, 9000], [8192, 8192], 2, 64, "mx").check(4, 256)
+@pytest.mark.parametrize("n", [65535, 65536, 65537, 150001])
+def test_a_long_context(n):
+    Cache([n, 9000], [8192, 8192], 2, 64, "mx").check(4, 256)
+
+
+def test_a_long_context_of_equal_weights():
+    c = Cache([70001], [8192], 2, 64, "bf16")
+    c.weights[0, 0] = 0.0
+    c.weights[0, 1] = (torch.arange(c.weights.shape[2]) % 7 == 0).float()
+    c.check(0, 0)
 
 
 @pytest.mark.parametrize("n", [40, 5000])
@@ -126,9 +135,9 @@ def test_weights_that_equal_each_other_and_odd_ones(n):
             c.check(3, 4)
 
 
-def test_weights_in_their_own_place():
+def test_outputs_wider_than_what_is_kept():
     c = Cache([5000, 300, 20], [1000, 100, 50], 2, 64, "bf16")
-    c.check(2, 9, in_place=True)
+    c.check(2, 9, wide=True)
 
 
 def test_shared_pages_stay_and_both_forks_get_their_own():
