@@ -2,9 +2,11 @@
 //
 // The formula is kvt_decode.hip's; the cost is streaming each sequence's 4-bit
 // K/V once from HBM (2 * 17/32 D bytes a key and kv-head).  Work decomposition:
-//   * one workgroup per (sequence, kv-head, key split, up to 32 of the kv-head's
-//     query heads), 4 waves; wave w takes the split's 32-key tiles w, w+4, ...
-//     and keeps two of them in flight in registers; no barrier in the loop;
+//   * the batch's 32-key tiles lie one after the other, and one workgroup per (equal
+//     share of them, kv-head, up to 32 of the kv-head's query heads) goes through
+//     the parts of sequences in its share; of each, wave w of 4 takes the tiles w,
+//     w+4, .. and keeps two of them in flight in registers, across the sequences'
+//     borders; no barrier in the loop;
 //   * v_mfma_f32_16x16x32_bf16 with 16 rows (NB = 1) or 32 (NB = 2): S^T = K Q^T.
 //     A lane's K operand is 8 columns of one key, in any order of the columns
 //     that Q's shares, so each lane takes D/4 neighbouring columns of its key:
@@ -27,10 +29,15 @@ using namespace dev;
 constexpr int kWaves = kDecWaves;
 constexpr int kTK = kDecKeysPerTile;   // keys per tile = 2 pages
 
+// A wave's V tile, [key][D] bf16, and its O rows for the merge, [row][D] fp32:
+// with 16 rows in a place of their own, so that a wave starts on the next sequence
+// while others still merge.
 template <int D, int NB>
 struct alignas(1024) MxDecSlot {
-  // V of one tile; at the end O, [row][D] fp32
-  char bytes[kTK * D * 2 > NB * 16 * D * 4 ? kTK * D * 2 : NB * 16 * D * 4];
+  static constexpr bool kApart = NB == 1;
+  char v[kTK * D * 2 > (kApart ? 0 : NB * 16 * D * 4) ? kTK * D * 2 : NB * 16 * D * 4];
+  char own[kApart ? NB * 16 * D * 4 : 16];
+  __device__ f32x4* rows() { return reinterpret_cast<f32x4*>(kApart ? own : v); }
 };
 
 // XOR swizzle of the 16-byte chunks of a V row in LDS.  A write takes 16 keys at
@@ -49,7 +56,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   constexpr int CT = D / 16;                     // 16-column tiles of the output
   constexpr int64_t kPage = mx_page_bytes(D);
   constexpr float kRescaleSlack = 8.0f;
-  constexpr int DEPTH = 2;                       // tiles in flight
   __shared__ MxDecSlot<D, NB> ring[kWaves];
   __shared__ float ml[kWaves][NB * 16][2];       // per wave and row: m (log2 units), l
 
@@ -73,7 +79,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const char* vpool = reinterpret_cast<const char*>(a.v_pool);
   const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
-  __bf16* vs = reinterpret_cast<__bf16*>(ring[wave].bytes);
+  __bf16* vs = reinterpret_cast<__bf16*>(ring[wave].v);
   const lds_bf16* vl = (const lds_bf16*)vs;
   const int vkey = 4 * qd + (l16 >> 2);          // key of this lane's transposed reads
   const int vrow = vkey * D + (l16 & 1) * 4, vsub = (l16 >> 1) & 1, vswz = swz_mx<D>(vkey);
@@ -82,35 +88,38 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   int si = share == 0 ? unit : find_seq(a.tile_begin, a.nseq, unit * share);
   int from = share == 0 ? a.tile_begin[si] : unit * share;
   const int to = share == 0 ? a.tile_begin[si + 1] : min(from + share, a.tile_begin[a.nseq]);
-  for (; from < to; ++si) {   // the sequences of this slot
-  const SeqDesc sd = a.seq[si];
-  const int begin = a.tile_begin[si], end = a.tile_begin[si + 1];
-  const int split = share == 0 ? 0 : unit - begin / share;
-  const int nsplit = share == 0 ? 1 : (end - 1) / share - begin / share + 1;
-  const int j0 = from - begin, j1 = min(to, end) - begin;
-  from = begin + j1;
-  const int L = sd.prefix + 1;                   // keys 0..P_b
-  const int nblk = (L + kBlock - 1) / kBlock;
-  const int nt = j1 - j0 > wave ? (j1 - j0 - wave + kWaves - 1) / kWaves : 0;   // this wave's tiles
 
-  // ---- this lane's query rows (rows past the last head repeat it and are
-  // dropped): columns qd * D/4 ..
-  const int64_t first_row = (int64_t)sd.row_off * a.num_q_heads + g * G + head0;
-  bf16x8 qreg[NB][KS][NT];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const T* qp = reinterpret_cast<const T*>(a.q) + (first_row + min(b * 16 + l16, heads - 1)) * D + qd * (D / 4);
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk) load_terms(qp + kk * 8, qreg[b][kk]);
-  }
-
-  const __attribute__((address_space(4))) int32_t* bt =
-      (const __attribute__((address_space(4))) int32_t*)(a.block_table + (int64_t)sd.seq * a.max_blocks);
-  auto page_ids = [&](int j, uint32_t (&ids)[2]) __attribute__((always_inline)) {
+  // ---- where the loads are: tile `j` of the sequence, this wave's next one in
+  // the slot.  They run ahead of the products across the sequences' borders, so
+  // that a short sequence does not wait for its first tiles.
+  typedef const __attribute__((address_space(4))) int32_t* Ids;
+  struct Place {
+    int si, j, j1, L, nblk;
+    Ids bt;
+  } at;
+  auto enter = [&](int x, int first_tile) __attribute__((always_inline)) {
+    const SeqDesc sd = a.seq[x];
+    at.si = x;
+    at.L = sd.prefix + 1;                        // keys 0..P_b
+    at.nblk = (at.L + kBlock - 1) / kBlock;
+    at.j = first_tile - a.tile_begin[x] + wave;
+    at.j1 = min(to, a.tile_begin[x + 1]) - a.tile_begin[x];
+    at.bt = (Ids)(a.block_table + (int64_t)sd.seq * a.max_blocks);
+  };
+  // the next tile with work for this wave; past the last one its place stays (on
+  // a tile of the slot's last sequence)
+  auto settle = [&]() __attribute__((always_inline)) {
+    while (at.j >= at.j1 && a.tile_begin[at.si + 1] < to) enter(at.si + 1, a.tile_begin[at.si + 1]);
+    at.j = min(at.j, at.j1 - 1);
+  };
+  enter(si, from);
+  settle();
+  uint32_t ids[2];                               // its pages
+  auto page_ids = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const int page = __builtin_amdgcn_readfirstlane(min(j * 2 + p, nblk - 1));
-      ids[p] = (uint32_t)bt[page];
+      const int page = __builtin_amdgcn_readfirstlane(min(at.j * 2 + p, at.nblk - 1));
+      ids[p] = (uint32_t)at.bt[page];
     }
   };
   // one tile in flight: per page, the lane's codes and scales of key l16
@@ -118,17 +127,18 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     unsigned k[2][KS], v[2][KS];
     unsigned char sk[2], sv[2];
   };
-  // positions past the end read the last real position (weight 0)
-  auto load_tile = [&](int j, const uint32_t (&ids)[2], Stage& st) __attribute__((always_inline)) {
+  // the tile at `at`, which moves on; positions past the sequence's end read the
+  // last real position (weight 0)
+  auto load_tile = [&](Stage& st) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const int page = min(j * 2 + p, nblk - 1);
-      const int slot = min(l16, L - 1 - page * kBlock);
-      const int64_t at = ((int64_t)min(ids[p], nb_max) * hkv + g) * kPage;
+      const int page = min(at.j * 2 + p, at.nblk - 1);
+      const int slot = min(l16, at.L - 1 - page * kBlock);
+      const int64_t record = ((int64_t)min(ids[p], nb_max) * hkv + g) * kPage;
       const int code = slot * (D / 2) + qd * (D / 8);
       const int scale = mx_code_bytes(D) + slot * (D / 32) + (D == 128 ? qd : qd >> 1);
-      const char* ks = kpool + at;
-      const char* vs = vpool + at;
+      const char* ks = kpool + record;
+      const char* vs = vpool + record;
       if constexpr (KS == 4) {
         const u32x4 k4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(ks + code));
         const u32x4 v4 = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vs + code));
@@ -143,19 +153,32 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       st.sk[p] = (unsigned char)ks[scale];
       st.sv[p] = (unsigned char)vs[scale];
     }
+    at.j += kWaves;
+    settle();
+    page_ids();
+  };
+
+  // ---- this lane's query rows (rows past the last head repeat it and are
+  // dropped): columns qd * D/4 ..
+  bf16x8 qreg[NB][KS][NT];
+  auto load_rows = [&](int64_t first_row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const T* qp = reinterpret_cast<const T*>(a.q) + (first_row + min(b * 16 + l16, heads - 1)) * D + qd * (D / 4);
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) load_terms(qp + kk * 8, qreg[b][kk]);
+    }
+  };
+  auto first_row_of = [&](int x) __attribute__((always_inline)) {
+    return (int64_t)a.seq[x].row_off * a.num_q_heads + g * G + head0;
   };
 
   f32x4 o[NB][CT];
   float m_ref[NB], l_run[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    m_ref[b] = -INFINITY, l_run[b] = 0.f;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) o[b][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  }
 
-  // ---- tile i from its stage; `next` refills the stage when it is free
-  auto tile = [&](Stage& st, int kb, auto&& next) __attribute__((always_inline)) {
+  // ---- the tile of a sequence of L keys that starts at key kb, from its stage,
+  // which is refilled as soon as it is free
+  auto tile = [&](Stage& st, int kb, int L) __attribute__((always_inline)) {
     // V into LDS.  A token that is not a number counts through K (its score is
     // one for the rows that see it); its V becomes 0, so that no other row
     // takes it in with a weight of 0.
@@ -185,7 +208,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
             s[b][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[b][kk][t], s[b][p], 0, 0, 0);
       }
     }
-    next();
+    load_tile(st);
     if (kb + kTK > L) {   // the sequence ends inside this tile
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -235,40 +258,54 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     }
   };
 
-  // ---- this wave's tiles j0 + wave + kWaves*i, two in flight.  Past the last
-  // one the loads bring it again, so that every step issues the same number of
-  // them: with a branch around them the compiler waits for all that are in
-  // flight at every step.
-  auto jt = [&](int i) { return j0 + wave + kWaves * min(i, nt - 1); };
-  Stage st[DEPTH];
-  uint32_t ids[2];
-  if (nt > 0) {
-    page_ids(jt(0), ids);
+  // ---- the sequences of this slot.  Two tiles are in flight, and every step
+  // issues the loads of one (past the wave's last tile they bring a tile again:
+  // with a branch around them the compiler waits for all loads at every step).
+  // `odd`: the next tile is in st[1].
+  Stage st[2];
+  page_ids();
+  load_tile(st[0]);
+  load_tile(st[1]);
+  load_rows(first_row_of(si));
+  bool odd = false, merged = false;
+  for (; from < to; ++si) {
+  const SeqDesc sd = a.seq[si];
+  const int begin = a.tile_begin[si], end = a.tile_begin[si + 1];
+  const int split = share == 0 ? 0 : unit - begin / share;
+  const int nsplit = share == 0 ? 1 : (end - 1) / share - begin / share + 1;
+  const int j0 = from - begin, j1 = min(to, end) - begin;
+  from = begin + j1;
+  const int L = sd.prefix + 1;
+  const int64_t first_row = first_row_of(si);
 #pragma unroll
-    for (int x = 0; x < DEPTH; ++x) {
-      load_tile(jt(x), ids, st[x]);
-      page_ids(jt(x + 1), ids);
-    }
-    auto step = [&](int i, Stage& s) __attribute__((always_inline)) {
-      tile(s, jt(i) * kTK, [&]() __attribute__((always_inline)) {
-        load_tile(jt(i + DEPTH), ids, s);
-        page_ids(jt(i + DEPTH + 1), ids);
-      });
-    };
-    int i = 0;
-    for (; i + DEPTH <= nt; i += DEPTH)
+  for (int b = 0; b < NB; ++b) {
+    m_ref[b] = -INFINITY, l_run[b] = 0.f;
 #pragma unroll
-      for (int x = 0; x < DEPTH; ++x) step(i + x, st[x]);
-#pragma unroll
-    for (int x = 0; x + 1 < DEPTH; ++x)
-      if (i + x < nt) step(i + x, st[x]);
+    for (int ct = 0; ct < CT; ++ct) o[b][ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
+  int j = j0 + wave;
+  if (odd && j < j1) {
+    tile(st[1], j * kTK, L);
+    j += kWaves;
+    odd = false;
+  }
+  for (; j + kWaves < j1; j += 2 * kWaves) {
+    tile(st[0], j * kTK, L);
+    tile(st[1], (j + kWaves) * kTK, L);
+  }
+  if (j < j1) {
+    tile(st[0], j * kTK, L);
+    odd = true;
+  }
+  if (from < to) load_rows(first_row_of(si + 1));   // in flight during the merge
 
   // ---- merge the four waves.  Each parks its O rows in its own slot (its reads
   // of V precede these writes in LDS order), four columns a piece, the pieces of
   // a row XOR-swizzled by the row.
   constexpr int Q4 = D / 4;
-  f32x4* ow = reinterpret_cast<f32x4*>(ring[wave].bytes);
+  f32x4* ow = ring[wave].rows();
+  if (MxDecSlot<D, NB>::kApart && merged) __syncthreads();   // the rows of the sequence before are read
+  merged = true;
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const float l_tot = quad_sum(l_run[b]);
@@ -295,7 +332,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       // are all NaN has m = -inf too, and its l is NaN
       const float wt = (mw == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mw - mstar);
       lsum += wt * ml[w][r][1];
-      acc += wt * reinterpret_cast<const f32x4*>(ring[w].bytes)[r * Q4 + (q ^ (r & 15))];
+      acc += wt * ring[w].rows()[r * Q4 + (q ^ (r & 15))];
     }
     if (nsplit == 1) {
       const int64_t row = first_row + r;
@@ -308,7 +345,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       if (q == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = (f32x2){mstar, lsum};
     }
   }
-  if (from < to) __syncthreads();   // the slots and ml are free again
+  if (!MxDecSlot<D, NB>::kApart && from < to) __syncthreads();   // the slots are free again
   }
 }
 
