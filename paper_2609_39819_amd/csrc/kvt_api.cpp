@@ -1352,17 +1352,22 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     a.nseq = n;
     int64_t units = 0, narrow = 0;
     const int keys = step ? kvt::kWeightsStepKeys : kvt::kWeightsWideKeys;
+    bool once = !step;   // turn: the rows of every sequence are one stage in LDS
     for (int i = 0; i < n; ++i) {
       const int b = order[c0 + i];
       const int64_t len = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
       a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
-      units += step ? (len + keys - 1) / keys : len / keys;
+      units += (len + keys - 1) / keys;
+      once = once && (int64_t)seqs->suffix_len[b] * G <= kvt::weights_stage_rows(pool->dtype);
     }
+    a.tiles = once ? (int32_t)((units * pool->num_kv_heads + device_cus() - 1) / device_cus()) : 0;
     // turn: wide workgroups in whole rounds of the CUs, and what a last, mostly
     // empty round would hold as narrow ones (a narrow one of 32 keys takes a third
     // of a wide one's time instead of an eighth: it loads as many rows)
     int64_t drop = 0;   // wide workgroups of each kv-head that become narrow ones
-    if (!step) {
+    if (!step && !once) {
+      units = 0;
+      for (int i = 0; i < n; ++i) units += ((int64_t)a.seq[i].prefix + a.seq[i].suffix) / keys;
       const int64_t excess = units * pool->num_kv_heads % device_cus();
       const int64_t thin = (excess * 8 + device_cus() - 1) / device_cus();   // rounds of narrow ones
       if (thin < 3) drop = (excess + pool->num_kv_heads - 1) / pool->num_kv_heads;
@@ -1372,12 +1377,16 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
       const int64_t len = (int64_t)a.seq[i].prefix + a.seq[i].suffix;
       a.unit_begin[i] = (int32_t)units;
       a.narrow_begin[i] = (int32_t)narrow;
-      int64_t wide = step ? (len + keys - 1) / keys : len / keys;
-      const int64_t fewer = std::min(wide, drop);
-      wide -= fewer;
-      drop -= fewer;
-      units += wide;
-      if (!step) narrow += (len - wide * keys + 31) / 32;
+      if (step) {
+        units += (len + keys - 1) / keys;
+      } else if (once) {
+        units += ((len + keys - 1) / keys + a.tiles - 1) / a.tiles;
+      } else {
+        const int64_t wide = len / keys - std::min(len / keys, drop);
+        drop -= len / keys - wide;
+        units += wide;
+        narrow += (len - wide * keys + 31) / 32;
+      }
       if ((units + narrow) * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
     }
     a.unit_begin[n] = (int32_t)units;

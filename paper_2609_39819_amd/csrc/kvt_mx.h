@@ -89,6 +89,7 @@ struct WeightsArgs {
   int32_t group;        // Hq / Hkv
   float scale_log2;
   int32_t share;        // step kernel: tiles of a workgroup
+  int32_t tiles;        // turn kernel: of a workgroup, if every sequence's rows are one stage; else 0
   int32_t nseq;
   int32_t unit_begin[kSeqsPerLaunch + 1];   // prefix sums of the sequences' tiles (step kernel) or wide workgroups
   int32_t narrow_begin[kSeqsPerLaunch + 1]; // turn kernel: of the narrow ones, for the keys after those
@@ -135,7 +136,8 @@ constexpr int kMx = 2;
 hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
 constexpr int kWeightsStepKeys = 32;      // step kernel: keys of one tile
-constexpr int kWeightsWideKeys = 256;     // turn kernel: keys of a wide workgroup (a narrow one: 32)
+constexpr int kWeightsWideKeys = 256;     // turn kernel: keys of a wide workgroup's tile (a narrow one's: 32)
+constexpr int weights_stage_rows(int dtype) { return dtype == 0 ? 256 : 64; }   // turn kernel: rows in LDS at a time
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t stream);
 hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int grid, hipStream_t stream);
 

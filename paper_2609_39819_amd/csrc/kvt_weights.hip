@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
 // Rows of queries in LDS at a time, as the operand terms of their type: [term][row][D] bf16,
 // the 16-byte chunks of a row XOR-swizzled as a key tile's in the extend kernel.
 template <typename T>
-constexpr int kTurnRows = sizeof(T) == 2 ? 256 : 64;
+constexpr int kTurnRows = weights_stage_rows(sizeof(T) == 2 ? 0 : 1);
 template <typename T, int D>
 struct TurnRows {
   __bf16 q[kTerms<T>][kTurnRows<T> * D];
@@ -266,7 +266,7 @@ struct TurnRows {
   int lim[kTurnRows<T>];
 };
 
-template <typename T, int D, int FORMAT>
+template <typename T, int D, int FORMAT, bool ONCE>
 __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) {
   constexpr bool kCodes = FORMAT == kMx;
   constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
@@ -282,51 +282,70 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   const int hh = lane >> 5, l32 = lane & 31;
 
   // ---- a wide workgroup has 32 keys per wave and every wave takes all rows, a
-  // narrow one has 32 keys and its waves take the row blocks in turn
+  // narrow one has 32 keys and its waves take the row blocks in turn.  ONCE: the
+  // rows of every sequence are one stage, which stays in LDS, and a workgroup (all
+  // are wide) goes through a.tiles tiles of keys, the next one's in flight.
   const int hkv = a.num_kv_heads, G = a.group;
   const int g = blockIdx.x % hkv;
   const int unit = blockIdx.x / hkv;
-  const bool narrow = unit >= a.unit_begin[a.nseq];
+  const bool narrow = !ONCE && unit >= a.unit_begin[a.nseq];
   const int at = narrow ? unit - a.unit_begin[a.nseq] : unit;
   const int si = find_seq(narrow ? a.narrow_begin : a.unit_begin, a.nseq, at);
   const SeqDesc sd = a.seq[si];
   const int P = sd.prefix, L = P + sd.suffix, rows = sd.suffix * G;
-  const int wide_keys = (a.unit_begin[si + 1] - a.unit_begin[si]) * kWeightsWideKeys;
-  const int kb0 = narrow ? wide_keys + (at - a.narrow_begin[si]) * 32 : (at - a.unit_begin[si]) * kWeightsWideKeys;
-  const int kb = narrow ? kb0 : kb0 + wave * 32;
+  const int stages = (rows + ROWS - 1) / ROWS;
+  const int step = narrow ? 32 : kWeightsWideKeys;       // keys of a tile
+  const int wide_keys = (a.unit_begin[si + 1] - a.unit_begin[si]) * kWeightsWideKeys;   // where there are narrow ones
+  const int start = narrow ? wide_keys + (at - a.narrow_begin[si]) * 32
+                           : (at - a.unit_begin[si]) * kWeightsWideKeys * (ONCE ? a.tiles : 1);
+  const int stop = ONCE ? min(L, start + a.tiles * kWeightsWideKeys) : start + step;
   const int nblk = (L + kBlock - 1) / kBlock;
+  float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
 
-  // ---- this wave's keys, as operands (past the end the last one: not stored)
-  bf16x8 kf[KSTEPS][KN];
-  {
-    const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
+  // ---- the keys from kb on, one a lane pair, as stored (past the end the last
+  // one: not stored)
+  const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
+  constexpr int KP = kCodes ? D / 64 : KSTEPS * (FORMAT == 0 ? 1 : 2);   // 16-byte pieces of a lane's columns
+  constexpr bool kFly = ONCE && FORMAT != 1;     // the next tile's in flight (fp32: too many registers)
+  u32x4 kraw[KP];
+  unsigned char kscale[kCodes ? D / 64 : 1];
+  auto page_of = [&](int kb) __attribute__((always_inline)) {
     const int pos = min(kb + l32, L - 1);
-    const uint32_t id =
-        min((uint32_t)a.block_table[(int64_t)sd.seq * a.max_blocks + min(pos / kBlock, nblk - 1)], nb_max);
-    const int slot = pos % kBlock;
-    const char* page = reinterpret_cast<const char*>(a.k_pool) + ((int64_t)id * hkv + g) * kPage;
+    return (uint32_t)a.block_table[(int64_t)sd.seq * a.max_blocks + min(pos / kBlock, nblk - 1)];
+  };
+  auto load_keys = [&](int kb, uint32_t id) __attribute__((always_inline)) {
+    const int slot = min(kb + l32, L - 1) % kBlock;
+    const char* page = reinterpret_cast<const char*>(a.k_pool) + ((int64_t)min(id, nb_max) * hkv + g) * kPage;
     if constexpr (kCodes) {
 #pragma unroll
-      for (int y = 0; y < D / 64; ++y) {         // 32 columns: four words under one scale
-        const u32x4 c4 = *reinterpret_cast<const u32x4*>(page + slot * (D / 2) + hh * (D / 4) + y * 16);
-        const float scale = mx_scale((unsigned char)page[mx_code_bytes(D) + slot * (D / 32) + hh * (D / 64) + y]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kf[y * 4 + i][0] = mx_values(c4[i], scale);
+      for (int y = 0; y < KP; ++y) {             // 32 columns: four words under one scale
+        kraw[y] = *reinterpret_cast<const u32x4*>(page + slot * (D / 2) + hh * (D / 4) + y * 16);
+        kscale[y] = (unsigned char)page[mx_code_bytes(D) + slot * (D / 32) + hh * (D / 64) + y];
       }
     } else {
-      typedef typename std::conditional<FORMAT == 0, __bf16, float>::type K;
+      constexpr int ES = FORMAT == 0 ? 2 : 4, PER = FORMAT == 0 ? 1 : 2;
 #pragma unroll
-      for (int kk = 0; kk < KSTEPS; ++kk)
-        load_terms(reinterpret_cast<const K*>(page) + slot * D + kk * 16 + hh * 8, kf[kk]);
+      for (int y = 0; y < KP; ++y)
+        kraw[y] = *reinterpret_cast<const u32x4*>(page + (slot * D + (y / PER) * 16 + hh * 8) * ES + 16 * (y % PER));
     }
-  }
+  };
+  bf16x8 kf[KSTEPS][KN];
+  auto take_keys = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int kk = 0; kk < KSTEPS; ++kk) {
+      if constexpr (kCodes) kf[kk][0] = mx_values(kraw[kk / 4][kk % 4], mx_scale(kscale[kk / 4]));
+      else if constexpr (FORMAT == 0) kf[kk][0] = __builtin_bit_cast(bf16x8, kraw[kk]);
+      else split3(__builtin_bit_cast(f32x4, kraw[2 * kk]), __builtin_bit_cast(f32x4, kraw[2 * kk + 1]), kf[kk]);
+    }
+  };
+  int kb = start + (narrow ? 0 : wave * 32);
+  uint32_t id = page_of(kb);
 
   // ---- rows in stages, from the first that sees one of the workgroup's keys.
   // Row r of a stage whose first row is head h0 of token t0 is head x - d * G of
   // token t0 + d, d = x / G, x = h0 + r (a product with 2^32 / G, rounded up: exact
   // for these small numbers).
-  const int first = kb0 > P ? (int)((int64_t)(kb0 - P) * G / ROWS) : 0;
-  const int stages = (rows + ROWS - 1) / ROWS;
+  const int first = !ONCE && start > P ? (int)((int64_t)(start - P) * G / ROWS) : 0;
   const int adv_t = ROWS / G, adv_h = ROWS - adv_t * G;
   int t0 = (int)((int64_t)first * ROWS / G), h0 = first * ROWS - t0 * G;    // of the stage that is loaded next
   const unsigned magic = G == 1 ? 0u : 0xffffffffu / (unsigned)G + 1u;
@@ -388,8 +407,6 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   };
 
   float acc[16];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
   const float c = a.scale_log2;
   auto scores = [&](const TurnRows<T, D>& from, int block) __attribute__((always_inline)) {
     const int row = block * 32 + l32;
@@ -415,65 +432,84 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
       else acc[e] += p;
     }
   };
-  if (first < stages) {
-    int seen = t0, seen_h = h0;                  // first row of the stage that is computed: it sees the fewest keys
-    load_stage(stage[0]);
-    drop(stage[0]);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    __syncthreads();
-    for (int i = first; i < stages; ++i) {
-      const TurnRows<T, D>& cur = stage[(i - first) & 1];
-      TurnRows<T, D>& fill = stage[(i + 1 - first) & 1];
-      if (i + 1 < stages) load_stage(fill);
-      const bool whole = P + seen >= kb + 31 && (i + 1) * ROWS <= rows;
-      if (narrow) {
-        if (wave < BLOCKS) add(cur, wave, scores(cur, wave), std::true_type());
-      } else if (whole) {
-        f32x16 s = scores(cur, 0);
+  // one stage of rows, the first of which is `seen`'s and sees the fewest keys
+  auto take_rows = [&](const TurnRows<T, D>& cur, int seen, int last) __attribute__((always_inline)) {
+    if (narrow) {
+      if (wave < BLOCKS) add(cur, wave, scores(cur, wave), std::true_type());
+    } else if (P + seen >= kb + 31 && last <= rows) {
+      f32x16 s = scores(cur, 0);
 #pragma unroll
-        for (int block = 0; block < BLOCKS; ++block) {
-          f32x16 s1 = s;
-          if (block + 1 < BLOCKS) s1 = scores(cur, block + 1);
-          add(cur, block, s, std::false_type());
-          s = s1;
-          if constexpr (QN == 1 && KN == 1) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+      for (int block = 0; block < BLOCKS; ++block) {
+        f32x16 s1 = s;
+        if (block + 1 < BLOCKS) s1 = scores(cur, block + 1);
+        add(cur, block, s, std::false_type());
+        s = s1;
+        if constexpr (QN == 1 && KN == 1) {      // the next products beside the exponentials
+          __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-            for (int i = 0; i < KSTEPS; ++i) {
-              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-              __builtin_amdgcn_sched_group_barrier(0x002, 48 / KSTEPS, 0);
-              __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
+          for (int i = 0; i < KSTEPS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 48 / KSTEPS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
           }
         }
-      } else {
-        for (int block = 0; block < BLOCKS; ++block) add(cur, block, scores(cur, block), std::true_type());
       }
-      seen += adv_t;
-      seen_h += adv_h;
-      if (seen_h >= G) seen_h -= G, ++seen;
-      if (i + 1 < stages) drop(fill);
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-      __syncthreads();
+    } else {
+      const int blocks = min(BLOCKS, (rows - (last - ROWS) + 31) / 32);
+      for (int block = 0; block < blocks; ++block) add(cur, block, scores(cur, block), std::true_type());
     }
-  }
-  // ---- sums over the rows: the lanes of a half, and of a narrow workgroup the
-  // waves, in order
-  float sum = scatter_sum(acc, lane, 16);        // of element l32 >> 1, half of it
-  sum += __shfl_xor(sum, 1);
-  const int e = l32 >> 1, k32 = 8 * (e >> 2) + 4 * hh + (e & 3);
-  float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
-  if (!narrow) {
-    if ((lane & 1) == 0 && kb + k32 < L) put(w, kb + k32, sd, sum);
-    return;
-  }
-  float* red = reinterpret_cast<float*>(turn_lds);   // the stages are done with
-  if ((lane & 1) == 0) red[wave * 32 + k32] = sum;
+  };
+  int seen = t0, seen_h = h0;
+  load_stage(stage[0]);
+  load_keys(kb, id);
+  drop(stage[0]);
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   __syncthreads();
-  if (tid < 32 && kb + tid < L) {
-    sum = 0.f;
-    for (int x = 0; x < 8; ++x) sum += red[x * 32 + tid];
-    put(w, kb + tid, sd, sum);
+  for (int base = start; base < stop; base += step) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    if (ONCE && !kFly && base != start) load_keys(kb, id);
+    take_keys();
+    const int e = l32 >> 1, k32 = 8 * (e >> 2) + 4 * hh + (e & 3);   // the key whose sum ends in this lane
+    const float old = w[min(kb + k32, L - 1)];
+    const int next = kb + step;
+    if constexpr (ONCE) {
+      if (base + step < stop) {
+        id = page_of(next);
+        if (kFly) load_keys(next, id);
+      }
+      take_rows(stage[0], 0, ROWS);
+    } else {
+      for (int i = first; i < stages; ++i) {
+        TurnRows<T, D>& fill = stage[(i + 1 - first) & 1];
+        if (i + 1 < stages) load_stage(fill);
+        take_rows(stage[(i - first) & 1], seen, (i + 1) * ROWS);
+        seen += adv_t;
+        seen_h += adv_h;
+        if (seen_h >= G) seen_h -= G, ++seen;
+        if (i + 1 < stages) drop(fill);
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        __syncthreads();
+      }
+    }
+    // ---- sums over the rows: the lanes of a half, and of a narrow workgroup the
+    // waves, in order
+    float sum = scatter_sum(acc, lane, 16);      // of element l32 >> 1, half of it
+    sum += __shfl_xor(sum, 1);
+    if (!narrow) {
+      if ((lane & 1) == 0 && kb + k32 < L) w[kb + k32] = kb + k32 < P ? old + sum : sum;
+    } else {
+      float* red = reinterpret_cast<float*>(turn_lds);   // the rows are done with
+      __syncthreads();
+      if ((lane & 1) == 0) red[wave * 32 + k32] = sum;
+      __syncthreads();
+      if (tid < 32 && kb + tid < L) {
+        sum = 0.f;
+        for (int x = 0; x < 8; ++x) sum += red[x * 32 + tid];
+        put(w, kb + tid, sd, sum);
+      }
+    }
+    kb = next;
   }
 }
 
@@ -486,7 +522,11 @@ void launch_step_as(const WeightsArgs& a, int grid, hipStream_t stream) {
 }
 template <typename T, int D, int FORMAT>
 void launch_turn_as(const WeightsArgs& a, int grid, hipStream_t stream) {
-  hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT>), dim3(grid), dim3(512), 2 * sizeof(TurnRows<T, D>), stream, a);
+  if (a.tiles > 0)
+    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, true>), dim3(grid), dim3(512), sizeof(TurnRows<T, D>), stream, a);
+  else
+    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, false>), dim3(grid), dim3(512), 2 * sizeof(TurnRows<T, D>),
+                       stream, a);
 }
 
 }  // namespace
