@@ -1215,6 +1215,16 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
     // a sequence lies in at most one slot more than its tiles fill
     share = std::max(share, (longest + kvt::kMaxPartials - 2) / (kvt::kMaxPartials - 1));
+    // A slot for each sequence needs no join (a launch, the workspace: 6.5 us); a
+    // workgroup takes 0.18 us a tile, all of them 5.5 TB/s.  Calls of one context of
+    // 1000, 2000 and 3000 keys, 32/8 heads of 128: 11.1, 15.8 and 21.7 us so, 16.5
+    // in shares; 48 contexts of 1000, 4000 and 6000: 14.6, 43.6 and 63.0; 20.6,
+    // 45.2 and 61.3.
+    const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
+    const double stream = (double)total * heads * tile_bytes / 5.5e6;
+    const int64_t rounds = (n + slots - 1) / slots;
+    const double alone = std::max(rounds * 0.18 * longest + (rounds - 1) * 3.0, stream);
+    if (alone <= 6.5 + std::max(0.18 * share, stream)) share = total;
     bool split = false;
     int64_t begin = 0;
     for (int i = 0; i < n; ++i) {

@@ -139,7 +139,10 @@ DECODES = [  # prefix, hq, hkv, d
     ([0], 4, 1, 64), ([0, 1, 14, 15, 16, 17, 30, 31, 32, 33, 63, 64, 127, 128, 129], 8, 2, 128),
     ([5000, 3, 700], 32, 8, 64), ([20000], 12, 1, 128), ([300, 2000], 16, 1, 64), ([300, 2000], 17, 1, 128),
     ([1000], 32, 1, 128), ([1000, 4097], 40, 1, 64), ([777], 96, 2, 128), ([100] * 40, 8, 8, 128),
-    ([6000, 100, 100, 3000], 24, 2, 128)]
+    ([6000, 100, 100, 3000], 24, 2, 128),
+    # shares that hold parts of one context and many whole short ones, and a second launch without long ones
+    ([20000] + list(range(130)), 8, 2, 128), ([9000, 7000, 33] + [30, 31, 63, 64, 95, 96, 127] * 8, 4, 1, 64),
+    ([12000] + [7 * b % 90 for b in range(299)], 24, 1, 64), ([30000, 2999, 0, 1] * 3, 16, 2, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
