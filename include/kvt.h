@@ -436,10 +436,11 @@ kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_
  * keeps fp32's precision.  lse is summed in fp32 from unrounded probabilities.
  * A token that is no number makes the rows that see it NaN, and no others.
  *
- * Arguments, workspace rules and errors as for kvt_extend_attention, with
- * kvt_mx_extend_workspace_bytes; the workspace of a call that is split may not
- * overlap q, out, lse or the pools (KVT_ERR_INVALID_ARG).  Results are
- * bit-reproducible for given arguments.
+ * Arguments and errors as for kvt_extend_attention.  workspace: NULL/0 runs
+ * without splitting, otherwise at least kvt_mx_extend_workspace_bytes() for the
+ * same arguments, 16-byte aligned and apart from q, out, lse and the pools (else
+ * KVT_ERR_WORKSPACE, KVT_ERR_INVALID_ARG; any workspace will do where that is
+ * 0).  Results are bit-reproducible for given arguments.
  */
 kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs,
                                  const void* q, int32_t num_q_heads, float scale,

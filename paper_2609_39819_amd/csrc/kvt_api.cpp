@@ -1181,18 +1181,24 @@ bool workspace_apart(const kvt_pool* pool, const void* q, const void* out, const
          (lse == nullptr || !overlaps(workspace, bytes, lse, (size_t)T * num_q_heads * sizeof(float)));
 }
 
-// A decoding step over 4-bit pages, launch by launch: see MxDecodeArgs.
+// A call of few query rows over 4-bit pages (a decoding step, short chunks), launch
+// by launch: see MxDecodeArgs.
 struct MxDecodePlan {
   std::vector<int> order;          // sequences, longest key range first
   std::vector<int32_t> share;      // by launch: tiles of a slot, 0: slot x is sequence x
   std::vector<int32_t> parts;      // by place in `order`: slots that hold a part of the sequence
-  int chunks = 1;                  // workgroups that share a kv-head's query heads
+  int chunks = 1;                  // workgroups that share the rows of a kv-head
   int64_t part_rows = 0;
   size_t ws_bytes = 0;
 };
 
 int64_t mx_tiles(const kvt_seqs* seqs, int b) {
-  return ((int64_t)seqs->prefix_len[b] + kvt::kDecKeysPerTile) / kvt::kDecKeysPerTile;
+  return ((int64_t)seqs->prefix_len[b] + seqs->suffix_len[b] + kvt::kDecKeysPerTile - 1) / kvt::kDecKeysPerTile;
+}
+bool mx_few_rows(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
+  for (int b = 0; b < seqs->num_seqs; ++b)
+    if ((int64_t)seqs->suffix_len[b] * (num_q_heads / pool->num_kv_heads) > kvt::kMxFewRows) return false;
+  return true;
 }
 size_t mx_part_o_bytes(const kvt_pool* pool, int64_t part_rows) {
   return ((size_t)part_rows * pool->head_dim * sizeof(float) + 255) / 256 * 256;
@@ -1201,7 +1207,9 @@ size_t mx_part_o_bytes(const kvt_pool* pool, int64_t part_rows) {
 MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   MxDecodePlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
-  p.chunks = (G + kvt::kMxDecMaxRows - 1) / kvt::kMxDecMaxRows;
+  int64_t most = 0;
+  for (int b = 0; b < B; ++b) most = std::max(most, (int64_t)seqs->suffix_len[b] * G);
+  p.chunks = (int)((most + kvt::kMxChunkRows - 1) / kvt::kMxChunkRows);
   p.order = longest_first(seqs);
   p.parts.assign(B, 1);
   const int64_t heads = (int64_t)pool->num_kv_heads * p.chunks;
@@ -1232,7 +1240,7 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
       const int parts = (int)((end - 1) / share - begin / share + 1);
       split = split || parts > 1;
       p.parts[c0 + i] = parts;
-      if (parts > 1) p.part_rows += (int64_t)parts * num_q_heads;
+      if (parts > 1) p.part_rows += (int64_t)parts * seqs->suffix_len[p.order[c0 + i]] * num_q_heads;
       begin = end;
     }
     p.share.push_back(split ? (int32_t)share : 0);
@@ -1244,6 +1252,84 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
   }
   if (p.part_rows > 0) p.ws_bytes = mx_part_o_bytes(pool, p.part_rows) + (size_t)p.part_rows * 2 * sizeof(float);
   return p;
+}
+
+// Launches of a call of few rows: the shares, then the join of what they split.
+kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads, float scale,
+                         void* out, float* lse, int64_t T, void* workspace, size_t workspace_bytes, void* stream) {
+  MxDecodePlan plan = mx_decode_plan(pool, seqs, num_q_heads);
+  if (plan.ws_bytes > 0) {
+    if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
+      plan.parts.assign(seqs->num_seqs, 1);
+      plan.share.assign(plan.share.size(), 0);
+      plan.ws_bytes = 0;
+    } else {
+      if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
+      if (!aligned16(workspace) || !workspace_apart(pool, q, out, lse, num_q_heads, T, workspace, plan.ws_bytes))
+        return KVT_ERR_INVALID_ARG;
+    }
+  }
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  kvt::MxDecodeArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.out = out;
+  a.lse = lse;
+  a.block_table = seqs->block_table;
+  a.num_blocks = pool->num_blocks;
+  a.max_blocks = seqs->max_blocks;
+  a.num_q_heads = num_q_heads;
+  a.num_kv_heads = pool->num_kv_heads;
+  a.group = num_q_heads / pool->num_kv_heads;
+  a.chunks = plan.chunks;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  if (plan.ws_bytes > 0) {
+    a.part_o = reinterpret_cast<float*>(workspace);
+    a.part_ml = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + mx_part_o_bytes(pool, plan.part_rows));
+  }
+  kvt::MxJoinArgs join;
+  join.part_o = a.part_o;
+  join.part_ml = a.part_ml;
+  join.out = out;
+  join.lse = lse;
+  std::vector<int32_t> row_off(seqs->num_seqs + 1, 0);
+  for (int b = 0; b < seqs->num_seqs; ++b) row_off[b + 1] = row_off[b] + seqs->suffix_len[b];
+  int64_t part_row = 0;
+  for (int c0 = 0, launch = 0; c0 < seqs->num_seqs; c0 += kvt::kSeqsPerLaunch, ++launch) {
+    const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - c0);
+    a.nseq = n;
+    a.share = plan.share[launch];
+    join.nseq = 0;
+    join.row_begin[0] = 0;
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) {
+      const int b = plan.order[c0 + i], parts = plan.parts[c0 + i];
+      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], seqs->suffix_len[b], row_off[b]};
+      a.tile_begin[i] = (int32_t)tiles;
+      a.part_row[i] = (int32_t)part_row;
+      tiles += mx_tiles(seqs, b);
+      if (parts > 1) {
+        const int32_t rows = seqs->suffix_len[b] * num_q_heads;
+        join.part_row[join.nseq] = (int32_t)part_row;
+        join.row[join.nseq] = row_off[b] * num_q_heads;
+        join.parts[join.nseq] = (uint8_t)parts;
+        join.row_begin[join.nseq + 1] = join.row_begin[join.nseq] + rows;
+        ++join.nseq;
+        part_row += (int64_t)parts * rows;
+      }
+    }
+    if (tiles > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    a.tile_begin[n] = (int32_t)tiles;
+    const int64_t slots = a.share > 0 ? (tiles + a.share - 1) / a.share : n;
+    const int64_t grid = slots * pool->num_kv_heads * plan.chunks;
+    if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, (int)grid, s);
+    if (e == hipSuccess && join.nseq > 0) e = kvt::launch_mx_join(join, pool->dtype, pool->head_dim, s);
+    if (e != hipSuccess) return device_error(e);
+  }
+  return KVT_OK;
 }
 
 // Token rows of a 4-bit append or read; fills the launch arguments.
@@ -1980,7 +2066,11 @@ kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_
 }
 
 size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) try {
-  return kvt_extend_workspace_bytes(pool, seqs, num_q_heads);
+  if (check_pool(pool) != KVT_OK) return 0;
+  int64_t T = 0;
+  if (check_seqs(seqs, &T) != KVT_OK || !heads_ok(pool, num_q_heads, T)) return 0;
+  if (mx_few_rows(pool, seqs, num_q_heads)) return mx_decode_plan(pool, seqs, num_q_heads).ws_bytes;
+  return extend_plan(pool, seqs, num_q_heads, T).ws_bytes;
 } catch (const std::bad_alloc&) {
   return 0;
 }
@@ -1991,6 +2081,8 @@ kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs, c
   int64_t T = 0;
   const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
   if (st != KVT_OK) return st;
+  if (mx_few_rows(pool, seqs, num_q_heads))
+    return launch_mx_few(pool, seqs, q, num_q_heads, scale, out, lse, T, workspace, workspace_bytes, stream);
   ExtendPlan plan = extend_plan(pool, seqs, num_q_heads, T);
   const kvt_status fit = fit_workspace(&plan, pool, T * num_q_heads, workspace, workspace_bytes);
   if (fit != KVT_OK) return fit;
@@ -2017,74 +2109,7 @@ kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, c
   const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
   if (st != KVT_OK) return st;
   if (T != seqs->num_seqs) return KVT_ERR_INVALID_ARG;   // one new token per sequence
-  MxDecodePlan plan = mx_decode_plan(pool, seqs, num_q_heads);
-  if (plan.ws_bytes > 0) {
-    if (workspace == nullptr && workspace_bytes == 0) {   // no scratch offered: run unsplit
-      plan.parts.assign(seqs->num_seqs, 1);
-      plan.share.assign(plan.share.size(), 0);
-      plan.ws_bytes = 0;
-    } else {
-      if (workspace == nullptr || workspace_bytes < plan.ws_bytes) return KVT_ERR_WORKSPACE;
-      if (!aligned16(workspace) || !workspace_apart(pool, q, out, lse, num_q_heads, T, workspace, plan.ws_bytes))
-        return KVT_ERR_INVALID_ARG;
-    }
-  }
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  kvt::MxDecodeArgs a;
-  std::memset(&a, 0, sizeof(a));
-  a.q = q;
-  a.k_pool = pool->k;
-  a.v_pool = pool->v;
-  a.out = out;
-  a.lse = lse;
-  a.block_table = seqs->block_table;
-  a.num_blocks = pool->num_blocks;
-  a.max_blocks = seqs->max_blocks;
-  a.num_q_heads = num_q_heads;
-  a.num_kv_heads = pool->num_kv_heads;
-  a.group = num_q_heads / pool->num_kv_heads;
-  a.chunks = plan.chunks;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  if (plan.ws_bytes > 0) {
-    a.part_o = reinterpret_cast<float*>(workspace);
-    a.part_ml = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + mx_part_o_bytes(pool, plan.part_rows));
-  }
-  kvt::MxJoinArgs join;
-  join.part_o = a.part_o;
-  join.part_ml = a.part_ml;
-  join.out = out;
-  join.lse = lse;
-  join.num_q_heads = num_q_heads;
-  int64_t part_row = 0;
-  for (int c0 = 0, launch = 0; c0 < seqs->num_seqs; c0 += kvt::kSeqsPerLaunch, ++launch) {
-    const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - c0);
-    a.nseq = n;
-    a.share = plan.share[launch];
-    join.nseq = 0;
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) {
-      const int b = plan.order[c0 + i], parts = plan.parts[c0 + i];
-      a.seq[i] = kvt::SeqDesc{b, seqs->prefix_len[b], 1, b};   // row of sequence b is b
-      a.tile_begin[i] = (int32_t)tiles;
-      a.part_row[i] = (int32_t)part_row;
-      tiles += mx_tiles(seqs, b);
-      if (parts > 1) {
-        join.part_row[join.nseq] = (int32_t)part_row;
-        join.row[join.nseq] = b * num_q_heads;
-        join.parts[join.nseq++] = (uint8_t)parts;
-        part_row += (int64_t)parts * num_q_heads;
-      }
-    }
-    if (tiles > INT32_MAX) return KVT_ERR_INVALID_ARG;
-    a.tile_begin[n] = (int32_t)tiles;
-    const int64_t slots = a.share > 0 ? (tiles + a.share - 1) / a.share : n;
-    const int64_t grid = slots * pool->num_kv_heads * plan.chunks;
-    if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
-    hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, (int)grid, s);
-    if (e == hipSuccess && join.nseq > 0) e = kvt::launch_mx_join(join, pool->dtype, pool->head_dim, s);
-    if (e != hipSuccess) return device_error(e);
-  }
-  return KVT_OK;
+  return launch_mx_few(pool, seqs, q, num_q_heads, scale, out, lse, T, workspace, workspace_bytes, stream);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }

@@ -30,14 +30,12 @@ struct MxRowsArgs {
   SeqDesc seq[kSeqsPerLaunch];  // in packed-row order
 };
 
-// Decoding: query heads of one kv-head that one workgroup serves.
-constexpr int kMxDecMaxRows = 32;
-
-// Decoding: the tiles of kDecKeysPerTile keys of a launch's sequences lie one
-// after the other, and slot x of a kv-head takes tiles x * share .. (x + 1) *
-// share - 1: parts of as many sequences as lie there.  share 0: slot x is
-// sequence x.  A sequence in more than one slot leaves a partial result in each,
-// n of them from row part_row on, [n][Hq].
+// Attention of few query rows (a decoding step, a short chunk).  The tiles of
+// kDecKeysPerTile keys of a launch's sequences lie one after the other, and slot x
+// of a kv-head takes tiles x * share .. (x + 1) * share - 1: parts of as many
+// sequences as lie there.  share 0: slot x is sequence x.  A sequence in more than
+// one slot leaves a partial result in each, parts of them from row part_row on,
+// [parts][S_b * Hq].
 struct MxDecodeArgs {
   const void* q;
   const void* k_pool;
@@ -52,7 +50,7 @@ struct MxDecodeArgs {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t group;        // Hq / Hkv
-  int32_t chunks;       // workgroups that share a kv-head's query heads
+  int32_t chunks;       // workgroups that share the rows of a kv-head (S_b * group): of the longest
   float scale_log2;
   int32_t share;
   int32_t nseq;
@@ -60,17 +58,19 @@ struct MxDecodeArgs {
   int32_t part_row[kSeqsPerLaunch];
   SeqDesc seq[kSeqsPerLaunch];
 };
+constexpr int kMxChunkRows = 32;   // rows of a workgroup at most
+constexpr int kMxFewRows = 64;     // rows of a kv-head up to which an extend call counts as one of few
 
-// The join of a step's split sequences.
+// The join of a launch's split sequences.
 struct MxJoinArgs {
   const float* part_o;
   const float* part_ml;
   void* out;
   float* lse;
-  int32_t num_q_heads;
   int32_t nseq;
+  int32_t row_begin[kSeqsPerLaunch + 1];   // prefix sums of the sequences' rows (S_b * Hq)
   int32_t part_row[kSeqsPerLaunch];
-  int32_t row[kSeqsPerLaunch];      // output row of head 0
+  int32_t row[kSeqsPerLaunch];             // first output row
   uint8_t parts[kSeqsPerLaunch];
 };
 

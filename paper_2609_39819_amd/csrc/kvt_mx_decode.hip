@@ -1,9 +1,10 @@
-// Decode attention over 4-bit pages, gfx950: one new token per sequence.
+// Attention of few query rows over 4-bit pages, gfx950: a decoding step, or chunks
+// of up to 64 rows (new tokens x query heads) of a kv-head.
 //
-// The formula is kvt_decode.hip's; the cost is streaming each sequence's 4-bit
+// The formula is kvt_decode.hip's, with a last visible position for each row; the cost is streaming each sequence's 4-bit
 // K/V once from HBM (2 * 17/32 D bytes a key and kv-head).  Work decomposition:
 //   * the batch's 32-key tiles lie one after the other, and one workgroup per (equal
-//     share of them, kv-head, up to 32 of the kv-head's query heads) goes through
+//     share of them, kv-head, up to 32 of the kv-head's rows) goes through
 //     the parts of sequences in its share; of each, wave w of 4 takes the tiles w,
 //     w+4, .. and keeps two of them in flight in registers, across the sequences'
 //     borders; no barrier in the loop;
@@ -49,7 +50,8 @@ __device__ __forceinline__ int swz_mx(int key) {
   else return (((key >> 1) & 3) << 1) | ((key >> 3) & 1);
 }
 
-template <typename T, int D, int NB>
+// STEP: one new token per sequence, which sees all of it.
+template <typename T, int D, int NB, bool STEP>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 ? 1 : 2) void mx_decode_kernel(const MxDecodeArgs a) {
   constexpr int NT = kTerms<T>;
   constexpr int KS = D / 32;                     // score steps = words of a lane's codes
@@ -65,16 +67,15 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   const int l16 = lane & 15;
   const int qd = lane >> 4;
 
-  // ---- which kv-head, query heads and tiles this workgroup owns
+  // ---- which kv-head, rows and tiles this workgroup owns (row r of a sequence is
+  // token r / G, head g * G + r % G)
   const int hkv = a.num_kv_heads;
   const int G = a.group;
   const int chunks = a.chunks;
   const int g = blockIdx.x % hkv;
   const int rest = blockIdx.x / hkv;
   const int unit = chunks == 1 ? rest : rest / chunks;
-  const int per_chunk = (G + chunks - 1) / chunks;
-  const int head0 = (rest - unit * chunks) * per_chunk;
-  const int heads = min(per_chunk, G - head0);
+  const int r0 = (rest - unit * chunks) * NB * 16;   // this workgroup's rows of a sequence start here
   const int share = a.share;
   const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const char* vpool = reinterpret_cast<const char*>(a.v_pool);
@@ -100,17 +101,17 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   auto enter = [&](int x, int first_tile) __attribute__((always_inline)) {
     const SeqDesc sd = a.seq[x];
     at.si = x;
-    at.L = sd.prefix + 1;                        // keys 0..P_b
+    at.L = sd.prefix + sd.suffix;
     at.nblk = (at.L + kBlock - 1) / kBlock;
     at.j = first_tile - a.tile_begin[x] + wave;
-    at.j1 = min(to, a.tile_begin[x + 1]) - a.tile_begin[x];
+    at.j1 = STEP || sd.suffix * G > r0 ? min(to, a.tile_begin[x + 1]) - a.tile_begin[x] : 0;   // 0: no rows, no tiles
     at.bt = (Ids)(a.block_table + (int64_t)sd.seq * a.max_blocks);
   };
   // the next tile with work for this wave; past the last one its place stays (on
   // a tile of the slot's last sequence)
   auto settle = [&]() __attribute__((always_inline)) {
     while (at.j >= at.j1 && a.tile_begin[at.si + 1] < to) enter(at.si + 1, a.tile_begin[at.si + 1]);
-    at.j = min(at.j, at.j1 - 1);
+    at.j = STEP ? min(at.j, at.j1 - 1) : max(0, min(at.j, at.j1 - 1));
   };
   enter(si, from);
   settle();
@@ -158,27 +159,29 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     page_ids();
   };
 
-  // ---- this lane's query rows (rows past the last head repeat it and are
-  // dropped): columns qd * D/4 ..
+  // ---- this lane's query rows (rows past the last repeat it and are dropped):
+  // columns qd * D/4 .., and the last position each sees
   bf16x8 qreg[NB][KS][NT];
-  auto load_rows = [&](int64_t first_row) __attribute__((always_inline)) {
+  int lim[STEP ? 1 : NB];
+  auto load_rows = [&](int x) __attribute__((always_inline)) {
+    const SeqDesc sd = a.seq[x];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const T* qp = reinterpret_cast<const T*>(a.q) + (first_row + min(b * 16 + l16, heads - 1)) * D + qd * (D / 4);
+      const unsigned r = min(r0 + b * 16 + l16, (STEP ? G : sd.suffix * G) - 1), t = STEP ? 0u : r / (unsigned)G;
+      const int64_t row = (int64_t)(sd.row_off + (int)t) * a.num_q_heads + g * G + (int)(r - t * G);
+      const T* qp = reinterpret_cast<const T*>(a.q) + row * D + qd * (D / 4);
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) load_terms(qp + kk * 8, qreg[b][kk]);
+      if constexpr (!STEP) lim[b] = sd.prefix + (int)t;
     }
-  };
-  auto first_row_of = [&](int x) __attribute__((always_inline)) {
-    return (int64_t)a.seq[x].row_off * a.num_q_heads + g * G + head0;
   };
 
   f32x4 o[NB][CT];
   float m_ref[NB], l_run[NB];
 
-  // ---- the tile of a sequence of L keys that starts at key kb, from its stage,
-  // which is refilled as soon as it is free
-  auto tile = [&](Stage& st, int kb, int L) __attribute__((always_inline)) {
+  // ---- the tile that starts at key kb, from its stage, which is refilled as soon
+  // as it is free; every row sees the keys before `seen`
+  auto tile = [&](Stage& st, int kb, int seen) __attribute__((always_inline)) {
     // V into LDS.  A token that is not a number counts through K (its score is
     // one for the rows that see it); its V becomes 0, so that no other row
     // takes it in with a weight of 0.
@@ -209,14 +212,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       }
     }
     load_tile(st);
-    if (kb + kTK > L) {   // the sequence ends inside this tile
+    if (kb + kTK > seen) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (kb + 16 * p + 4 * qd + e >= L) s[b][p][e] = -INFINITY;
+            if (kb + 16 * p + 4 * qd + e > (STEP ? seen - 1 : lim[b])) s[b][p][e] = -INFINITY;
     }
     bf16x8 pb[NB][NT];
 #pragma unroll
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   page_ids();
   load_tile(st[0]);
   load_tile(st[1]);
-  load_rows(first_row_of(si));
+  load_rows(si);
   bool odd = false, merged = false;
   for (; from < to; ++si) {
   const SeqDesc sd = a.seq[si];
@@ -275,8 +278,12 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   const int nsplit = share == 0 ? 1 : (end - 1) / share - begin / share + 1;
   const int j0 = from - begin, j1 = min(to, end) - begin;
   from = begin + j1;
-  const int L = sd.prefix + 1;
-  const int64_t first_row = first_row_of(si);
+  const int rows = min(NB * 16, (STEP ? G : sd.suffix * G) - r0);
+  if (!STEP && rows <= 0) {                               // chunks past this sequence's rows
+    if (from < to) load_rows(si + 1);
+    continue;
+  }
+  const int seen = sd.prefix + (STEP ? 0 : r0 / G) + 1;   // keys of the first row
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     m_ref[b] = -INFINITY, l_run[b] = 0.f;
@@ -285,19 +292,19 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   }
   int j = j0 + wave;
   if (odd && j < j1) {
-    tile(st[1], j * kTK, L);
+    tile(st[1], j * kTK, seen);
     j += kWaves;
     odd = false;
   }
   for (; j + kWaves < j1; j += 2 * kWaves) {
-    tile(st[0], j * kTK, L);
-    tile(st[1], (j + kWaves) * kTK, L);
+    tile(st[0], j * kTK, seen);
+    tile(st[1], (j + kWaves) * kTK, seen);
   }
   if (j < j1) {
-    tile(st[0], j * kTK, L);
+    tile(st[0], j * kTK, seen);
     odd = true;
   }
-  if (from < to) load_rows(first_row_of(si + 1));   // in flight during the merge
+  if (from < to) load_rows(si + 1);              // in flight during the merge
 
   // ---- merge the four waves.  Each parks its O rows in its own slot (its reads
   // of V precede these writes in LDS order), four columns a piece, the pieces of
@@ -318,7 +325,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
     }
   }
   __syncthreads();
-  for (int idx = tid; idx < heads * Q4; idx += kWaves * 64) {
+  for (int idx = tid; idx < rows * Q4; idx += kWaves * 64) {
     const int r = idx / Q4, q = idx - r * Q4;
     float mstar = -INFINITY;
 #pragma unroll
@@ -334,13 +341,15 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
       lsum += wt * ml[w][r][1];
       acc += wt * ring[w].rows()[r * Q4 + (q ^ (r & 15))];
     }
+    const unsigned t = STEP ? 0u : (unsigned)(r0 + r) / (unsigned)G;
+    const int local = (int)t * a.num_q_heads + g * G + (r0 + r - (int)t * G);   // row of the sequence
     if (nsplit == 1) {
-      const int64_t row = first_row + r;
+      const int64_t row = (int64_t)sd.row_off * a.num_q_heads + local;
       const float inv = 1.0f / lsum;
       store4(reinterpret_cast<T*>(a.out) + row * D + q * 4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
       if (a.lse != nullptr && q == 0) a.lse[row] = (mstar + __builtin_log2f(lsum)) * kLn2;
     } else {
-      const int64_t prow = a.part_row[si] + (int64_t)split * a.num_q_heads + g * G + head0 + r;
+      const int64_t prow = a.part_row[si] + (int64_t)split * sd.suffix * a.num_q_heads + local;
       *reinterpret_cast<f32x4*>(a.part_o + prow * D + q * 4) = acc;
       if (q == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = (f32x2){mstar, lsum};
     }
@@ -361,14 +370,14 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const MxJoinArgs a) {
   __shared__ float sums[WIDE ? GROUPS : 1];
   const int q = threadIdx.x % Q4, group = threadIdx.x / Q4;
   const int64_t at = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * GROUPS + group;
-  const bool live = at < (int64_t)a.nseq * a.num_q_heads;
-  const int64_t x = live ? at : 0;
-  const int si = (int)(x / a.num_q_heads), h = (int)(x - (int64_t)si * a.num_q_heads);
+  const bool live = at < a.row_begin[a.nseq];
+  const int x = live ? (int)at : 0;
+  const int si = find_seq(a.row_begin, a.nseq, x), h = x - a.row_begin[si];
   const int n = a.parts[si];
   const int64_t first = a.part_row[si] + h;
   const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
   const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + first * D) + q;
-  const int64_t step = a.num_q_heads;
+  const int64_t step = a.row_begin[si + 1] - a.row_begin[si];
   float mstar = -INFINITY;
   for (int s = q; s < n; s += Q4) mstar = fmaxf(mstar, ml[s * step][0]);
 #pragma unroll
@@ -408,7 +417,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const MxJoinArgs a) {
 
 template <typename T, int D>
 void launch_join_as(const MxJoinArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.nseq * a.num_q_heads, groups = 256 / (D / 4);
+  const int64_t rows = a.row_begin[a.nseq], groups = 256 / (D / 4);
   if (rows < 4096)
     hipLaunchKernelGGL((mx_join_kernel<T, D, true>), dim3((unsigned)rows), dim3(256), 0, stream, a);
   else
@@ -418,11 +427,16 @@ void launch_join_as(const MxJoinArgs& a, hipStream_t stream) {
 
 template <typename T, int D>
 void launch_as(const MxDecodeArgs& a, int grid, hipStream_t stream) {
-  const int per_chunk = (a.group + a.chunks - 1) / a.chunks;
-  if (per_chunk <= 16)
-    hipLaunchKernelGGL((mx_decode_kernel<T, D, 1>), dim3(grid), dim3(kWaves * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((mx_decode_kernel<T, D, 2>), dim3(grid), dim3(kWaves * 64), 0, stream, a);
+  int most = 0, longest = 0;
+  for (int i = 0; i < a.nseq; ++i) {
+    longest = a.seq[i].suffix > longest ? a.seq[i].suffix : longest;
+    most = a.seq[i].suffix * a.group > most ? a.seq[i].suffix * a.group : most;
+  }
+  const dim3 g(grid), b(kWaves * 64);
+  if (longest == 1 && most <= 16) hipLaunchKernelGGL((mx_decode_kernel<T, D, 1, true>), g, b, 0, stream, a);
+  else if (longest == 1) hipLaunchKernelGGL((mx_decode_kernel<T, D, 2, true>), g, b, 0, stream, a);
+  else if (most <= 16) hipLaunchKernelGGL((mx_decode_kernel<T, D, 1, false>), g, b, 0, stream, a);
+  else hipLaunchKernelGGL((mx_decode_kernel<T, D, 2, false>), g, b, 0, stream, a);
 }
 
 }  // namespace

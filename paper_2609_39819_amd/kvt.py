@@ -1009,7 +1009,7 @@ def evict(k_pool, v_pool, block_table, length: Sequence[int], keep: Sequence[int
     four = k_pool.dtype == torch.uint8
     pool = _mx_pool_args(k_pool, v_pool, torch.bfloat16) if four else _pool_args(k_pool, v_pool)
     entry = "kvt_mx_evict" if four else "kvt_evict"
-    length, keep = [int(x) for x in length], [int(x) for x in keep]
+    length, keep = list(map(int, length)), list(map(int, keep))
     if len(keep) != len(length) or not length:
         raise ValueError("keep must hold one count for each sequence")
     head, _ = _head(entry, pool, [x - 1 for x in length], None, block_table, checked)
@@ -1020,7 +1020,7 @@ def evict(k_pool, v_pool, block_table, length: Sequence[int], keep: Sequence[int
     _check_table(block_table, n, device, v_pool, to_table)
     _check_table(to_table, n, device)
     stride = _head_rows(weights, "weights", n, hkv, max(length), torch.float32, device)
-    width = max(1, max(min(a, b) for a, b in zip(length, keep)))
+    width = max(1, *map(min, length, keep))
     with _on_device(k_pool):
         if positions is None:
             cols = width if weights_out is None else weights_out.shape[-1]

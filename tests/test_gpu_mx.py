@@ -119,7 +119,11 @@ EXTENDS = [  # prefix, suffix, hq, hkv, d
     ([0], [1], 4, 1, 64), ([0], [17], 4, 1, 128), ([15, 16, 31, 0], [1, 2, 17, 33], 8, 2, 128),
     ([240], [16], 4, 1, 64), ([1000, 5, 64], [70, 3, 129], 6, 2, 128), ([700, 3000], [5, 40], 32, 8, 64),
     ([63], [1], 8, 8, 128), ([2047], [66], 12, 1, 128), ([0], [400], 8, 2, 64), ([5000], [3], 40, 1, 128),
-    ([9000], [65], 8, 2, 128)]
+    ([9000], [65], 8, 2, 128),
+    # up to 64 rows of a kv-head: chunks of 32, of which shorter sequences have fewer
+    ([1000, 20, 3000, 0, 77], [16, 1, 3, 9, 8], 8, 2, 128), ([20000, 100, 50], [4, 16, 1], 12, 3, 64),
+    ([300, 9000], [50, 64], 2, 2, 64), ([15000] + list(range(100)), [3] * 101, 8, 2, 64), ([0, 5], [64, 1], 3, 3, 128),
+    ([12000, 30], [2, 11], 5, 1, 128), ([500] + [5 * b % 70 for b in range(270)], [1 + b % 5 for b in range(271)], 6, 1, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
