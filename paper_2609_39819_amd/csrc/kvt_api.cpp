@@ -1320,7 +1320,7 @@ kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void*
         part_row += (int64_t)parts * rows;
       }
     }
-    if (tiles > INT32_MAX) return KVT_ERR_INVALID_ARG;
+    if (tiles > INT32_MAX / 2) return KVT_ERR_INVALID_ARG;   // (the kernel adds a share to a tile)
     a.tile_begin[n] = (int32_t)tiles;
     const int64_t slots = a.share > 0 ? (tiles + a.share - 1) / a.share : n;
     const int64_t grid = slots * pool->num_kv_heads * plan.chunks;
@@ -1456,7 +1456,9 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
       units += (len + keys - 1) / keys;
       once = once && (int64_t)seqs->suffix_len[b] * G <= kvt::weights_stage_rows(pool->dtype);
     }
-    a.tiles = once ? (int32_t)((units * pool->num_kv_heads + device_cus() - 1) / device_cus()) : 0;
+    // (the first sequence is the longest)
+    const int64_t longest = ((int64_t)a.seq[0].prefix + a.seq[0].suffix + keys - 1) / keys;
+    a.tiles = once ? (int32_t)std::min((units * pool->num_kv_heads + device_cus() - 1) / device_cus(), longest) : 0;
     // turn: wide workgroups in whole rounds of the CUs, and what a last, mostly
     // empty round would hold as narrow ones (a narrow one of 32 keys takes a third
     // of a wide one's time instead of an eighth: it loads as many rows)
@@ -1483,7 +1485,7 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
         units += wide;
         narrow += (len - wide * keys + 31) / 32;
       }
-      if ((units + narrow) * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
+      if ((units + narrow) * pool->num_kv_heads > INT32_MAX / 2) return KVT_ERR_INVALID_ARG;
     }
     a.unit_begin[n] = (int32_t)units;
     a.narrow_begin[n] = (int32_t)narrow;

@@ -21,7 +21,8 @@ using namespace dev;
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kSelBins = 2048, kSelCopies = 2;     // histograms: fewer waves on one counter
+constexpr int kSelBins = 2048, kSelCopies = 4;     // counters of a bin, side by side
+constexpr int kSelHeld = 640;                      // keys that a wave keeps in LDS (two workgroups fit a CU)
 
 // Unsigned keys in the order of the weights, between 0, for places past the
 // end, and kForced: -0 is 0, and a NaN, of either sign, comes after +infinity.
@@ -37,9 +38,10 @@ __device__ __forceinline__ unsigned order_key(float w) {
 // 10.4; 16 contexts of 8192..65536 positions, 8 kv-heads: 72 and 47.5).
 template <int BY>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
-  __shared__ unsigned hist[kSelCopies][kSelBins];
+  __shared__ u32x4 hist[kSelBins];                 // a lane in four counts in each component
   __shared__ unsigned pick[2];                     // bin, count above it
   __shared__ unsigned totals[2][kSelWaves];
+  __shared__ unsigned held[kSelWaves][kSelHeld];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % a.num_kv_heads, i = blockIdx.x / a.num_kv_heads;
@@ -68,13 +70,20 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
   // is 2 us; held in registers they spill); what takes time is the instructions for
   // each, so groups that compete as a whole skip the tests for the rest.
   auto each = [&](auto&& f) __attribute__((always_inline)) {
+    float next[BY];                                // the group after, in flight (past the end: the last weight)
+    auto load = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < BY; ++j) next[j] = w[min(from + (j0 + j) * 64, L - 1)];
+    };
+    load(0);
     for (int j0 = 0; j0 < steps; j0 += BY) {
       const int p0 = from + j0 * 64;
       const int g0 = __builtin_amdgcn_readfirstlane(p0 - lane), g1 = g0 + BY * 64;   // of the group
       if (g0 >= end) break;
-      float raw[BY];                               // loads without a branch between them: all in flight
+      float raw[BY];
 #pragma unroll
-      for (int j = 0; j < BY; ++j) raw[j] = w[min(p0 + j * 64, L - 1)];
+      for (int j = 0; j < BY; ++j) raw[j] = next[j];
+      load(j0 + BY);
       if (g0 >= lo && g1 <= hi && g1 <= end) {
 #pragma unroll
         for (int j = 0; j < BY; ++j) f(order_key(raw[j]), p0 + j * 64);
@@ -88,33 +97,55 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     }
   };
 
-  // ---- the n-th largest key: larger ones stay, and the first `even` equal to it
-  unsigned edge = 0, even = (unsigned)n;
-  for (int b = tid; b < kSelCopies * kSelBins; b += kSelThreads) (&hist[0][0])[b] = 0;
+  // ---- the n-th largest key: larger ones stay, and the first `even` equal to it.
+  // The second pass keeps the keys that agree with the first one's digit (`count`
+  // of this wave), and how many are above them (`sure`): what follows needs only
+  // those, or, where they do not fit, all of the wave's keys again.
+  unsigned edge = 0, even = (unsigned)n, sure = 0, count = 0;
+  unsigned* list = held[wave];
+  unsigned* mine = reinterpret_cast<unsigned*>(hist) + lane % kSelCopies;
+  auto again = [&](auto&& f) __attribute__((always_inline)) {
+    if (count > kSelHeld) {
+      each([&](unsigned u, int) __attribute__((always_inline)) { f(u); });
+    } else {
+      for (unsigned x = 0; x < count; x += 64) f(x + lane < count ? list[x + lane] : 0u);
+    }
+  };
+  for (int b = tid; b < kSelBins; b += kSelThreads) hist[b] = (u32x4){0u, 0u, 0u, 0u};
   __syncthreads();
   for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    unsigned* mine = hist[wave % kSelCopies];
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     if (pass == 0) {
       each([&](unsigned u, int) __attribute__((always_inline)) {
-        if (u != 0) atomicAdd(&mine[u >> 21], 1u);
+        if (u != 0) atomicAdd(&mine[(u >> 21) * kSelCopies], 1u);
+      });
+    } else if (pass == 1) {
+      const unsigned agreed = edge >> 21;
+      each([&](unsigned u, int) __attribute__((always_inline)) {
+        sure += __builtin_popcountll(__builtin_amdgcn_ballot_w64((u >> 21) > agreed));
+        const bool in = (u >> 21) == agreed;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(in);
+        if (all == 0) return;
+        const unsigned place =
+            __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, count));
+        if (in) {
+          atomicAdd(&mine[(u >> 10 & (kSelBins - 1)) * kSelCopies], 1u);
+          if (place < kSelHeld) list[place] = u;
+        }
+        count += __builtin_popcountll(all);
       });
     } else {
-      const int top = pass == 1 ? 21 : 10;
-      const unsigned agreed = edge >> top;
-      each([&](unsigned u, int) __attribute__((always_inline)) {
-        if ((u >> top) == agreed) atomicAdd(&mine[u >> shift & (bins - 1)], 1u);
+      again([&](unsigned u) __attribute__((always_inline)) {
+        if ((u >> 10) == edge >> 10) atomicAdd(&mine[(u & 1023) * kSelCopies], 1u);
       });
     }
     __syncthreads();
     // counts from the largest bin down; thread t holds bins 2047 - 2t and 2046 - 2t,
     // and clears them for the next pass
-    unsigned c0 = 0, c1 = 0;
-#pragma unroll
-    for (int x = 0; x < kSelCopies; ++x) {
-      c0 += hist[x][kSelBins - 1 - 2 * tid], c1 += hist[x][kSelBins - 2 - 2 * tid];
-      hist[x][kSelBins - 1 - 2 * tid] = hist[x][kSelBins - 2 - 2 * tid] = 0;
-    }
+    u32x4& h0 = hist[kSelBins - 1 - 2 * tid];
+    u32x4& h1 = hist[kSelBins - 2 - 2 * tid];
+    const unsigned c0 = h0[0] + h0[1] + h0[2] + h0[3], c1 = h1[0] + h1[1] + h1[2] + h1[3];
+    h0 = h1 = (u32x4){0u, 0u, 0u, 0u};
     unsigned upto = c0 + c1;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -133,8 +164,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
   }
 
   // ---- the places of what stays: what the waves before this one keep, then ballots
-  unsigned s = 0, e = 0;
-  each([&](unsigned u, int) __attribute__((always_inline)) {
+  unsigned s = count > kSelHeld ? 0 : sure, e = 0;
+  again([&](unsigned u) __attribute__((always_inline)) {
     s += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u > edge));
     e += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == edge));
   });
@@ -144,13 +175,13 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
   s = e = 0;
   for (int x = 0; x < wave; ++x) s += totals[0][x], e += totals[1][x];
   each([&](unsigned u, int p) __attribute__((always_inline)) {
-    const uint64_t sure = __builtin_amdgcn_ballot_w64(u > edge), equal = __builtin_amdgcn_ballot_w64(u == edge);
-    if ((sure | equal) == 0) return;
-    const unsigned sb = __builtin_amdgcn_mbcnt_hi((unsigned)(sure >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)sure, s));
+    const uint64_t above = __builtin_amdgcn_ballot_w64(u > edge), equal = __builtin_amdgcn_ballot_w64(u == edge);
+    if ((above | equal) == 0) return;
+    const unsigned sb = __builtin_amdgcn_mbcnt_hi((unsigned)(above >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)above, s));
     const unsigned eb =
         __builtin_amdgcn_mbcnt_hi((unsigned)(equal >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)equal, e));
     if (u > edge || (u == edge && eb < even)) out[sb + min(eb, even)] = p;
-    s += __builtin_popcountll(sure), e += __builtin_popcountll(equal);
+    s += __builtin_popcountll(above), e += __builtin_popcountll(equal);
   });
 }
 

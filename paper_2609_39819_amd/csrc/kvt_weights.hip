@@ -298,7 +298,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   const int wide_keys = (a.unit_begin[si + 1] - a.unit_begin[si]) * kWeightsWideKeys;   // where there are narrow ones
   const int start = narrow ? wide_keys + (at - a.narrow_begin[si]) * 32
                            : (at - a.unit_begin[si]) * kWeightsWideKeys * (ONCE ? a.tiles : 1);
-  const int stop = ONCE ? min(L, start + a.tiles * kWeightsWideKeys) : start + step;
+  const int stop = start + (ONCE ? min(L - start, a.tiles * kWeightsWideKeys) : step);
   const int nblk = (L + kBlock - 1) / kBlock;
   float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
 

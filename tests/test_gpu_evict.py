@@ -118,6 +118,15 @@ def test_a_long_context_of_equal_weights():
     c.check(0, 0)
 
 
+@pytest.mark.parametrize("keep", [2000, 9000, 30000])
+def test_a_long_context_whose_weights_are_dense_in_places(keep):
+    """40000 positions, of which a stretch has weights within 1 % of each other and a stretch equal ones."""
+    c = Cache([40000], [keep], 2, 64, "mx")
+    c.weights[0, 0, 5000:17000] = 0.75 + 0.007 * c.weights[0, 0, 5000:17000]
+    c.weights[0, 1, 20000:33333] = 0.75
+    c.check(4, 100)
+
+
 @pytest.mark.parametrize("n", [40, 5000])
 def test_weights_that_equal_each_other_and_odd_ones(n):
     """Ties at the border, zeros of both signs, negatives, infinities and NaN of both signs."""

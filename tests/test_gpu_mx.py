@@ -191,6 +191,25 @@ def test_a_token_that_is_no_number_reaches_the_rows_that_see_it_and_no_others(dt
         assert bool(bad[0, :4].all()) and not bool(bad[0, 4:].any()) and not bool(bad[1].any())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("suffix", [[2, 1], [7, 3], [12, 2]])
+def test_a_token_that_is_no_number_in_a_short_message(dtype, suffix):
+    """Few rows of a kv-head (8, 28 and 48): a reused token that every row sees, and a new one that later ones do."""
+    prefix, T = [5000, 70], sum(suffix)
+    for pos in (1234, 5000 + suffix[0] // 2):
+        c = Batch(prefix, suffix, 8, 2, 64, dtype, seed=pos)
+        want, bound, _, _ = c.attention()
+        mark(c, 0, pos, 1)
+        seen = torch.zeros((T, 8), dtype=torch.bool)
+        seen[max(0, pos - 5000):suffix[0], 4:] = True
+        for use in (True, False):
+            out, lse = kvt.mx_extend_attention(c.q, c.k_pool, c.v_pool, c.table, prefix, suffix, return_lse=True,
+                                               use_workspace=use)
+            assert torch.equal(out.isnan().all(-1).cpu(), seen) and torch.equal(out.isnan().any(-1).cpu(), seen)
+            assert torch.equal(lse.isnan().cpu(), seen)
+            within(out.cpu()[~seen], want[~seen], bound[~seen], "others")
+
+
 def test_every_score_alike_and_one_far_above():
     """Equal keys (all weights 1/n) and one key that takes all the weight, at the largest scale that bf16 queries
     reach with it; values stay what they stand for."""

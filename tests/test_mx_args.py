@@ -108,6 +108,18 @@ def test_workspaces():
 
 
 @no_gpu_only
+def test_batches_beyond_the_tile_counts_are_rejected():
+    """Tiles of 32 keys are counted in 32 bits, with room for a workgroup's share: 33 sequences of 2^30 - 1 are more."""
+    p = pool(nb=1 << 20)
+    many = dict(P=[2 ** 30 - 2] * 33, S=[1] * 33, max_blocks=1 << 26)
+    assert decode(p, seqs(**many)) == E and extend(p, seqs(**many)) == E
+    few = dict(P=[2 ** 30 - 10] * 33, S=[9] * 33, max_blocks=1 << 26)
+    assert extend(p, seqs(**few)) == E
+    for name in ("kvt_attention_weights", "kvt_mx_attention_weights"):
+        assert getattr(kvt.lib(), name)(ref(p), ref(seqs(**many)), FAKE_Q, 4, 0.125, LSE, WEIGHTS, 1 << 30, None) == E
+
+
+@no_gpu_only
 @pytest.mark.parametrize("name", ["kvt_mx_append_kv", "kvt_mx_read_kv"])
 def test_bad_rows_are_rejected(name):
     def call(p, s, k=rows(FAKE_Q), v=rows(FAKE_OUT)):
