@@ -1441,6 +1441,9 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     row_off[b + 1] = row_off[b] + seqs->suffix_len[b];
     most_rows = std::max(most_rows, (int64_t)seqs->suffix_len[b] * G);
   }
+  // up to the 32 rows that it takes, the step kernel streams the keys (8 new tokens,
+  // 32/8 heads of 128, 16 contexts of 8000: 60.6 us, by the turn kernel 67.5; over
+  // 4-bit pages 25.3 and 41.6; one of 32000 20.5 and 17.1)
   const bool step = most_rows <= 32;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
@@ -1448,7 +1451,10 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     a.nseq = n;
     int64_t units = 0, narrow = 0;
     const int keys = step ? kvt::kWeightsStepKeys : kvt::kWeightsWideKeys;
-    bool once = !step;   // turn: the rows of every sequence are one stage in LDS
+    // turn: the rows of every sequence are one stage, which stays in LDS while the
+    // keys stream (32/8 heads of 128: 16 new tokens over 32000 keys 18.6 us, 28.8 a
+    // tile at a time; 8 sequences adding 64 over 8000 each 53.3, 83.8)
+    bool once = !step;
     for (int i = 0; i < n; ++i) {
       const int b = order[c0 + i];
       const int64_t len = (int64_t)seqs->prefix_len[b] + seqs->suffix_len[b];
@@ -1460,15 +1466,24 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     const int64_t longest = ((int64_t)a.seq[0].prefix + a.seq[0].suffix + keys - 1) / keys;
     a.tiles = once ? (int32_t)std::min((units * pool->num_kv_heads + device_cus() - 1) / device_cus(), longest) : 0;
     // turn: wide workgroups in whole rounds of the CUs, and what a last, mostly
-    // empty round would hold as narrow ones (a narrow one of 32 keys takes a third
-    // of a wide one's time instead of an eighth: it loads as many rows)
+    // empty round would hold as narrow ones.  A narrow one has an eighth of the keys
+    // but loads as many rows, and a round of them takes 0.4 of a wide one's time:
+    // one round pays (32/8 heads, 512 new tokens over 8192: 54.4 us, 78.8 with wide
+    // ones only; fp32 214, 281), and two where bf16 rows are many (512 over 9216:
+    // 69.3, 78.8; 140, 560 rows: 33.3, 32.5; 70: 26.4, 22.6; fp32, 512: 126, 116).
     int64_t drop = 0;   // wide workgroups of each kv-head that become narrow ones
     if (!step && !once) {
       units = 0;
-      for (int i = 0; i < n; ++i) units += ((int64_t)a.seq[i].prefix + a.seq[i].suffix) / keys;
+      int64_t rest = 0;   // narrow ones in any case
+      for (int i = 0; i < n; ++i) {
+        const int64_t len = (int64_t)a.seq[i].prefix + a.seq[i].suffix;
+        units += len / keys;
+        rest += (len % keys + 31) / 32;
+      }
       const int64_t excess = units * pool->num_kv_heads % device_cus();
-      const int64_t thin = (excess * 8 + device_cus() - 1) / device_cus();   // rounds of narrow ones
-      if (thin < 3) drop = (excess + pool->num_kv_heads - 1) / pool->num_kv_heads;
+      const int64_t thin = (excess * 8 + rest * pool->num_kv_heads + device_cus() - 1) / device_cus();   // rounds of narrow ones
+      const bool many = pool->dtype == KVT_DTYPE_BF16 && most_rows > 4 * kvt::weights_stage_rows(pool->dtype);
+      if (thin < 2 || (thin == 2 && many)) drop = (excess + pool->num_kv_heads - 1) / pool->num_kv_heads;
     }
     units = 0;
     for (int i = 0; i < n; ++i) {
@@ -1491,7 +1506,11 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     a.narrow_begin[n] = (int32_t)narrow;
     hipError_t e;
     if (step) {
-      const int64_t slots = std::max<int64_t>(1, 4 * (int64_t)device_cus() / pool->num_kv_heads);   // four to a CU
+      // as many workgroups as run on a CU at once, in one round.  One context of
+      // 131000 and 48 of 1024..16384, 32/8 heads of 128, with 2, 3 and 4 on a CU: bf16
+      // 55.2, 55.6, 60.7 us and 121.7, 124.0, 126.2; 4-bit 21.8, 20.9, 21.8 and 46.8,
+      // 43.1, 42.8, with fp32 queries 23.8, 22.3, 26.0 (one); fp32 101, 104, 106
+      const int64_t slots = std::max<int64_t>(1, (mx ? 3 : 2) * (int64_t)device_cus() / pool->num_kv_heads);
       a.share = (int32_t)std::max<int64_t>(4, (units + slots - 1) / slots);
       e = kvt::launch_weights_step(a, format, pool->dtype, pool->head_dim,
                                    (int)((units + a.share - 1) / a.share) * pool->num_kv_heads, s);
