@@ -416,7 +416,7 @@ size_t kvt_diff_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seq
  * not overlap.
  */
 kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_new, const kvt_rows* v_new,
-                          void* stream);
+                            void* stream);
 
 /*
  * kvt_mx_read_kv -- the values that 4-bit pages hold at positions P_b .. P_b+S_b-1
@@ -425,7 +425,7 @@ kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kv
  * mirror of the table an id outside the pool gives unspecified values.
  */
 kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_out, const kvt_rows* v_out,
-                        void* stream);
+                          void* stream);
 
 /*
  * kvt_mx_extend_attention -- kvt_extend_attention over 4-bit pages.
@@ -443,9 +443,9 @@ kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_
  * 0).  Results are bit-reproducible for given arguments.
  */
 kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs,
-                                 const void* q, int32_t num_q_heads, float scale,
-                                 void* out, float* lse,
-                                 void* workspace, size_t workspace_bytes, void* stream);
+                                   const void* q, int32_t num_q_heads, float scale,
+                                   void* out, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
 size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
 
 /*
@@ -458,9 +458,9 @@ size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
  * KVT_ERR_INVALID_ARG; any workspace will do where that is 0).
  */
 kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
-                                 const void* q, int32_t num_q_heads, float scale,
-                                 void* out, float* lse,
-                                 void* workspace, size_t workspace_bytes, void* stream);
+                                   const void* q, int32_t num_q_heads, float scale,
+                                   void* out, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
 size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads);
 
 /*
@@ -479,15 +479,16 @@ size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
  * the longest sequence), 4-byte aligned, apart from q, lse and the pools; row b
  * belongs to sequence b, a forked sequence has a row of its own.  Scores keep
  * fp32's precision in every dtype (fp32 inputs are not rounded to bf16 here).
- * Each weight is summed in one fixed order: results are bit-reproducible.  A
- * non-finite key leaves its own weight unspecified, and no other.
+ * Each weight is summed in one fixed order: results are bit-reproducible.  A row
+ * whose lse is NaN makes every weight that it adds to NaN; a non-finite key by
+ * itself leaves its own weight unspecified, and no other.
  */
 kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
                                  const void* q, int32_t num_q_heads, float scale, const float* lse,
                                  float* weights, int64_t weights_stride, void* stream);
 kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
-                                  const void* q, int32_t num_q_heads, float scale, const float* lse,
-                                  float* weights, int64_t weights_stride, void* stream);
+                                    const void* q, int32_t num_q_heads, float scale, const float* lse,
+                                    float* weights, int64_t weights_stride, void* stream);
 
 /* What an eviction keeps, and where it goes. */
 typedef struct {

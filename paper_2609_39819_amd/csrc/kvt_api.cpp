@@ -1218,15 +1218,17 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     int64_t total = 0;
     for (int i = 0; i < n; ++i) total += mx_tiles(seqs, p.order[c0 + i]);
     const int64_t longest = mx_tiles(seqs, p.order[c0]);
-    // two workgroups to a CU, of at least 16 tiles (four for each wave)
+    // two workgroups to a CU, of at least 16 tiles (four for each wave).  One context
+    // of 131072 keys and 64 of 1024..16384, 96/8 heads of 128, with one, two and
+    // four: 41.0, 33.4 and 33.4 us, 107, 84 and 90
     const int64_t slots = std::max<int64_t>(1, 2 * device_cus() / heads);
     int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
     // a sequence lies in at most one slot more than its tiles fill
     share = std::max(share, (longest + kvt::kMaxPartials - 2) / (kvt::kMaxPartials - 1));
     // A slot for each sequence needs no join (a launch, the workspace: 6.5 us); a
-    // workgroup takes 0.18 us a tile, all of them 5.5 TB/s.  Calls of one context of
-    // 1000, 2000 and 3000 keys, 32/8 heads of 128: 11.1, 15.8 and 21.7 us so, 16.5
-    // in shares; 48 contexts of 1000, 4000 and 6000: 14.6, 43.6 and 63.0; 20.6,
+    // workgroup takes 0.18 us a tile, all of them 5.5 TB/s.  A step of one context
+    // of 1000, 2000 and 3000 keys, 32/8 heads of 128: 11.1, 15.8 and 21.7 us so, 16.5
+    // in shares; of 48 contexts of 1000, 4000 and 6000: 14.6, 43.6 and 63.0; 20.6,
     // 45.2 and 61.3.
     const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
     const double stream = (double)total * heads * tile_bytes / 5.5e6;
@@ -1334,7 +1336,7 @@ kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void*
 
 // Token rows of a 4-bit append or read; fills the launch arguments.
 kvt_status check_mx_rows(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k, const kvt_rows* v, bool writes,
-                       int64_t* T, kvt::MxRowsArgs* a) {
+                         int64_t* T, kvt::MxRowsArgs* a) {
   kvt_status st = check_pool(pool);
   if (st != KVT_OK) return st;
   if ((st = check_seqs(seqs, T)) != KVT_OK) return st;
@@ -2062,7 +2064,7 @@ kvt_status kvt_diff_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs,
 }
 
 kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_new, const kvt_rows* v_new,
-                          void* stream) try {
+                            void* stream) try {
   kvt::MxRowsArgs a;
   std::memset(&a, 0, sizeof(a));
   int64_t T = 0;
@@ -2075,7 +2077,7 @@ kvt_status kvt_mx_append_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kv
 }
 
 kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_rows* k_out, const kvt_rows* v_out,
-                        void* stream) try {
+                          void* stream) try {
   kvt::MxRowsArgs a;
   std::memset(&a, 0, sizeof(a));
   int64_t T = 0;
@@ -2097,8 +2099,8 @@ size_t kvt_mx_extend_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
 }
 
 kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
-                                 float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                                 void* stream) try {
+                                   float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                   void* stream) try {
   int64_t T = 0;
   const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
   if (st != KVT_OK) return st;
@@ -2124,8 +2126,8 @@ size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
 }
 
 kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
-                                 float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
-                                 void* stream) try {
+                                   float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                   void* stream) try {
   int64_t T = 0;
   const kvt_status st = check_extend(pool, seqs, q, num_q_heads, scale, out, lse, &T, true);
   if (st != KVT_OK) return st;
@@ -2144,8 +2146,8 @@ kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, con
 }
 
 kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
-                                  float scale, const float* lse, float* weights, int64_t weights_stride,
-                                  void* stream) try {
+                                    float scale, const float* lse, float* weights, int64_t weights_stride,
+                                    void* stream) try {
   return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, stream, true);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);

@@ -20,6 +20,12 @@
 //     product then keeps fp32's 24 bits (the 4-bit values are exact in bf16);
 //   * at the end the four waves' (m, l, O) merge through LDS into the output or
 //     a partial of the key split.
+//
+// Measured, bf16 queries: one context of 131072 keys, 96/8 heads of 128, 143 MB,
+// 33.4 us with the join (4.3 TB/s; the first tiles and the join's launch are
+// about 8 us of it), 64 contexts of 1024..16384 84 us (5.0 TB/s; a plain read of
+// 2 GiB 6.1).  Messages of 2, 8 and 16 tokens over 131000 keys, 32/8 heads: 33.2,
+// 50.8 and 67.6 us; by the extend kernel 93.7, 94.6 and 97.8.
 #include "kvt_mx_device.h"
 
 namespace kvt {

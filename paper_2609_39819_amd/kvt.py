@@ -814,7 +814,7 @@ def _mx_pool_args(k_pool, v_pool, dtype) -> tuple:
 
 
 def mx_append_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], k_new, v_new, *,
-               stream=None, checked: bool = False) -> None:
+                 stream=None, checked: bool = False) -> None:
     """The new tokens' K/V ([T][Hkv][D], bf16 or fp32, whose tokens may lie apart)
     into their 4-bit pages (``kvt_mx_append_kv``)."""
     if stream is not None:
@@ -833,7 +833,7 @@ def mx_append_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_
 
 
 def mx_read_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int], dtype, *, k_out=None,
-             v_out=None, stream=None, checked: bool = False):
+               v_out=None, stream=None, checked: bool = False):
     """The values that 4-bit pages hold at positions ``prefix_len[b]`` ..
     ``prefix_len[b] + suffix_len[b] - 1`` (``kvt_mx_read_kv``): (k, v), each
     [T][Hkv][D] of ``dtype``.  The tokens of ``k_out`` and ``v_out`` may lie apart."""
@@ -841,7 +841,7 @@ def mx_read_kv(k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_le
     if stream is not None:   # what is allocated here belongs to the stream that it is written on
         with _on_stream(stream, k_pool):
             return mx_read_kv(k_pool, v_pool, block_table, prefix_len, suffix_len, dtype, k_out=k_out, v_out=v_out,
-                            checked=checked)
+                              checked=checked)
     pool = _mx_pool_args(k_pool, v_pool, dtype)
     hkv, d, device = pool[3], pool[4], k_pool.get_device()
     head, T = _head("kvt_mx_read_kv", pool, prefix_len, suffix_len, block_table, checked)
@@ -868,12 +868,12 @@ def mx_extend_workspace_bytes(k_pool, v_pool, block_table, prefix_len, suffix_le
 
 
 def mx_extend_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Sequence[int],
-                      scale: Optional[float] = None, *, out=None, lse=None, return_lse: bool = False,
-                      workspace=None, use_workspace: bool = True, stream=None, checked: bool = False):
+                        scale: Optional[float] = None, *, out=None, lse=None, return_lse: bool = False,
+                        workspace=None, use_workspace: bool = True, stream=None, checked: bool = False):
     """``extend_attention`` over 4-bit pages (``kvt_mx_extend_attention``): ``q`` is
     bf16 or fp32, and so is the result.  Other arguments as there."""
     return _mx_attention("kvt_mx_extend_attention", "kvt_mx_extend_workspace_bytes", q, k_pool, v_pool, block_table,
-                       prefix_len, suffix_len, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
+                         prefix_len, suffix_len, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
 
 
 def mx_decode_workspace_bytes(k_pool, v_pool, block_table, prefix_len, num_q_heads: int, dtype) -> int:
@@ -883,22 +883,22 @@ def mx_decode_workspace_bytes(k_pool, v_pool, block_table, prefix_len, num_q_hea
 
 
 def mx_decode_attention(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], scale: Optional[float] = None, *,
-                      out=None, lse=None, return_lse: bool = False, workspace=None, use_workspace: bool = True,
-                      stream=None, checked: bool = False):
+                        out=None, lse=None, return_lse: bool = False, workspace=None, use_workspace: bool = True,
+                        stream=None, checked: bool = False):
     """``decode_attention`` over 4-bit pages (``kvt_mx_decode_attention``): row b of
     ``q`` ([B][Hq][D], bf16 or fp32) is the new token of sequence b at position
     ``prefix_len[b]``, whose K/V was appended first."""
     return _mx_attention("kvt_mx_decode_attention", "kvt_mx_decode_workspace_bytes", q, k_pool, v_pool, block_table,
-                       prefix_len, None, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
+                         prefix_len, None, scale, out, lse, return_lse, workspace, use_workspace, stream, checked)
 
 
 def _mx_attention(entry: str, ws_entry: str, q, k_pool, v_pool, block_table, prefix_len, suffix_len, scale, out, lse,
-                return_lse, workspace, use_workspace, stream, checked):
+                  return_lse, workspace, use_workspace, stream, checked):
     import torch
     if stream is not None:   # what is allocated here belongs to the stream that the kernels run on
         with _on_stream(stream, k_pool):
             return _mx_attention(entry, ws_entry, q, k_pool, v_pool, block_table, prefix_len, suffix_len, scale, out,
-                               lse, return_lse, workspace, use_workspace, None, checked)
+                                 lse, return_lse, workspace, use_workspace, None, checked)
     native = _native()
     pool = _mx_pool_args(k_pool, v_pool, q.dtype)
     head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
