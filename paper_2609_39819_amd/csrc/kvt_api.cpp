@@ -1444,8 +1444,8 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     most_rows = std::max(most_rows, (int64_t)seqs->suffix_len[b] * G);
   }
   // up to the 32 rows that it takes, the step kernel streams the keys (8 new tokens,
-  // 32/8 heads of 128, 16 contexts of 8000: 60.6 us, by the turn kernel 67.5; over
-  // 4-bit pages 25.3 and 41.6; one of 32000 20.5 and 17.1)
+  // 32/8 heads of 128, 16 contexts of 8000: 59.9 us, by the turn kernel 67.5; over
+  // 4-bit pages 23.2 and 41.6; one of 32000 20.0 and 17.1)
   const bool step = most_rows <= 32;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
@@ -1508,10 +1508,11 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     a.narrow_begin[n] = (int32_t)narrow;
     hipError_t e;
     if (step) {
-      // as many workgroups as run on a CU at once, in one round.  One context of
-      // 131000 and 48 of 1024..16384, 32/8 heads of 128, with 2, 3 and 4 on a CU: bf16
-      // 55.2, 55.6, 60.7 us and 121.7, 124.0, 126.2; 4-bit 21.8, 20.9, 21.8 and 46.8,
-      // 43.1, 42.8, with fp32 queries 23.8, 22.3, 26.0 (one); fp32 101, 104, 106
+      // Loads of two or three workgroups keep a CU busy, more end at different times.
+      // One context of 131000 and 48 of 1024..16384, 32/8 heads of 128, with 2, 3 and
+      // 4 on a CU: bf16 54.6, 54.9, 60.1 us and 119.0, 121.3, 124.3; 4-bit 19.9,
+      // 18.8, 20.0 and 40.0, 37.7, 38.6, with fp32 queries 22.2, 21.0, 21.8 (one);
+      // fp32 103, 106, 109
       const int64_t slots = std::max<int64_t>(1, (mx ? 3 : 2) * (int64_t)device_cus() / pool->num_kv_heads);
       a.share = (int32_t)std::max<int64_t>(4, (units + slots - 1) / slots);
       e = kvt::launch_weights_step(a, format, pool->dtype, pool->head_dim,

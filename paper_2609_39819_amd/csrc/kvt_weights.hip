@@ -11,10 +11,12 @@
 // Two kernels, by the rows that the largest sequence adds:
 //   * step (at most 32 rows, a decoding step): HBM-bound on K.  4 waves stream
 //     32-key tiles from HBM into their operands (no LDS), 16 or 32 rows by
-//     v_mfma_f32_16x16x32_bf16.  The batch's tiles lie one after the other and every
-//     workgroup takes an equal share, of as many sequences as lie there.  48
-//     contexts of 1024..16384 keys over 4-bit pages, 32/8 heads of 128: 43 us; one
-//     of 131000 over bf16 pages 55 us (5.0 TB/s);
+//     v_mfma_f32_16x16x32_bf16, whose result holds four rows' scores of a key in a
+//     lane: most of a key's sum is in the lane (with the keys' scores of a row in a
+//     lane instead, 48 contexts took 42.8 us).  The batch's tiles lie one after the
+//     other and every workgroup takes an equal share, of as many sequences as lie
+//     there.  48 contexts of 1024..16384 keys over 4-bit pages, 32/8 heads of 128:
+//     37.7 us; one of 131000 over bf16 pages 54.6 us (5.1 TB/s);
 //   * turn: bound by the products and the exponentials (16 cycles of a wave's vector
 //     unit for 64 of them, 8 more for a score's product and sum).  Every wave holds 32
 //     keys as operands in registers; the rows pass through LDS, 256 in bf16 or 64
@@ -33,14 +35,15 @@ using namespace dev;
 template <int FORMAT>
 constexpr int kKeyTerms = FORMAT == 1 ? 3 : 1;
 
-// s += K Q^T over the terms of both whose product counts
+// s += Q K^T (a lane has a key's scores of four rows), or K Q^T, over the terms of
+// both whose product counts
 template <int KN, int QN>
 __device__ __forceinline__ void products16(f32x4& s, const bf16x8 (&k)[KN], const bf16x8 (&q)[QN]) {
 #pragma unroll
   for (int i = 0; i < KN; ++i)
 #pragma unroll
     for (int j = 0; j < QN; ++j)
-      if (i + j < 3) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i], q[j], s, 0, 0, 0);
+      if (i + j < 3) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[j], k[i], s, 0, 0, 0);
 }
 template <int KN, int QN>
 __device__ __forceinline__ void products32(f32x16& s, const bf16x8 (&k)[KN], const bf16x8 (&q)[QN]) {
@@ -68,33 +71,22 @@ __device__ __forceinline__ float scatter_sum(float (&v)[N], int lane, int top) {
   return v[0];
 }
 
-// Sum over the 16 lanes of a row, in all of them.
-__device__ __forceinline__ float row_sum(float x) {
-  auto add = [](float v, auto ctrl) __attribute__((always_inline)) {
-    const int u = __builtin_bit_cast(int, v);
-    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  x = add(x, std::integral_constant<int, 0xb1>());    // lane ^ 1
-  x = add(x, std::integral_constant<int, 0x4e>());    // lane ^ 2
-  x = add(x, std::integral_constant<int, 0x141>());   // 7 - lane of 8
-  return add(x, std::integral_constant<int, 0x140>());   // 15 - lane of 16
-}
-
-// Four floats at any 4-byte aligned place.
-struct __attribute__((packed, aligned(4))) Four {
-  float x[4];
-};
-
 // Old weights are those of the reused positions; the new ones have none.
 __device__ __forceinline__ void put(float* w, int key, const SeqDesc& sd, float sum) {
   w[key] = key < sd.prefix ? w[key] + sum : sum;
 }
 
-template <typename T, int D, int FORMAT, int NB>
+// R: rows at most, 4, 8, 16 or 32.  A lane's four scores of a key are rows 4 qd ..
+// of 16 (twice with 32).  Up to 8 rows are there more than once, so that a lane
+// takes the exponentials of one of a tile's two pages only, and fewer lanes have
+// to add up a key's sum.
+template <typename T, int D, int FORMAT, int R>
 __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs a) {
   constexpr bool kCodes = FORMAT == kMx;
   constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
   constexpr int KS = D / 32;
+  constexpr int NB = R == 32 ? 2 : 1;
+  constexpr bool kOnePage = R <= 8;              // of a tile, for each lane: page `half`
   constexpr int kTK = 32;
   constexpr int kPieces = kCodes ? 1 : FORMAT == 0 ? KS : 2 * KS;   // 16-byte loads per page and lane
   constexpr int64_t kPage = kCodes ? mx_page_bytes(D) : (int64_t)kBlock * D * (FORMAT == 0 ? 2 : 4);
@@ -103,6 +95,9 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, qd = lane >> 4;
+  const int half = R == 8 ? qd >> 1 : qd & 1;    // the page whose weights this lane ends up with ...
+  const bool writes = R == 8 ? (qd & 1) == 0 : qd < 2;   // ... and puts into place, key l16 of it
+  const int mine = 16 * half + l16;
 
   const int hkv = a.num_kv_heads, G = a.group;
   const int g = blockIdx.x % hkv;
@@ -118,21 +113,31 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
   from = a.unit_begin[si] + j1;
   const int nt = j1 - j0 > wave ? (j1 - j0 - wave + 3) / 4 : 0;
 
-  // ---- this lane's query rows; rows past the last see nothing
+  // ---- the query rows: this lane's operand is row l16 (% R) of 16, its scores are
+  // those of rows 4 qd + e (% R).  A row past the last sees nothing.
   bf16x8 qreg[NB][KS][QN];
-  float lse2[NB];
-  int lim[NB];
+  float lse2[NB][4];
+  int lim[NB][4];
+  auto row_at = [&](int r, int& tok) __attribute__((always_inline)) {
+    r = min(r, rows - 1);
+    tok = r / G;
+    return (int64_t)(sd.row_off + tok) * a.num_q_heads + g * G + (r - tok * G);
+  };
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const int r = min(b * 16 + l16, rows - 1), t = r / G;
-    const int64_t row = (int64_t)(sd.row_off + t) * a.num_q_heads + g * G + (r - t * G);
-    const T* qp = reinterpret_cast<const T*>(a.q) + row * D;
+    int tok;
+    const T* qp = reinterpret_cast<const T*>(a.q) + row_at(b * 16 + l16 % min(R, 16), tok) * D;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) load_terms(qp + (kCodes ? qd * (D / 4) + kk * 8 : kk * 32 + qd * 8), qreg[b][kk]);
-    // a row past the last: 2^(s - infinity) = 0 (or NaN for a key that is one
-    // anyway)
-    lse2[b] = b * 16 + l16 < rows ? a.lse[row] * kLog2e : INFINITY;
-    lim[b] = P + t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = b * 16 + (4 * qd + e) % min(R, 16);
+      const float lse = a.lse[row_at(r, tok)];
+      // a row past the last: 2^(s - infinity) = 0 (or NaN for a key that is one
+      // anyway)
+      lse2[b][e] = r < rows ? lse * kLog2e : INFINITY;
+      lim[b][e] = P + tok;
+    }
   }
   float* w = a.weights + ((int64_t)sd.seq * hkv + g) * a.stride;
   const __attribute__((address_space(4))) int32_t* bt =
@@ -144,19 +149,17 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
       ids[p] = (uint32_t)bt[page];
     }
   };
-  // (and the old weights of keys 4 qd .. + 3 of each page, of which there are 4
-  // at least, or else any 16 readable bytes)
-  const float* old = P >= 4 ? w : reinterpret_cast<const float*>(a.q);
+  // (and the old weight of this lane's key, or else any 4 readable bytes)
+  const float* old = P >= 1 ? w : reinterpret_cast<const float*>(a.q);
   struct Stage {
     u32x4 k[2][kPieces];
     unsigned char scale[2];
-    Four old[2];
+    float old;
   };
   auto load_tile = [&](int j, const uint32_t (&ids)[2], Stage& st) __attribute__((always_inline)) {
+    st.old = old[max(0, min(j * kTK + mine, P - 1))];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      // (a tile that reaches past the old ones reads them when it stores)
-      st.old[p] = *reinterpret_cast<const Four*>(old + max(0, min(j * kTK + 16 * p + 4 * qd, P - 4)));
       const int page = min(j * 2 + p, nblk - 1);
       const int slot = min(l16, L - 1 - page * kBlock);
       const char* at = kpool + ((int64_t)min(ids[p], nb_max) * hkv + g) * kPage;
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
   const float c = a.scale_log2;
   auto tile = [&](Stage& st, int kb, auto&& next) __attribute__((always_inline)) {
     f32x4 s[NB][2];
-    const Four before[2] = {st.old[0], st.old[1]};
+    const float before = st.old;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
 #pragma unroll
@@ -200,36 +203,43 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
       }
     }
     next();
-    float sum[8];
-    if (kb + kTK <= P) {   // every row sees all of the tile, every key has an old weight
+    auto sum_of = [&](auto masked) __attribute__((always_inline)) {
+      auto p_of = [&](float x, int b, int e, int key) __attribute__((always_inline)) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, -lse2[b][e]));
+        return decltype(masked)::value && key > lim[b][e] ? 0.f : p;
+      };
+      if constexpr (kOnePage) {
+        float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum[e] = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          sum[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e >> 2][e & 3], c, -lse2[b]));
-        sum[e] = row_sum(sum[e]);
-      }
-      if (l16 == 0) {
+        for (int e = 0; e < 4; ++e) sum += p_of(half ? s[0][1][e] : s[0][0][e], 0, e, kb + mine);
+        if constexpr (R == 8) {                  // rows 0..3 here, 4..7 in lane l ^ 16
+          float x, y;
+          row_values(sum, x, y);
+          sum = x + y;
+        }
+        return sum;
+      } else {
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          *reinterpret_cast<Four*>(w + kb + 16 * p + 4 * qd) =
-              Four{{before[p].x[0] + sum[4 * p], before[p].x[1] + sum[4 * p + 1], before[p].x[2] + sum[4 * p + 2],
-                    before[p].x[3] + sum[4 * p + 3]}};
-      }
-      return;
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int key = kb + 16 * (e >> 2) + 4 * qd + (e & 3);
-      sum[e] = 0.f;
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e >> 2][e & 3], c, -lse2[b]));
-        sum[e] += key > lim[b] ? 0.f : p;
+            for (int e = 0; e < 4; ++e) sum[p] += p_of(s[b][p][e], b, e, kb + 16 * p + l16);
+        // lanes of even 16s keep page 0's and odd ones page 1's, of four rows here and four there
+        const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, sum[0]),
+                                                           __builtin_bit_cast(unsigned, sum[1]), false, false);
+        const unsigned x = both[0], y = both[1];
+        return pair_sum(__builtin_bit_cast(float, x) + __builtin_bit_cast(float, y));
       }
-      sum[e] = row_sum(sum[e]);
-      if (l16 == 0 && key < L) put(w, key, sd, sum[e]);
+    };
+    const int key = kb + mine;
+    if (kb + kTK <= P) {                         // every row sees all of the tile, every key has an old weight
+      const float sum = sum_of(std::false_type());
+      if (writes) w[key] = before + sum;
+    } else {
+      const float sum = sum_of(std::true_type());
+      if (writes && key < L) w[key] = key < P ? before + sum : sum;
     }
   };
 
@@ -521,8 +531,11 @@ template <typename T, int D, int FORMAT>
 void launch_step_as(const WeightsArgs& a, int grid, hipStream_t stream) {
   int rows = 0;
   for (int i = 0; i < a.nseq; ++i) rows = a.seq[i].suffix * a.group > rows ? a.seq[i].suffix * a.group : rows;
-  if (rows <= 16) hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 1>), dim3(grid), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 2>), dim3(grid), dim3(256), 0, stream, a);
+  const dim3 g(grid), b(256);
+  if (rows <= 4) hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 4>), g, b, 0, stream, a);
+  else if (rows <= 8) hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 8>), g, b, 0, stream, a);
+  else if (rows <= 16) hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 16>), g, b, 0, stream, a);
+  else hipLaunchKernelGGL((weights_step_kernel<T, D, FORMAT, 32>), g, b, 0, stream, a);
 }
 template <typename T, int D, int FORMAT>
 void launch_turn_as(const WeightsArgs& a, int grid, hipStream_t stream) {

@@ -33,7 +33,11 @@ CALLS = [  # prefix, suffix, hq, hkv, d
     ([0], [1], 4, 1, 64), ([0, 1, 15, 16, 31, 32, 100], [1] * 7, 8, 2, 128), ([3000, 5], [1, 1], 32, 8, 64),
     ([700], [1], 32, 1, 128), ([700, 80], [1, 1], 40, 1, 64), ([50, 0, 333], [2, 5, 8], 8, 2, 128),
     ([0], [33], 4, 1, 64), ([240], [16], 12, 1, 128), ([1000, 3, 64], [70, 129, 1], 6, 2, 128), ([2500], [300], 8, 8, 64),
-    ([0, 17], [500, 64], 8, 2, 128), ([63], [97], 24, 2, 64)]
+    ([0, 17], [500, 64], 8, 2, 128), ([63], [97], 24, 2, 64),
+    # up to 4, 8, 16 and 32 rows of a kv-head, sequences of fewer among them
+    ([1000, 33, 0], [2, 1, 2], 8, 2, 128), ([500, 64], [1, 1], 7, 1, 64), ([129, 3, 40], [3, 1, 2], 5, 1, 64),
+    ([5000, 30, 200, 1], [1] * 4, 16, 1, 128), ([9000], [1], 4, 4, 64), ([40, 8000], [4, 2], 6, 3, 128),
+    ([2000, 31], [3, 7], 4, 1, 64)]
 
 
 @pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "mx"), ("f32", "mx")])
