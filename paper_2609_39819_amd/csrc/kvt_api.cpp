@@ -1224,17 +1224,22 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     const int64_t slots = std::max<int64_t>(1, 2 * device_cus() / heads);
     int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
     // a sequence lies in at most one slot more than its tiles fill
-    share = std::max(share, (longest + kvt::kMaxPartials - 2) / (kvt::kMaxPartials - 1));
-    // A slot for each sequence needs no join (a launch, the workspace: 6.5 us); a
-    // workgroup takes 0.18 us a tile, all of them 5.5 TB/s.  A step of one context
-    // of 1000, 2000 and 3000 keys, 32/8 heads of 128: 11.1, 15.8 and 21.7 us so, 16.5
-    // in shares; of 48 contexts of 1000, 4000 and 6000: 14.6, 43.6 and 63.0; 20.6,
-    // 45.2 and 61.3.
+    share = std::max(share, (longest + kvt::kMxMaxParts - 2) / (kvt::kMxMaxParts - 1));
+    // A slot for each sequence needs no join (a launch, the workspace: 6.5 us) and no
+    // merge where a share goes on to the next sequence (1.5 us).  A workgroup takes
+    // 0.18 us a tile, 0.30 while another one runs on its CU; all of them read 5.5
+    // TB/s, one to a CU 4.3; and the shortest sequence starts last.  Steps of 32/8
+    // heads of 128 so and in shares: one context of 1000, 2000 and 3000 keys 11.1,
+    // 15.8 and 21.7 us, 16.5; 200 of 500..3000 62.9, 74.0 (16/2 heads 25.6, 31.5); 256
+    // of 100..600 28.2, 38.8; 100 of 1024..16384 131.8, 121.7; 70 of 6000 109.1, 87.5
+    // (4/4 heads 60.3, 47.3).
     const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
     const double stream = (double)total * heads * tile_bytes / 5.5e6;
-    const int64_t rounds = (n + slots - 1) / slots;
-    const double alone = std::max(rounds * 0.18 * longest + (rounds - 1) * 3.0, stream);
-    if (alone <= 6.5 + std::max(0.18 * share, stream)) share = total;
+    const int64_t first = device_cus() / heads;   // sequences that have a CU of their own
+    const double beside = n > slots ? longest : n > first ? mx_tiles(seqs, p.order[c0 + first]) : 0;
+    const double last = n > slots ? mx_tiles(seqs, p.order[c0 + n - 1]) : 0;
+    const double alone = std::max(0.18 * longest + 0.12 * beside, stream * (n > first ? 1.0 : 5.5 / 4.3) + 0.18 * last);
+    if (alone <= 6.5 + std::max(0.18 * share, stream) + 1.5 * n * share / total) share = total;
     bool split = false;
     int64_t begin = 0;
     for (int i = 0; i < n; ++i) {

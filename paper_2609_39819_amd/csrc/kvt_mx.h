@@ -59,6 +59,7 @@ struct MxDecodeArgs {
   SeqDesc seq[kSeqsPerLaunch];
 };
 constexpr int kMxChunkRows = 32;   // rows of a workgroup at most
+constexpr int kMxMaxParts = 255;   // slots that hold a part of one sequence at most
 // Rows of a kv-head up to which an extend call counts as one of few.  32/8 heads of
 // 128, by the chunks of the decode kernel and by the extend kernel: 64 rows over 4000
 // keys 17.9 and 17.7 us, over 131000 67.6 and 97.8; 128 rows 19.6 and 23.1, 112.7

@@ -123,7 +123,7 @@ EXTENDS = [  # prefix, suffix, hq, hkv, d
     # up to 64 rows of a kv-head: chunks of 32, of which shorter sequences have fewer
     ([1000, 20, 3000, 0, 77], [16, 1, 3, 9, 8], 8, 2, 128), ([20000, 100, 50], [4, 16, 1], 12, 3, 64),
     ([300, 9000], [50, 64], 2, 2, 64), ([15000] + list(range(100)), [3] * 101, 8, 2, 64), ([0, 5], [64, 1], 3, 3, 128),
-    ([12000, 30], [2, 11], 5, 1, 128), ([500] + [5 * b % 70 for b in range(270)], [1 + b % 5 for b in range(271)], 6, 1, 64)]
+    ([12000, 30], [2, 11], 5, 1, 128), ([150000], [5], 4, 1, 64), ([500] + [5 * b % 70 for b in range(270)], [1 + b % 5 for b in range(271)], 6, 1, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -146,7 +146,9 @@ DECODES = [  # prefix, hq, hkv, d
     ([6000, 100, 100, 3000], 24, 2, 128),
     # shares that hold parts of one context and many whole short ones, and a second launch without long ones
     ([20000] + list(range(130)), 8, 2, 128), ([9000, 7000, 33] + [30, 31, 63, 64, 95, 96, 127] * 8, 4, 1, 64),
-    ([12000] + [7 * b % 90 for b in range(299)], 24, 1, 64), ([30000, 2999, 0, 1] * 3, 16, 2, 128)]
+    ([12000] + [7 * b % 90 for b in range(299)], 24, 1, 64), ([30000, 2999, 0, 1] * 3, 16, 2, 128),
+    # one context in as many shares as a join takes, fewer and more rows
+    ([150000], 4, 1, 64), ([140000, 20], 33, 1, 64), ([100000], 2, 2, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

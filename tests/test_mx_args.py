@@ -96,6 +96,9 @@ def test_workspaces():
     for inside in (FAKE_Q, FAKE_OUT, LSE, FAKE_K, FAKE_V):
         assert decode(p, seqs(**long), hq=32, ws=inside, ws_bytes=bytes_) == E
     assert need("kvt_mx_decode_workspace_bytes", p, seqs(P=(100,), S=(1,)), 32) == 0
+    deep = dict(P=(2 ** 30 - 2,), S=(1,), max_blocks=1 << 26)          # at most 255 partial results of each row
+    most = need("kvt_mx_decode_workspace_bytes", pool(nb=1 << 20, hkv=1, d=128), seqs(**deep), 32)
+    assert 0 < most <= 255 * 32 * (128 + 2) * 4 + 256
     assert need("kvt_mx_decode_workspace_bytes", p, seqs(P=(100,), S=(2,)), 32) == 0
     assert need("kvt_mx_decode_workspace_bytes", pool(d=96), seqs(**long), 32) == 0
     turn = dict(P=(60000,), S=(16,), max_blocks=4000)
