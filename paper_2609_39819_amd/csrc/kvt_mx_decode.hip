@@ -22,10 +22,12 @@
 //     a partial of the key split.
 //
 // Measured, bf16 queries: one context of 131072 keys, 96/8 heads of 128, 143 MB,
-// 33.4 us with the join (4.3 TB/s; the first tiles and the join's launch are
-// about 8 us of it), 64 contexts of 1024..16384 84 us (5.0 TB/s; a plain read of
-// 2 GiB 6.1).  Messages of 2, 8 and 16 tokens over 131000 keys, 32/8 heads: 33.2,
-// 50.8 and 67.6 us; by the extend kernel 93.7, 94.6 and 97.8.
+// 32.7 us with the join (4.4 TB/s; the first tiles and the join's launch are
+// about 8 us of it), 64 contexts of 1024..16384 83 us (5.1 TB/s; a plain read of
+// 2 GiB 6.1; this kernel's loads alone 78.6), heads of 64 57 us (3.7 TB/s, its loads
+// alone 52: pages of half the bytes in as many places).  Messages of 2, 8 and 16
+// tokens over 131000 keys, 32/8 heads: 33.0, 50.4 and 67.4 us; by the extend kernel
+// 93.7, 94.6 and 97.8.
 #include "kvt_mx_device.h"
 
 namespace kvt {
@@ -77,11 +79,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 4 && D == 128 && NB == 2 
   // token r / G, head g * G + r % G)
   const int hkv = a.num_kv_heads;
   const int G = a.group;
-  const int chunks = a.chunks;
-  const int g = blockIdx.x % hkv;
-  const int rest = blockIdx.x / hkv;
-  const int unit = chunks == 1 ? rest : rest / chunks;
-  const int r0 = (rest - unit * chunks) * NB * 16;   // this workgroup's rows of a sequence start here
+  const int heads = hkv * a.chunks;
+  const Place8 at8 = place_of(blockIdx.x, gridDim.x, heads);
+  const int unit = at8.unit;
+  const int g = at8.head % hkv;
+  const int r0 = at8.head / hkv * NB * 16;       // this workgroup's rows of a sequence start here
   const int share = a.share;
   const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const char* vpool = reinterpret_cast<const char*>(a.v_pool);

@@ -26,6 +26,21 @@ __device__ __forceinline__ bf16x8 mx_values(unsigned codes, float scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// Unit and head of workgroup b of n = units * heads.  Workgroups go to the 8 XCDs
+// in turn: all heads of a unit to one, 8 units at a time, so that its L2 holds the
+// pages of a unit's tokens, where neighbouring records share lines (64 contexts of
+// 1024..16384 keys, 8 kv-heads of 128: 445 -> 421 MB read, of 64 248 -> 209, and
+// 84.9 -> 83.0 us, 58.8 -> 57.2).
+struct Place8 {
+  int unit, head;
+};
+__device__ __forceinline__ Place8 place_of(int b, int n, int heads) {
+  const int group = b / (8 * heads), first = group * 8 * heads;
+  const int width = min(8, (n - first) / heads);
+  const int in = b - first;
+  return {group * 8 + in % width, in / width};
+}
+
 // Terms of an element of T as bf16 numbers: bf16 is one, an fp32 number the sum
 // of three (8 + 8 + 8 significant bits; the rest is under 2^-24 of it, and
 // under 2^-133 where the terms reach the end of bf16's range).

@@ -16,7 +16,7 @@
 //     lane instead, 48 contexts took 42.8 us).  The batch's tiles lie one after the
 //     other and every workgroup takes an equal share, of as many sequences as lie
 //     there.  48 contexts of 1024..16384 keys over 4-bit pages, 32/8 heads of 128:
-//     37.7 us; one of 131000 over bf16 pages 54.6 us (5.1 TB/s);
+//     37.2 us; one of 131000 over bf16 pages 54.6 us (5.1 TB/s);
 //   * turn: bound by the products and the exponentials (16 cycles of a wave's vector
 //     unit for 64 of them, 8 more for a score's product and sum).  Every wave holds 32
 //     keys as operands in registers; the rows pass through LDS, 256 in bf16 or 64
@@ -100,10 +100,14 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
   const int mine = 16 * half + l16;
 
   const int hkv = a.num_kv_heads, G = a.group;
-  const int g = blockIdx.x % hkv;
+  // neighbouring records of 4-bit pages share lines: one XCD for all heads of a share
+  // (37.7 -> 37.2 us; bf16 pages 54.6 -> 55.7, there a kv-head has an XCD)
+  const Place8 at8 = kCodes ? place_of(blockIdx.x, gridDim.x, hkv)
+                            : Place8{(int)(blockIdx.x / hkv), (int)(blockIdx.x % hkv)};
+  const int g = at8.head;
   const char* kpool = reinterpret_cast<const char*>(a.k_pool);
   const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
-  int from = blockIdx.x / hkv * a.share;
+  int from = at8.unit * a.share;
   const int to = min(from + a.share, a.unit_begin[a.nseq]);
   for (int si = find_seq(a.unit_begin, a.nseq, from); from < to; ++si) {   // the sequences of this slot
   const SeqDesc sd = a.seq[si];
