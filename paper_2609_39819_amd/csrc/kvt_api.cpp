@@ -1615,8 +1615,12 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
     a.unit_begin[n] = (int32_t)pages;
     hipError_t e = kvt::launch_evict_select(a, s);
     if (e != hipSuccess) return device_error(e);
-    e = kvt::launch_evict_move(a, mx ? kvt::kMx : pool->dtype, pool->head_dim, (int)(pages * pool->num_kv_heads), s);
-    if (e != hipSuccess) return device_error(e);
+    constexpr int32_t kMost = 1 << 23;   // a launch holds less than 2^32 threads
+    const int32_t blocks = (int32_t)(pages * pool->num_kv_heads);
+    for (a.first_block = 0; a.first_block < blocks; a.first_block += std::min(kMost, blocks - a.first_block)) {
+      e = kvt::launch_evict_move(a, mx ? kvt::kMx : pool->dtype, pool->head_dim, std::min(kMost, blocks - a.first_block), s);
+      if (e != hipSuccess) return device_error(e);
+    }
   }
   return KVT_OK;
 }

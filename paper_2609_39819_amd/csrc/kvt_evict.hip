@@ -196,8 +196,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a) {
   constexpr int kPieces = ROW / 16;
   constexpr int64_t kPage = kBlock * (ROW + SCALE);
   const int hkv = a.num_kv_heads;
-  const int g = blockIdx.x % hkv;
-  const int unit = blockIdx.x / hkv;
+  const int block = (int)blockIdx.x + a.first_block;
+  const int g = block % hkv;
+  const int unit = block / hkv;
   const int si = find_seq(a.unit_begin, a.nseq, unit);
   const EvictDesc sd = a.seq[si];
   const int page = unit - a.unit_begin[si];
@@ -250,8 +251,8 @@ hipError_t launch_evict_select(const EvictArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int grid, hipStream_t stream) {
-  const dim3 g(grid), b(256);
+hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int blocks, hipStream_t stream) {
+  const dim3 g(blocks), b(256);
   const bool wide = head_dim == 128;
   if (format == 0 && wide) hipLaunchKernelGGL((evict_move_kernel<256, 0>), g, b, 0, stream, a);
   else if (format == 0) hipLaunchKernelGGL((evict_move_kernel<128, 0>), g, b, 0, stream, a);

@@ -124,6 +124,7 @@ struct EvictArgs {
   int32_t sinks;
   int32_t recent;
   int32_t nseq;
+  int32_t first_block;      // move kernel: of this launch
   int32_t unit_begin[kSeqsPerLaunch + 1];   // move kernel: prefix sums of the sequences' target pages
   EvictDesc seq[kSeqsPerLaunch];
 };
@@ -144,6 +145,6 @@ constexpr int kWeightsStepKeys = 32;      // step kernel: keys of one tile
 constexpr int kWeightsWideKeys = 256;     // turn kernel: keys of a wide workgroup's tile (a narrow one's: 32)
 constexpr int weights_stage_rows(int dtype) { return dtype == 0 ? 256 : 64; }   // turn kernel: rows in LDS at a time
 hipError_t launch_evict_select(const EvictArgs& a, hipStream_t stream);
-hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int grid, hipStream_t stream);
+hipError_t launch_evict_move(const EvictArgs& a, int format, int head_dim, int blocks, hipStream_t stream);
 
 }  // namespace kvt

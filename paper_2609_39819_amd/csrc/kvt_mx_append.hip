@@ -11,8 +11,10 @@
 // Both kernels are HBM-bound scatters: a lane takes 8 columns of K and of V (a
 // group is four lanes, whose maximum meets through cross-lane moves), so a
 // row's 16 lanes (D = 128) read 256 contiguous bytes and write 64.  14336 tokens
-// of 8 kv-heads of 128, bf16, 74 MB: written in 19.8 us (3.8 TB/s), read back in
-// 16.1 (4.6; a copy of 2 GiB reaches 4.9).  256 single tokens: 3.3 us each, a launch.
+// of 8 kv-heads of 128, bf16, 74 MB: written in 18.5 us (4.0 TB/s), read back in
+// 13.5 (5.5; a copy of 2 GiB reaches 4.9).  With a workgroup's lanes along the heads
+// of two tokens instead, the lines of a page's scales went to several XCDs: 19.8
+// and 16.1 us, 35 MB read for 16.  256 single tokens: 3.5 us each, a launch.
 #include "kvt_mx_device.h"
 
 namespace kvt {
@@ -32,28 +34,35 @@ __device__ __forceinline__ int owner(const MxRowsArgs& a, int32_t row) {
   return lo;
 }
 
-// One lane's piece: token row, kv-head and first column of 8, and its page.
+// One lane's piece: token row, kv-head and first column of 8, and its page.  A
+// workgroup takes consecutive rows of one kv-head, 16 (D = 128) or 32, so that a
+// page's lines, its scales' above all, are used at once.
 struct Piece {
   int32_t row, g, c, slot;
   int64_t page;   // -1: an id outside the pool
 };
 template <int D>
-__device__ __forceinline__ Piece piece_of(const MxRowsArgs& a, int64_t idx) {
-  constexpr int kLanes = D / 8;
-  const int32_t per_row = a.num_kv_heads * kLanes;
-  const int32_t r = (int32_t)(idx / per_row);
-  const int32_t rem = (int32_t)(idx - (int64_t)r * per_row);
-  Piece p;
+constexpr int kRows = 256 / (D / 8);
+template <int D>
+__device__ __forceinline__ bool piece_of(const MxRowsArgs& a, int32_t unit, Piece& p) {
+  const int32_t r = unit / a.num_kv_heads * kRows<D> + (int32_t)threadIdx.x / (D / 8);
+  if (r >= a.rows) return false;   // a row's lanes are in or out together
   p.row = a.row_begin + r;
-  p.g = rem / kLanes;
-  p.c = rem % kLanes;
+  p.g = unit % a.num_kv_heads;
+  p.c = threadIdx.x % (D / 8);
   const SeqDesc sd = a.seq[owner(a, p.row)];
   const int32_t pos = sd.prefix + (p.row - sd.row_off);
   const int32_t id = a.block_table[(int64_t)sd.seq * a.max_blocks + pos / kBlock];
   p.page = id < 0 || (int64_t)id >= a.num_blocks ? -1 : id;
   p.slot = pos % kBlock;
-  return p;
+  return true;
 }
+
+template <int D>
+__host__ __device__ int64_t units_of(const MxRowsArgs& a) {
+  return (int64_t)((a.rows + kRows<D> - 1) / kRows<D>) * a.num_kv_heads;
+}
+constexpr int64_t kMostBlocks = 1 << 20;
 
 struct Eight {
   float x[8];
@@ -98,12 +107,9 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void mx_append_kernel(const MxRowsArgs a) {
   constexpr int kLanes = D / 8;
   constexpr int64_t kPage = mx_page_bytes(D);
-  const int64_t total = (int64_t)a.rows * a.num_kv_heads * kLanes;
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  // whole waves take part (total is a multiple of the row's lanes, whole rows
-  // of lanes are in or out)
-  for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += stride) {
-    const Piece p = piece_of<D>(a, idx);
+  for (int64_t unit = blockIdx.x; unit < units_of<D>(a); unit += gridDim.x) {
+    Piece p;
+    if (!piece_of<D>(a, (int32_t)unit, p)) continue;
     const int64_t col = (int64_t)p.g * D + p.c * 8;
     const Eight k = load_eight(reinterpret_cast<const T*>(a.k) + p.row * a.k_stride + col);
     const Eight v = load_eight(reinterpret_cast<const T*>(a.v) + p.row * a.v_stride + col);
@@ -146,10 +152,9 @@ __device__ __forceinline__ void store_eight(float* p, bf16x8 x) {
 template <typename T, int D>
 __global__ __launch_bounds__(256) void mx_read_kernel(const MxRowsArgs a) {
   constexpr int64_t kPage = mx_page_bytes(D);
-  const int64_t total = (int64_t)a.rows * a.num_kv_heads * (D / 8);
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x; idx < total; idx += stride) {
-    const Piece p = piece_of<D>(a, idx);
+  for (int64_t unit = blockIdx.x; unit < units_of<D>(a); unit += gridDim.x) {
+    Piece p;
+    if (!piece_of<D>(a, (int32_t)unit, p)) continue;
     const int64_t page = p.page < 0 ? a.num_blocks - 1 : p.page;
     const int64_t at = (page * a.num_kv_heads + p.g) * kPage;
     const char* kp = reinterpret_cast<const char*>(a.k_pool) + at;
@@ -164,9 +169,8 @@ __global__ __launch_bounds__(256) void mx_read_kernel(const MxRowsArgs a) {
 }
 
 unsigned blocks_for(const MxRowsArgs& a, int head_dim) {
-  const int64_t lanes = (int64_t)a.rows * a.num_kv_heads * (head_dim / 8);
-  const int64_t blocks = (lanes + 255) / 256;
-  return (unsigned)(blocks > 16384 ? 16384 : blocks);   // grid-stride beyond
+  const int64_t units = head_dim == 128 ? units_of<128>(a) : units_of<64>(a);
+  return (unsigned)(units > kMostBlocks ? kMostBlocks : units);   // grid-stride beyond
 }
 
 }  // namespace
