@@ -1475,9 +1475,9 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
     // turn: wide workgroups in whole rounds of the CUs, and what a last, mostly
     // empty round would hold as narrow ones.  A narrow one has an eighth of the keys
     // but loads as many rows, and a round of them takes 0.4 of a wide one's time:
-    // one round pays (32/8 heads, 512 new tokens over 8192: 54.4 us, 78.8 with wide
-    // ones only; fp32 214, 281), and two where bf16 rows are many (512 over 9216:
-    // 69.3, 78.8; 140, 560 rows: 33.3, 32.5; 70: 26.4, 22.6; fp32, 512: 126, 116).
+    // one round pays (32/8 heads of 128, 512 new tokens over 8192: 54.4 us, 78.8 with
+    // wide ones only; fp32 192, 281), and two where the rows are many (512 over 9216:
+    // 69.3, 78.8, fp32 229, 281; 140, 560 rows: 33.3, 32.5; 70: 26.4, 22.6).
     int64_t drop = 0;   // wide workgroups of each kv-head that become narrow ones
     if (!step && !once) {
       units = 0;
@@ -1489,7 +1489,7 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
       }
       const int64_t excess = units * pool->num_kv_heads % device_cus();
       const int64_t thin = (excess * 8 + rest * pool->num_kv_heads + device_cus() - 1) / device_cus();   // rounds of narrow ones
-      const bool many = pool->dtype == KVT_DTYPE_BF16 && most_rows > 4 * kvt::weights_stage_rows(pool->dtype);
+      const bool many = most_rows > (pool->dtype == KVT_DTYPE_BF16 ? 1024 : 768);
       if (thin < 2 || (thin == 2 && many)) drop = (excess + pool->num_kv_heads - 1) / pool->num_kv_heads;
     }
     units = 0;

@@ -290,6 +290,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
   constexpr int KSTEPS = D / 16, CHUNKS = D / 8;
   constexpr int ROWS = kTurnRows<T>, BLOCKS = ROWS / 32;
+  static_assert(QN == 3 || BLOCKS == 8, "a narrow workgroup's waves have a block each");
   constexpr int64_t kPage = kCodes ? mx_page_bytes(D) : (int64_t)kBlock * D * (FORMAT == 0 ? 2 : 4);
   constexpr int PIECES = ROWS * CHUNKS / 512;    // of 8 columns, per thread and stage
   extern __shared__ __attribute__((aligned(1024))) char turn_lds[];
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   const int hh = lane >> 5, l32 = lane & 31;
 
   // ---- a wide workgroup has 32 keys per wave and every wave takes all rows, a
-  // narrow one has 32 keys and its waves take the row blocks in turn.  ONCE: the
+  // narrow one has 32 keys and its waves take the blocks of 32 rows in turn.  ONCE: the
   // rows of every sequence are one stage, which stays in LDS, and a workgroup (all
   // are wide) goes through a.tiles tiles of keys, the next one's in flight.
   const int hkv = a.num_kv_heads, G = a.group;
@@ -358,6 +359,58 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   };
   int kb = start + (narrow ? 0 : wave * 32);
   uint32_t id = page_of(kb);
+
+  const float c = a.scale_log2;
+  const int k32 = 8 * (l32 >> 3) + 4 * hh + (l32 >> 1 & 3);   // the key whose sum ends in this lane
+  // the waves' sums of the keys from kb on, as scatter_sum leaves them
+  auto join_waves = [&](float sum) __attribute__((always_inline)) {
+    float* red = reinterpret_cast<float*>(turn_lds);   // the rows are done with
+    __syncthreads();
+    if ((lane & 1) == 0) red[wave * 32 + k32] = sum;
+    __syncthreads();
+    if (tid < 32 && kb + tid < L) {
+      sum = 0.f;
+      for (int x = 0; x < 8; ++x) sum += red[x * 32 + tid];
+      put(w, kb + tid, sd, sum);
+    }
+  };
+  if constexpr (!ONCE && QN == 3) {
+    // a narrow workgroup's fp32 rows, each used once, go straight into operands: a
+    // stage holds blocks for two of the waves only (512 new tokens over 8192, 32/8
+    // heads of 128: 214 us by stages, 192 so, of 64 over 4-bit pages 91 and 59; bf16
+    // rows, whose stages hold eight blocks, 54.5 and 61)
+    if (narrow) {
+      load_keys(kb, id);
+      take_keys();
+      float acc[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+      const int blocks = (rows + 31) / 32;
+      const int seeing = start > P ? (int)((int64_t)(start - P) * G / 32) : 0;   // blocks before see none of the keys
+      for (int block = seeing + wave; block < blocks; block += 8) {
+        const unsigned x = (unsigned)block * 32u + (unsigned)l32, r = min(x, (unsigned)rows - 1u), tok = r / (unsigned)G;
+        const int64_t row = (int64_t)(sd.row_off + (int)tok) * a.num_q_heads + g * G + (int)(r - tok * G);
+        const T* q = reinterpret_cast<const T*>(a.q) + row * D;
+        const float lse2 = a.lse[row] * kLog2e;
+        const int thr = (x < (unsigned)rows ? P + (int)tok : -1) - kb - 4 * hh;    // keys past it: not seen
+        f32x16 s = (f32x16){};
+#pragma unroll
+        for (int kk = 0; kk < KSTEPS; ++kk) {
+          bf16x8 qf[QN];
+          load_terms(q + (kCodes ? hh * (D / 16) + kk : 2 * kk + hh) * 8, qf);
+          products32(s, kf[kk], qf);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse2));
+          acc[e] += 8 * (e >> 2) + (e & 3) > thr ? 0.f : p;
+        }
+      }
+      const float sum = scatter_sum(acc, lane, 16);
+      join_waves(sum + __shfl_xor(sum, 1));
+      return;
+    }
+  }
 
   // ---- rows in stages, from the first that sees one of the workgroup's keys.
   // Row r of a stage whose first row is head h0 of token t0 is head x - d * G of
@@ -425,7 +478,6 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   };
 
   float acc[16];
-  const float c = a.scale_log2;
   auto scores = [&](const TurnRows<T, D>& from, int block) __attribute__((always_inline)) {
     const int row = block * 32 + l32;
     f32x16 s = (f32x16){};
@@ -452,8 +504,8 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   };
   // one stage of rows, the first of which is `seen`'s and sees the fewest keys
   auto take_rows = [&](const TurnRows<T, D>& cur, int seen, int last) __attribute__((always_inline)) {
-    if (narrow) {
-      if (wave < BLOCKS) add(cur, wave, scores(cur, wave), std::true_type());
+    if (QN == 1 && narrow) {
+      add(cur, wave, scores(cur, wave), std::true_type());
     } else if (P + seen >= kb + 31 && last <= rows) {
       f32x16 s = scores(cur, 0);
 #pragma unroll
@@ -488,7 +540,6 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
     if (ONCE && !kFly && base != start) load_keys(kb, id);
     take_keys();
-    const int e = l32 >> 1, k32 = 8 * (e >> 2) + 4 * hh + (e & 3);   // the key whose sum ends in this lane
     const float old = w[min(kb + k32, L - 1)];
     const int next = kb + step;
     if constexpr (ONCE) {
@@ -517,15 +568,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     if (!narrow) {
       if ((lane & 1) == 0 && kb + k32 < L) w[kb + k32] = kb + k32 < P ? old + sum : sum;
     } else {
-      float* red = reinterpret_cast<float*>(turn_lds);   // the rows are done with
-      __syncthreads();
-      if ((lane & 1) == 0) red[wave * 32 + k32] = sum;
-      __syncthreads();
-      if (tid < 32 && kb + tid < L) {
-        sum = 0.f;
-        for (int x = 0; x < 8; ++x) sum += red[x * 32 + tid];
-        put(w, kb + tid, sd, sum);
-      }
+      join_waves(sum);
     }
     kb = next;
   }

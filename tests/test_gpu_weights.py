@@ -37,7 +37,9 @@ CALLS = [  # prefix, suffix, hq, hkv, d
     # up to 4, 8, 16 and 32 rows of a kv-head, sequences of fewer among them
     ([1000, 33, 0], [2, 1, 2], 8, 2, 128), ([500, 64], [1, 1], 7, 1, 64), ([129, 3, 40], [3, 1, 2], 5, 1, 64),
     ([5000, 30, 200, 1], [1] * 4, 16, 1, 128), ([9000], [1], 4, 4, 64), ([40, 8000], [4, 2], 6, 3, 128),
-    ([2000, 31], [3, 7], 4, 1, 64)]
+    ([2000, 31], [3, 7], 4, 1, 64),
+    # whole rounds of wide workgroups and what is left of them in narrow ones
+    ([7900], [330], 32, 8, 64), ([4100, 4000], [100, 450], 8, 8, 64)]
 
 
 @pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "mx"), ("f32", "mx")])
