@@ -130,7 +130,8 @@ class Batch:
     def weights(self, old, lse):
         """(weights, bound) in float64 from old weights [B][Hkv][stride] and the float32 lse of the call.  A term is
         off by the score, the lse in log2 units (2^-23 of it) and the exponential; the sum over R rows by 2^-23 R; the
-        old weight and the sum are rounded once together."""
+        old weight and the sum are rounded once together.  A term under fp32's smallest normal number may become 0, as
+        may the sum: less than (R + 1) 2^-126 in all."""
         want, bound = old.double().clone(), torch.zeros(old.shape, dtype=torch.float64)
         for b, rows, s, v, off in self.parts():
             p, n = self.prefix[b], self.suffix[b]
@@ -141,7 +142,7 @@ class Batch:
             want[b, :, :p] += got[:, :p]
             want[b, :, p:p + n] = got[:, p:]
             bound[b, :, :p + n] = (term * err).sum(dim=(1, 2)) + 2.0 ** -23 * (n * self.hq // self.hkv + 2) * got
-            bound[b, :, :p + n] += 2.0 ** -23 * want[b, :, :p + n].abs()
+            bound[b, :, :p + n] += 2.0 ** -23 * want[b, :, :p + n].abs() + (n * self.hq // self.hkv + 1) * 2.0 ** -126
         return want, bound
 
 
