@@ -472,13 +472,16 @@ size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
  *   a = sum_{i < S_b, P_b + i >= j} sum_{h of g} exp(scale <q[off_b+i][h], K_b[j]> - lse[off_b+i][h])
  *   weights[b][g][j] = (j < P_b ? weights[b][g][j] : 0) + a
  * with the q, scale and lse of that attention call (extend, cascade or decode,
- * after it on the stream).  The new positions are set, so a row needs no
- * clearing; entries from P_b + S_b on are left as they were.
+ * after it on the stream; over fp32 pages by kvt_attention_weights_ex, see there).
+ * The new positions are set, so a row needs no clearing; entries from P_b + S_b on
+ * are left as they were.
  *
  * weights: device float [B][Hkv], rows weights_stride elements apart (at least
  * the longest sequence), 4-byte aligned, apart from q, lse and the pools; row b
  * belongs to sequence b, a forked sequence has a row of its own.  Scores keep
- * fp32's precision in every dtype (fp32 inputs are not rounded to bf16 here).
+ * fp32's precision in every dtype (fp32 inputs are not rounded to bf16 here), and a
+ * new token's row adds up to 1 as far as its lse is that of its scores: over bf16
+ * pages within 2^-8, as the attention calls sum probabilities rounded to bf16.
  * Each weight is summed in one fixed order: results are bit-reproducible.  A row
  * whose lse is NaN makes every weight that it adds to NaN; a non-finite key by
  * itself leaves its own weight unspecified, and no other.
@@ -486,6 +489,18 @@ size_t kvt_mx_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seqs,
 kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
                                  const void* q, int32_t num_q_heads, float scale, const float* lse,
                                  float* weights, int64_t weights_stride, void* stream);
+
+/* Scores of kvt_attention_weights_ex.  The attention calls over fp32 pages round q
+ * and K to bf16, and so does ROUNDED, for the lse that they return.  EXACT (what
+ * kvt_attention_weights does) is for an lse of unrounded scores: with theirs, row
+ * sums and weights are off by exp(the rounding of a score), several percent
+ * where scores are large.  Over bf16 pages the two are the same.  Any
+ * other value gives KVT_ERR_INVALID_ARG.  (4-bit pages need no choice: their
+ * attention calls keep fp32 queries.) */
+typedef enum { KVT_WEIGHTS_EXACT = 0, KVT_WEIGHTS_ROUNDED = 1 } kvt_weights_scores;
+kvt_status kvt_attention_weights_ex(const kvt_pool* pool, const kvt_seqs* seqs,
+                                    const void* q, int32_t num_q_heads, float scale, const float* lse,
+                                    float* weights, int64_t weights_stride, int32_t scores, void* stream);
 kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs,
                                     const void* q, int32_t num_q_heads, float scale, const float* lse,
                                     float* weights, int64_t weights_stride, void* stream);

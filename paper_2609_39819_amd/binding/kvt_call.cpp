@@ -353,23 +353,30 @@ PyObject* mx_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
-// weights(head..., q, num_q_heads, scale, lse, weights, stride, stream) -> status
+// weights(head..., q, num_q_heads, scale, lse, weights, stride, stream[, scores]) -> status;
+// with `scores` the entry is kvt_attention_weights_ex
 PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Head h;
   void *q, *lse, *w, *stream;
   int32_t hq;
+  int32_t scores = -1;
   long long stride;
-  if (!count_is(n, kHead + 7) || !head(a, &h) || !address(a[kHead], &q) || !int32(a[kHead + 1], &hq)) return nullptr;
+  const bool chosen = n == kHead + 8;
+  if (!(chosen || count_is(n, kHead + 7)) || !head(a, &h) || !address(a[kHead], &q) || !int32(a[kHead + 1], &hq))
+    return nullptr;
   const double scale = PyFloat_AsDouble(a[kHead + 2]);
   if (scale == -1.0 && PyErr_Occurred()) return nullptr;
   if (!address(a[kHead + 3], &lse) || !address(a[kHead + 4], &w) || !integer(a[kHead + 5], &stride) ||
-      !address(a[kHead + 6], &stream))
+      !address(a[kHead + 6], &stream) || (chosen && !int32(a[kHead + 7], &scores)))
     return nullptr;
   kvt_status st;
+  const float* l = reinterpret_cast<const float*>(lse);
+  float* sums = reinterpret_cast<float*>(w);
   Py_BEGIN_ALLOW_THREADS
-  st = reinterpret_cast<decltype(&kvt_attention_weights)>(h.fn)(&h.pool, &h.seqs, q, hq, (float)scale,
-                                                                reinterpret_cast<const float*>(lse),
-                                                                reinterpret_cast<float*>(w), stride, stream);
+  st = chosen ? reinterpret_cast<decltype(&kvt_attention_weights_ex)>(h.fn)(&h.pool, &h.seqs, q, hq, (float)scale, l,
+                                                                            sums, stride, scores, stream)
+              : reinterpret_cast<decltype(&kvt_attention_weights)>(h.fn)(&h.pool, &h.seqs, q, hq, (float)scale, l,
+                                                                         sums, stride, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }

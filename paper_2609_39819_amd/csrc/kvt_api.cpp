@@ -1405,9 +1405,11 @@ int64_t longest_sequence(const kvt_seqs* seqs) {
 }
 
 kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
-                             float scale, const float* lse, float* weights, int64_t stride, void* stream, bool mx) {
+                             float scale, const float* lse, float* weights, int64_t stride, int32_t scores,
+                             void* stream, bool mx) {
   kvt_status st = check_pool(pool);
   if (st != KVT_OK) return st;
+  if (scores != KVT_WEIGHTS_EXACT && scores != KVT_WEIGHTS_ROUNDED) return KVT_ERR_INVALID_ARG;
   int64_t T = 0;
   if ((st = check_seqs(seqs, &T)) != KVT_OK) return st;
   if (q == nullptr || lse == nullptr || weights == nullptr || !aligned16(q) || ((uintptr_t)lse & 3) != 0 ||
@@ -1440,7 +1442,8 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
   a.num_kv_heads = pool->num_kv_heads;
   a.group = G;
   a.scale_log2 = scale * 1.4426950408889634f;
-  const int format = mx ? kvt::kMx : pool->dtype;
+  const bool rounded = scores == KVT_WEIGHTS_ROUNDED && pool->dtype == KVT_DTYPE_F32;
+  const int format = mx ? kvt::kMx : rounded ? kvt::kRounded : pool->dtype;
   const std::vector<int> order = longest_first(seqs);
   int64_t most_rows = 0;
   std::vector<int32_t> row_off(B + 1, 0);
@@ -2150,7 +2153,16 @@ kvt_status kvt_mx_decode_attention(const kvt_pool* pool, const kvt_seqs* seqs, c
 kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
                                  float scale, const float* lse, float* weights, int64_t weights_stride,
                                  void* stream) try {
-  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, stream, false);
+  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, KVT_WEIGHTS_EXACT, stream,
+                           false);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_attention_weights_ex(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
+                                    float scale, const float* lse, float* weights, int64_t weights_stride,
+                                    int32_t scores, void* stream) try {
+  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, scores, stream, false);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }
@@ -2158,7 +2170,8 @@ kvt_status kvt_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, con
 kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const void* q, int32_t num_q_heads,
                                     float scale, const float* lse, float* weights, int64_t weights_stride,
                                     void* stream) try {
-  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, stream, true);
+  return attention_weights(pool, seqs, q, num_q_heads, scale, lse, weights, weights_stride, KVT_WEIGHTS_EXACT, stream,
+                           true);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }

@@ -137,8 +137,11 @@ hipError_t launch_mx_read(const MxRowsArgs& a, int dtype, int head_dim, hipStrea
 hipError_t launch_mx_extend(const ExtendArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_mx_decode(const MxDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_mx_join(const MxJoinArgs& a, int dtype, int head_dim, hipStream_t stream);
-// format: a kvt_dtype of the K pool, or kMx for 4-bit pages; dtype is q's.
+// format: a kvt_dtype of the K pool, kMx for 4-bit pages, or kRounded for fp32
+// pages and queries that are rounded to bf16 as the other attention calls round
+// them (attention weights only); dtype is q's.
 constexpr int kMx = 2;
+constexpr int kRounded = 3;
 hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
 hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int head_dim, int grid, hipStream_t stream);
 constexpr int kWeightsStepKeys = 32;      // step kernel: keys of one tile

@@ -65,6 +65,9 @@ __device__ __forceinline__ void split3(f32x4 a, f32x4 b, bf16x8 (&t)[3]) {
 __device__ __forceinline__ void load_terms(const __bf16* p, bf16x8 (&t)[1]) {
   t[0] = __builtin_bit_cast(bf16x8, load8(p));
 }
+__device__ __forceinline__ void load_terms(const float* p, bf16x8 (&t)[1]) {   // rounded
+  t[0] = __builtin_bit_cast(bf16x8, load8(p));
+}
 __device__ __forceinline__ void load_terms(const float* p, bf16x8 (&t)[3]) {
   split3(*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4), t);
 }

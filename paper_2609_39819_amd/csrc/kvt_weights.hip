@@ -6,7 +6,10 @@
 // K once and no V.  Every weight is summed by one workgroup in a fixed order.
 // Scores are fp32 sums of exact products: bf16 and 4-bit keys are bf16
 // operands; fp32 ones three bf16 terms, whose products with a query's three
-// are the six that reach 2^-24.
+// are the six that reach 2^-24.  The log-sum-exp of the plain attention calls over
+// fp32 pages is that of operands rounded to bf16, and weights that go with it need
+// the same scores (kRounded).  8/2 heads over 4000 keys, scores spread over tens:
+// rows add up to 1 within 1e-4 so, of the six products within 5e-2.
 //
 // Two kernels, by the rows that the largest sequence adds:
 //   * step (at most 32 rows, a decoding step): HBM-bound on K.  4 waves stream
@@ -22,7 +25,7 @@
 //     keys as operands in registers; the rows pass through LDS, 256 in bf16 or 64
 //     in fp32 at a time, two such stages in turn, for all waves of the workgroup.
 //     512 new tokens over 8192, 32/8 heads of 128: 54.5 us, of which a full round of
-//     wide workgroups is 39 (880 TFLOP/s).
+//     wide workgroups is 39 (880 TFLOP/s); fp32 195, rounded 91.
 #include <type_traits>
 
 #include "kvt_mx_device.h"
@@ -34,6 +37,16 @@ using namespace dev;
 
 template <int FORMAT>
 constexpr int kKeyTerms = FORMAT == 1 ? 3 : 1;
+template <typename T, int FORMAT>
+constexpr int kQueryTerms = FORMAT == kRounded ? 1 : kTerms<T>;
+
+// 8 fp32 columns of a key as its terms.
+__device__ __forceinline__ void key_terms(u32x4 a, u32x4 b, bf16x8 (&t)[1]) {
+  t[0] = __builtin_bit_cast(bf16x8, round8(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, b)));
+}
+__device__ __forceinline__ void key_terms(u32x4 a, u32x4 b, bf16x8 (&t)[3]) {
+  split3(__builtin_bit_cast(f32x4, a), __builtin_bit_cast(f32x4, b), t);
+}
 
 // s += Q K^T (a lane has a key's scores of four rows), or K Q^T, over the terms of
 // both whose product counts
@@ -83,7 +96,7 @@ __device__ __forceinline__ void put(float* w, int key, const SeqDesc& sd, float 
 template <typename T, int D, int FORMAT, int R>
 __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs a) {
   constexpr bool kCodes = FORMAT == kMx;
-  constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
+  constexpr int QN = kQueryTerms<T, FORMAT>, KN = kKeyTerms<FORMAT>;
   constexpr int KS = D / 32;
   constexpr int NB = R == 32 ? 2 : 1;
   constexpr bool kOnePage = R <= 8;              // of a tile, for each lane: page `half`
@@ -201,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
         bf16x8 kf[KN];
         if constexpr (kCodes) kf[0] = mx_values(st.k[p][0][kk], scale);
         else if constexpr (FORMAT == 0) kf[0] = __builtin_bit_cast(bf16x8, st.k[p][kk]);
-        else split3(__builtin_bit_cast(f32x4, st.k[p][2 * kk]), __builtin_bit_cast(f32x4, st.k[p][2 * kk + 1]), kf);
+        else key_terms(st.k[p][2 * kk], st.k[p][2 * kk + 1], kf);
 #pragma unroll
         for (int b = 0; b < NB; ++b) products16(s[b][p], kf, qreg[b][kk]);
       }
@@ -277,9 +290,9 @@ __global__ __launch_bounds__(256, 2) void weights_step_kernel(const WeightsArgs 
 // the 16-byte chunks of a row XOR-swizzled as a key tile's in the extend kernel.
 template <typename T>
 constexpr int kTurnRows = weights_stage_rows(sizeof(T) == 2 ? 0 : 1);
-template <typename T, int D>
+template <typename T, int D, int QN>
 struct TurnRows {
-  __bf16 q[kTerms<T>][kTurnRows<T> * D];
+  __bf16 q[QN][kTurnRows<T> * D];
   float lse[kTurnRows<T>];
   int lim[kTurnRows<T>];
 };
@@ -287,14 +300,16 @@ struct TurnRows {
 template <typename T, int D, int FORMAT, bool ONCE>
 __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) {
   constexpr bool kCodes = FORMAT == kMx;
-  constexpr int QN = kTerms<T>, KN = kKeyTerms<FORMAT>;
+  constexpr bool kDirect = sizeof(T) == 2;       // rows go straight into LDS
+  constexpr int QN = kQueryTerms<T, FORMAT>, KN = kKeyTerms<FORMAT>;
   constexpr int KSTEPS = D / 16, CHUNKS = D / 8;
   constexpr int ROWS = kTurnRows<T>, BLOCKS = ROWS / 32;
-  static_assert(QN == 3 || BLOCKS == 8, "a narrow workgroup's waves have a block each");
+  static_assert(!kDirect || BLOCKS == 8, "a narrow workgroup's waves have a block each");
+  typedef TurnRows<T, D, QN> Rows;
   constexpr int64_t kPage = kCodes ? mx_page_bytes(D) : (int64_t)kBlock * D * (FORMAT == 0 ? 2 : 4);
   constexpr int PIECES = ROWS * CHUNKS / 512;    // of 8 columns, per thread and stage
   extern __shared__ __attribute__((aligned(1024))) char turn_lds[];
-  TurnRows<T, D>* stage = reinterpret_cast<TurnRows<T, D>*>(turn_lds);   // two
+  Rows* stage = reinterpret_cast<Rows*>(turn_lds);   // two
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -325,7 +340,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
   // one: not stored)
   const uint32_t nb_max = (uint32_t)min<int64_t>(a.num_blocks, 0x7fffffff) - 1u;
   constexpr int KP = kCodes ? D / 64 : KSTEPS * (FORMAT == 0 ? 1 : 2);   // 16-byte pieces of a lane's columns
-  constexpr bool kFly = ONCE && FORMAT != 1;     // the next tile's in flight (fp32: too many registers)
+  constexpr bool kFly = ONCE && (kCodes || FORMAT == 0);   // the next tile's in flight (fp32: too many registers)
   u32x4 kraw[KP];
   unsigned char kscale[kCodes ? D / 64 : 1];
   auto page_of = [&](int kb) __attribute__((always_inline)) {
@@ -354,7 +369,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     for (int kk = 0; kk < KSTEPS; ++kk) {
       if constexpr (kCodes) kf[kk][0] = mx_values(kraw[kk / 4][kk % 4], mx_scale(kscale[kk / 4]));
       else if constexpr (FORMAT == 0) kf[kk][0] = __builtin_bit_cast(bf16x8, kraw[kk]);
-      else split3(__builtin_bit_cast(f32x4, kraw[2 * kk]), __builtin_bit_cast(f32x4, kraw[2 * kk + 1]), kf[kk]);
+      else key_terms(kraw[2 * kk], kraw[2 * kk + 1], kf[kk]);
     }
   };
   int kb = start + (narrow ? 0 : wave * 32);
@@ -374,7 +389,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
       put(w, kb + tid, sd, sum);
     }
   };
-  if constexpr (!ONCE && QN == 3) {
+  if constexpr (!ONCE && !kDirect) {
     // a narrow workgroup's fp32 rows, each used once, go straight into operands: a
     // stage holds blocks for two of the waves only (512 new tokens over 8192, 32/8
     // heads of 128: 214 us by stages, 192 so, of 64 over 4-bit pages 91 and 59; bf16
@@ -428,22 +443,22 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     row = (int64_t)(sd.row_off + (past ? 0 : tok)) * a.num_q_heads + g * G + (x - d * G);
   };
   constexpr int QP = (int)sizeof(T) / 2;
-  u32x4 raw[QN == 1 ? 1 : PIECES][QP];
+  u32x4 raw[kDirect ? 1 : PIECES][QP];
   float lse_raw = 0.f;
   int lim_raw = -1;
   // bf16 rows go straight into LDS: load i of a wave brings 64 pieces, and lane l
   // lands at piece l of them, so it fetches the chunk that the swizzle puts there;
   // fp32 rows pass through registers (drop), where they become their terms
-  auto load_stage = [&](TurnRows<T, D>& to) __attribute__((always_inline)) {
+  auto load_stage = [&](Rows& to) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < PIECES; ++x) {
-      const int p = (QN == 1 ? (wave * PIECES + x) * 64 + lane : tid + x * 512);
-      const int r = p / CHUNKS, chunk = QN == 1 ? (p % CHUNKS) ^ swz<D>(r) : p % CHUNKS;
+      const int p = (kDirect ? (wave * PIECES + x) * 64 + lane : tid + x * 512);
+      const int r = p / CHUNKS, chunk = kDirect ? (p % CHUNKS) ^ swz<D>(r) : p % CHUNKS;
       int tok;
       int64_t row;
       place(r, tok, row);
       const char* q = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.q) + row * D + chunk * 8);
-      if constexpr (QN == 1) {
+      if constexpr (kDirect) {
         __builtin_amdgcn_global_load_lds(
             (const void*)q, (__attribute__((address_space(3))) void*)((lds_bf16*)to.q[0] + (wave * PIECES + x) * 512), 16,
             0, 0);
@@ -463,22 +478,22 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     h0 += adv_h;
     if (h0 >= G) h0 -= G, ++t0;
   };
-  auto drop = [&](TurnRows<T, D>& to) __attribute__((always_inline)) {
-    if constexpr (QN == 3) {
+  auto drop = [&](Rows& to) __attribute__((always_inline)) {
+    if constexpr (!kDirect) {
 #pragma unroll
       for (int x = 0; x < PIECES; ++x) {
         const int p = tid + x * 512, r = p / CHUNKS, piece = r * D + (((p % CHUNKS) ^ swz<D>(r)) << 3);
-        bf16x8 t3[3];
-        split3(__builtin_bit_cast(f32x4, raw[x][0]), __builtin_bit_cast(f32x4, raw[x][1]), t3);
+        bf16x8 terms[QN];
+        key_terms(raw[x][0], raw[x][1], terms);
 #pragma unroll
-        for (int y = 0; y < QN; ++y) *reinterpret_cast<u32x4*>(to.q[y] + piece) = __builtin_bit_cast(u32x4, t3[y]);
+        for (int y = 0; y < QN; ++y) *reinterpret_cast<u32x4*>(to.q[y] + piece) = __builtin_bit_cast(u32x4, terms[y]);
       }
     }
     if (tid < ROWS) to.lse[tid] = lse_raw, to.lim[tid] = lim_raw;
   };
 
   float acc[16];
-  auto scores = [&](const TurnRows<T, D>& from, int block) __attribute__((always_inline)) {
+  auto scores = [&](const Rows& from, int block) __attribute__((always_inline)) {
     const int row = block * 32 + l32;
     f32x16 s = (f32x16){};
 #pragma unroll
@@ -492,7 +507,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     }
     return s;
   };
-  auto add = [&](const TurnRows<T, D>& from, int block, const f32x16& s, auto masked) __attribute__((always_inline)) {
+  auto add = [&](const Rows& from, int block, const f32x16& s, auto masked) __attribute__((always_inline)) {
     const float lse2 = from.lse[block * 32 + l32] * kLog2e;
     const int thr = decltype(masked)::value ? from.lim[block * 32 + l32] - kb - 4 * hh : 0;   // keys past lim: offset > thr
 #pragma unroll
@@ -503,8 +518,8 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
     }
   };
   // one stage of rows, the first of which is `seen`'s and sees the fewest keys
-  auto take_rows = [&](const TurnRows<T, D>& cur, int seen, int last) __attribute__((always_inline)) {
-    if (QN == 1 && narrow) {
+  auto take_rows = [&](const Rows& cur, int seen, int last) __attribute__((always_inline)) {
+    if (kDirect && narrow) {
       add(cur, wave, scores(cur, wave), std::true_type());
     } else if (P + seen >= kb + 31 && last <= rows) {
       f32x16 s = scores(cur, 0);
@@ -550,7 +565,7 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
       take_rows(stage[0], 0, ROWS);
     } else {
       for (int i = first; i < stages; ++i) {
-        TurnRows<T, D>& fill = stage[(i + 1 - first) & 1];
+        Rows& fill = stage[(i + 1 - first) & 1];
         if (i + 1 < stages) load_stage(fill);
         take_rows(stage[(i - first) & 1], seen, (i + 1) * ROWS);
         seen += adv_t;
@@ -586,11 +601,11 @@ void launch_step_as(const WeightsArgs& a, int grid, hipStream_t stream) {
 }
 template <typename T, int D, int FORMAT>
 void launch_turn_as(const WeightsArgs& a, int grid, hipStream_t stream) {
+  constexpr unsigned kStage = sizeof(TurnRows<T, D, kQueryTerms<T, FORMAT>>);
   if (a.tiles > 0)
-    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, true>), dim3(grid), dim3(512), sizeof(TurnRows<T, D>), stream, a);
+    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, true>), dim3(grid), dim3(512), kStage, stream, a);
   else
-    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, false>), dim3(grid), dim3(512), 2 * sizeof(TurnRows<T, D>),
-                       stream, a);
+    hipLaunchKernelGGL((weights_turn_kernel<T, D, FORMAT, false>), dim3(grid), dim3(512), 2 * kStage, stream, a);
 }
 
 }  // namespace
@@ -599,6 +614,7 @@ hipError_t launch_weights_step(const WeightsArgs& a, int format, int dtype, int 
   const bool wide = head_dim == 128;
   if (format == 0) wide ? launch_step_as<__bf16, 128, 0>(a, grid, stream) : launch_step_as<__bf16, 64, 0>(a, grid, stream);
   else if (format == 1) wide ? launch_step_as<float, 128, 1>(a, grid, stream) : launch_step_as<float, 64, 1>(a, grid, stream);
+  else if (format == kRounded) wide ? launch_step_as<float, 128, kRounded>(a, grid, stream) : launch_step_as<float, 64, kRounded>(a, grid, stream);
   else if (dtype == 0) wide ? launch_step_as<__bf16, 128, kMx>(a, grid, stream) : launch_step_as<__bf16, 64, kMx>(a, grid, stream);
   else wide ? launch_step_as<float, 128, kMx>(a, grid, stream) : launch_step_as<float, 64, kMx>(a, grid, stream);
   return hipGetLastError();
@@ -608,6 +624,7 @@ hipError_t launch_weights_turn(const WeightsArgs& a, int format, int dtype, int 
   const bool wide = head_dim == 128;
   if (format == 0) wide ? launch_turn_as<__bf16, 128, 0>(a, grid, stream) : launch_turn_as<__bf16, 64, 0>(a, grid, stream);
   else if (format == 1) wide ? launch_turn_as<float, 128, 1>(a, grid, stream) : launch_turn_as<float, 64, 1>(a, grid, stream);
+  else if (format == kRounded) wide ? launch_turn_as<float, 128, kRounded>(a, grid, stream) : launch_turn_as<float, 64, kRounded>(a, grid, stream);
   else if (dtype == 0) wide ? launch_turn_as<__bf16, 128, kMx>(a, grid, stream) : launch_turn_as<__bf16, 64, kMx>(a, grid, stream);
   else wide ? launch_turn_as<float, 128, kMx>(a, grid, stream) : launch_turn_as<float, 64, kMx>(a, grid, stream);
   return hipGetLastError();

@@ -40,7 +40,7 @@ MGR_EXPORTED = ("kvt_mgr_append", "kvt_mgr_begin_request", "kvt_mgr_create", "kv
 MGR_OPS = ("spawn", "fork", "append", "one_off", "pin", "unpin", "replace", "remove", "terminate", "begin_request",
            "start_prefill", "prefill_done", "end_request")   # KVT_MGR_OP_* in this order
 EXPORTED = ("kvt_append_kv", "kvt_mx_append_kv", "kvt_append_kv_rotary", "kvt_attention_weights",
-            "kvt_mx_attention_weights", "kvt_cascade_extend_attention",
+            "kvt_attention_weights_ex", "kvt_mx_attention_weights", "kvt_cascade_extend_attention",
             "kvt_cascade_extend_attention_ex", "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
             "kvt_copy_blocks",
             "kvt_decode_attention", "kvt_mx_decode_attention", "kvt_decode_workspace_bytes",
@@ -51,6 +51,7 @@ EXPORTED = ("kvt_append_kv", "kvt_mx_append_kv", "kvt_append_kv_rotary", "kvt_at
             "kvt_last_hip_error", "kvt_mx_read_kv", "kvt_rotate",
             "kvt_status_str") + MGR_EXPORTED
 CASCADE_AUTO, CASCADE_SHARED_PASS, CASCADE_PLAIN = 0, 1, 2    # kvt_cascade_mode
+WEIGHTS_EXACT, WEIGHTS_ROUNDED = 0, 1                         # kvt_weights_scores
 KVT_COPY_TO_HOST = 0
 KVT_COPY_TO_DEVICE = 1
 KVT_PINNED, KVT_ACTIVE, KVT_SUSPENDED, KVT_EXPIRED, KVT_TEMPORARY = 0, 1, 2, 3, 4
@@ -181,6 +182,8 @@ def lib():
             getattr(L, name).argtypes = [P(KvtPool), P(KvtSeqs), ctypes.c_void_p, ctypes.c_int32, ctypes.c_float,
                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
             getattr(L, name).restype = ctypes.c_int
+        L.kvt_attention_weights_ex.argtypes = [*L.kvt_attention_weights.argtypes[:-1], ctypes.c_int32, ctypes.c_void_p]
+        L.kvt_attention_weights_ex.restype = ctypes.c_int
         for name in ("kvt_evict", "kvt_mx_evict"):
             getattr(L, name).argtypes = [P(KvtPool), P(KvtSeqs), P(KvtEviction), ctypes.c_void_p]
             getattr(L, name).restype = ctypes.c_int
@@ -952,7 +955,8 @@ def _head_rows(t, name: str, seqs: int, hkv: int, least: int, dtype, device: int
 
 
 def attention_weights(q, k_pool, v_pool, block_table, prefix_len: Sequence[int], suffix_len: Optional[Sequence[int]],
-                      lse, weights, scale: Optional[float] = None, *, stream=None, checked: bool = False):
+                      lse, weights, scale: Optional[float] = None, *, rounded: bool = False, stream=None,
+                      checked: bool = False):
     """What the attention of the new tokens gave every position, summed per
     kv-head onto ``weights`` (``kvt_attention_weights``, over 4-bit pools
     ``kvt_mx_attention_weights``).
@@ -961,16 +965,22 @@ def attention_weights(q, k_pool, v_pool, block_table, prefix_len: Sequence[int],
     None) ``decode_attention`` call with the same pools, table, lengths and
     scale.  ``weights``: float32 [B][Hkv][>= longest sequence]; reused positions
     are added to, new ones set, the entries past a sequence are left alone.
-    Returns ``weights``.
+    ``rounded`` (plain pools only): over float32 pools those calls round ``q`` and K to
+    bf16, and their ``lse`` needs weights of scores that are rounded alike; without it
+    scores keep float32's precision, for an ``lse`` of such scores.  Over bf16 pools
+    it changes nothing.  Returns ``weights``.
     """
     import torch
     if stream is not None:
         with _on_stream(stream, k_pool):
             return attention_weights(q, k_pool, v_pool, block_table, prefix_len, suffix_len, lse, weights, scale,
-                                     checked=checked)
+                                     rounded=rounded, checked=checked)
     four = k_pool.dtype == torch.uint8
+    if four and rounded:
+        raise ValueError("attention over 4-bit pools does not round its operands")
     pool = _mx_pool_args(k_pool, v_pool, q.dtype) if four else _pool_args(k_pool, v_pool)
-    entry = "kvt_mx_attention_weights" if four else "kvt_attention_weights"
+    entry = ("kvt_mx_attention_weights" if four else "kvt_attention_weights_ex" if rounded
+             else "kvt_attention_weights")
     head, T = _head(entry, pool, prefix_len, suffix_len, block_table, checked)
     Hq, d, device = int(q.shape[1]), pool[4], k_pool.get_device()
     _check_tokens(q, "q", T, Hq, d, q.dtype if four else k_pool.dtype)
@@ -981,7 +991,7 @@ def attention_weights(q, k_pool, v_pool, block_table, prefix_len: Sequence[int],
         scale = 1.0 / math.sqrt(d)
     with _on_device(k_pool):
         st = _native().weights(*head, q.data_ptr(), Hq, float(scale), lse.data_ptr(), weights.data_ptr(), stride,
-                               _stream_handle(k_pool))
+                               _stream_handle(k_pool), *((WEIGHTS_ROUNDED,) if rounded else ()))
     if st != KVT_OK:
         raise KvtError(st, entry)
     return weights
