@@ -404,7 +404,10 @@ size_t kvt_diff_decode_workspace_bytes(const kvt_pool* pool, const kvt_seqs* seq
  * kv-head: its scale bytes are 255 and its values read as NaN.
  *
  * Block tables, sequences, checked mode, ordering and asynchrony are those of
- * the other calls.  A page moves, is shared and is freed as any other page.
+ * the other calls.  A page is shared and freed as any other page, and
+ * kvt_mx_copy_blocks moves it to and from the host.  Nothing in a kvt_pool tells
+ * 4-bit pages from plain ones: a call for plain pages takes a record for
+ * 16 * head_dim elements of dtype, and reads and writes past the pool.
  * ---------------------------------------------------------------------- */
 #define KVT_MX_PAGE_BYTES(head_dim) (KVT_BLOCK_SIZE * ((head_dim) / 2 + (head_dim) / 32))
 
@@ -571,6 +574,11 @@ typedef enum {
  */
 kvt_status kvt_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host,
                            int64_t num_ids, void* host, int32_t direction, void* stream);
+
+/* kvt_copy_blocks for 4-bit pages: host is a packed
+ * [num_ids][2][Hkv][KVT_MX_PAGE_BYTES(head_dim)] array of bytes. */
+kvt_status kvt_mx_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host,
+                              int64_t num_ids, void* host, int32_t direction, void* stream);
 
 /* ------------------------------------------------------------------------
  * Host block manager (CPU only; no HIP calls).

@@ -121,11 +121,12 @@ kvt_status check_append_targets(const kvt_seqs* seqs, int64_t T) {
   return KVT_OK;
 }
 
-// Bytes of one of a pool's two tensors; `mx`: of 4-bit pages.
+// Bytes of one kv-head's page, and of one of a pool's two tensors; `mx`: 4-bit pages.
+int64_t page_bytes_of_head(const kvt_pool* pool, bool mx) {
+  return mx ? kvt::mx_page_bytes(pool->head_dim) : (int64_t)kvt::kBlock * pool->head_dim * elem_bytes(pool->dtype);
+}
 size_t pool_tensor_bytes(const kvt_pool* pool, bool mx) {
-  const size_t page = mx ? (size_t)kvt::mx_page_bytes(pool->head_dim)
-                          : (size_t)kvt::kBlock * pool->head_dim * elem_bytes(pool->dtype);
-  return (size_t)pool->num_blocks * pool->num_kv_heads * page;
+  return (size_t)pool->num_blocks * pool->num_kv_heads * (size_t)page_bytes_of_head(pool, mx);
 }
 
 bool overlaps(const void* a, size_t an, const void* b, size_t bn) {
@@ -1628,6 +1629,50 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
   return KVT_OK;
 }
 
+// Pages to or from pinned host memory; `mx`: 4-bit pages.
+kvt_status copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host, int64_t num_ids,
+                       void* host, int32_t direction, void* stream, bool mx) {
+  kvt_status st = check_pool(pool);
+  if (st != KVT_OK) return st;
+  if (num_ids < 0 || (num_ids > 0 && (block_ids == nullptr || host == nullptr))) return KVT_ERR_INVALID_ARG;
+  if (direction != KVT_COPY_TO_HOST && direction != KVT_COPY_TO_DEVICE) return KVT_ERR_INVALID_ARG;
+  if (num_ids == 0) return KVT_OK;
+  const int64_t page_bytes = (int64_t)pool->num_kv_heads * page_bytes_of_head(pool, mx);
+  if (num_ids > (INT64_MAX / 4) / (2 * page_bytes)) return KVT_ERR_INVALID_ARG;
+  if (block_ids_host != nullptr) {
+    std::unordered_set<int32_t> seen;
+    for (int64_t i = 0; i < num_ids; ++i) {
+      const int32_t id = block_ids_host[i];
+      if (id < 0 || id >= pool->num_blocks) return KVT_ERR_OUT_OF_RANGE;
+      // two host pages landing on one pool page would race
+      if (direction == KVT_COPY_TO_DEVICE && !seen.insert(id).second) return KVT_ERR_OUT_OF_RANGE;
+    }
+  }
+  // the host side must be pinned memory the device can address
+  hipPointerAttribute_t attr;
+  std::memset(&attr, 0, sizeof(attr));
+  if (hipPointerGetAttributes(&attr, host) != hipSuccess) {
+    (void)hipGetLastError();
+    return KVT_ERR_INVALID_ARG;
+  }
+  if (attr.type != hipMemoryTypeHost) return KVT_ERR_INVALID_ARG;
+  void* host_dev = attr.devicePointer != nullptr ? attr.devicePointer : host;
+
+  kvt::CopyArgs a;
+  a.k_pool = pool->k;
+  a.v_pool = pool->v;
+  a.ids = block_ids;
+  a.n = num_ids;
+  a.host = host_dev;
+  a.page_bytes = page_bytes;
+  a.num_blocks = pool->num_blocks;
+  a.to_host = direction == KVT_COPY_TO_HOST ? 1 : 0;
+  const int64_t pieces = num_ids * 2 * page_bytes / 16;
+  const int grid = (int)std::min<int64_t>((pieces + 255) / 256, 8192);
+  const hipError_t e = kvt::launch_copy_blocks(a, grid, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? KVT_OK : device_error(e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1830,46 +1875,10 @@ kvt_status kvt_extend_attention_noalloc(const kvt_pool* pool, const kvt_seqs* se
 }
 
 kvt_status kvt_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host,
-                           int64_t num_ids, void* host, int32_t direction, void* stream) {
-  kvt_status st = check_pool(pool);
-  if (st != KVT_OK) return st;
-  if (num_ids < 0 || (num_ids > 0 && (block_ids == nullptr || host == nullptr))) return KVT_ERR_INVALID_ARG;
-  if (direction != KVT_COPY_TO_HOST && direction != KVT_COPY_TO_DEVICE) return KVT_ERR_INVALID_ARG;
-  if (num_ids == 0) return KVT_OK;
-  const int64_t page_bytes = (int64_t)pool->num_kv_heads * kvt::kBlock * pool->head_dim * elem_bytes(pool->dtype);
-  if (num_ids > (INT64_MAX / 4) / (2 * page_bytes)) return KVT_ERR_INVALID_ARG;
-  if (block_ids_host != nullptr) {
-    std::unordered_set<int32_t> seen;
-    for (int64_t i = 0; i < num_ids; ++i) {
-      const int32_t id = block_ids_host[i];
-      if (id < 0 || id >= pool->num_blocks) return KVT_ERR_OUT_OF_RANGE;
-      // two host pages landing on one pool page would race
-      if (direction == KVT_COPY_TO_DEVICE && !seen.insert(id).second) return KVT_ERR_OUT_OF_RANGE;
-    }
-  }
-  // the host side must be pinned memory the device can address
-  hipPointerAttribute_t attr;
-  std::memset(&attr, 0, sizeof(attr));
-  if (hipPointerGetAttributes(&attr, host) != hipSuccess) {
-    (void)hipGetLastError();
-    return KVT_ERR_INVALID_ARG;
-  }
-  if (attr.type != hipMemoryTypeHost) return KVT_ERR_INVALID_ARG;
-  void* host_dev = attr.devicePointer != nullptr ? attr.devicePointer : host;
-
-  kvt::CopyArgs a;
-  a.k_pool = pool->k;
-  a.v_pool = pool->v;
-  a.ids = block_ids;
-  a.n = num_ids;
-  a.host = host_dev;
-  a.page_bytes = page_bytes;
-  a.num_blocks = pool->num_blocks;
-  a.to_host = direction == KVT_COPY_TO_HOST ? 1 : 0;
-  const int64_t pieces = num_ids * 2 * page_bytes / 16;
-  const int grid = (int)std::min<int64_t>((pieces + 255) / 256, 8192);
-  const hipError_t e = kvt::launch_copy_blocks(a, grid, reinterpret_cast<hipStream_t>(stream));
-  return e == hipSuccess ? KVT_OK : device_error(e);
+                           int64_t num_ids, void* host, int32_t direction, void* stream) try {
+  return copy_blocks(pool, block_ids, block_ids_host, num_ids, host, direction, stream, false);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
 }
 
 size_t kvt_cascade_workspace_bytes_ex(const kvt_pool* pool, const kvt_seqs* seqs, int32_t shared_len,
@@ -2178,6 +2187,13 @@ kvt_status kvt_mx_attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, 
 
 kvt_status kvt_evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction* eviction, void* stream) try {
   return evict(pool, seqs, eviction, stream, false);
+} catch (const std::bad_alloc&) {
+  return device_error(hipErrorOutOfMemory);
+}
+
+kvt_status kvt_mx_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host,
+                              int64_t num_ids, void* host, int32_t direction, void* stream) try {
+  return copy_blocks(pool, block_ids, block_ids_host, num_ids, host, direction, stream, true);
 } catch (const std::bad_alloc&) {
   return device_error(hipErrorOutOfMemory);
 }

@@ -3,7 +3,7 @@
 // The multi-tier cache moves whole pages between GPU HBM and host memory
 // (offload of pages leaving HBM, reload of pages coming back).  One launch
 // moves an arbitrary list of pages: the host side is a packed array
-// [n][K | V][Hkv][16][D] in page-list order, the device side the pages
+// [n][K | V][Hkv][16][D] (of 4-bit pages [n][K | V][Hkv][record]) in page-list order, the device side the pages
 // block_ids[i] of the K and V pools.  The GPU reads and writes the pinned
 // host buffer directly over the host link, so a scattered page list costs
 // one launch instead of one DMA request per page.

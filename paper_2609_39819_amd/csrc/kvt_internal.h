@@ -101,7 +101,7 @@ struct CopyArgs {
   const int32_t* ids;   // device, n page ids
   int64_t n;
   void* host;           // pinned host buffer [n][K|V][page_bytes], device-accessible
-  int64_t page_bytes;   // bytes of one page of one tensor: Hkv * 16 * D * elem
+  int64_t page_bytes;   // bytes of one page of one tensor: Hkv * 16 * D * elem, or Hkv records of 4-bit pages
   int64_t num_blocks;
   int32_t to_host;      // 1: pool -> host; 0: host -> pool
 };

@@ -42,7 +42,7 @@ MGR_OPS = ("spawn", "fork", "append", "one_off", "pin", "unpin", "replace", "rem
 EXPORTED = ("kvt_append_kv", "kvt_mx_append_kv", "kvt_append_kv_rotary", "kvt_attention_weights",
             "kvt_attention_weights_ex", "kvt_mx_attention_weights", "kvt_cascade_extend_attention",
             "kvt_cascade_extend_attention_ex", "kvt_cascade_uses_shared_pass", "kvt_cascade_workspace_bytes", "kvt_cascade_workspace_bytes_ex",
-            "kvt_copy_blocks",
+            "kvt_copy_blocks", "kvt_mx_copy_blocks",
             "kvt_decode_attention", "kvt_mx_decode_attention", "kvt_decode_workspace_bytes",
             "kvt_mx_decode_workspace_bytes", "kvt_diff_decode_attention",
             "kvt_diff_decode_workspace_bytes", "kvt_diff_extend_attention", "kvt_diff_extend_workspace_bytes",
@@ -155,6 +155,7 @@ def lib():
         L.kvt_copy_blocks.argtypes = [P(KvtPool), ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32), ctypes.c_int64,
                                       ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
         L.kvt_copy_blocks.restype = ctypes.c_int
+        L.kvt_mx_copy_blocks.argtypes, L.kvt_mx_copy_blocks.restype = L.kvt_copy_blocks.argtypes, ctypes.c_int
         L.kvt_decode_attention.argtypes = L.kvt_extend_attention.argtypes
         L.kvt_decode_attention.restype = ctypes.c_int
         L.kvt_decode_workspace_bytes.argtypes = L.kvt_extend_workspace_bytes.argtypes
@@ -607,9 +608,12 @@ def cascade_extend_attention(q, k_pool, v_pool, block_table, prefix_len, suffix_
 
 def copy_blocks(k_pool, v_pool, block_ids, host, to_host: bool, *, stream=None, checked: bool = False):
     """Pages ``block_ids`` (device int32) of the pools to (``to_host``) or from a
-    pinned host tensor [n][2][Hkv][16][D] of the pool dtype (``kvt_copy_blocks``)."""
+    pinned host tensor [n][2][Hkv][16][D] of the pool dtype (``kvt_copy_blocks``);
+    of 4-bit pools [n][2][Hkv][mx_page_bytes(D)] of uint8 (``kvt_mx_copy_blocks``)."""
     import torch
-    pool = KvtPool(*_pool_args(k_pool, v_pool))
+    four = k_pool.dtype == torch.uint8
+    pool = KvtPool(*(_mx_pool_args(k_pool, v_pool, torch.bfloat16) if four else _pool_args(k_pool, v_pool)))
+    entry = "kvt_mx_copy_blocks" if four else "kvt_copy_blocks"
     if block_ids.dtype != torch.int32 or not block_ids.is_cuda or not block_ids.is_contiguous():
         raise ValueError("block_ids must be a contiguous int32 device tensor")
     n = int(block_ids.numel())
@@ -622,12 +626,12 @@ def copy_blocks(k_pool, v_pool, block_ids, host, to_host: bool, *, stream=None, 
     if checked:
         ids_np = np.ascontiguousarray(block_ids.cpu().numpy(), dtype=np.int32)
         ids_host = ids_np.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
-    st = lib().kvt_copy_blocks(ctypes.byref(pool), block_ids.data_ptr() if n else None, ids_host, n,
+    st = getattr(lib(), entry)(ctypes.byref(pool), block_ids.data_ptr() if n else None, ids_host, n,
                                host.data_ptr() if n else None,
                                KVT_COPY_TO_HOST if to_host else KVT_COPY_TO_DEVICE,
                                _stream_handle(k_pool, stream))
     if st != KVT_OK:
-        raise KvtError(st, "kvt_copy_blocks")
+        raise KvtError(st, entry)
 
 
 def decode_workspace_bytes(k_pool, v_pool, block_table, prefix_len, num_q_heads: int) -> int:

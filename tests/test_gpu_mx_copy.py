@@ -1,0 +1,90 @@
+"""4-bit pages to pinned host memory and back (``kvt_mx_copy_blocks``): bit copies of records, and nothing beside them."""
+import pytest
+
+from paper_2609_39819_amd import kvt
+
+from mx_common import PAGE, Batch, page_bytes
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    torch.cuda.set_device(0)
+    yield
+    torch.cuda.synchronize()
+
+
+def pinned(n, hkv, d):
+    """Room for n pages, and one behind them that no copy may touch."""
+    room = torch.empty((n + 1, 2, hkv, page_bytes(d)), dtype=torch.uint8, pin_memory=True)
+    room.fill_(0xA5)
+    return room[:n], room[n]
+
+
+@pytest.mark.timeout(300)
+@pytest.mark.parametrize("hkv, d, n", [(8, 128, 700), (1, 64, 37), (3, 64, 1), (2, 128, 2)])
+def test_offload_and_reload_are_bit_exact(hkv, d, n):
+    g = torch.Generator().manual_seed(n)
+    nb = 2 * n + 5
+    # two pages behind the pools that no reload may touch
+    rooms = [torch.randint(0, 256, (nb + 2, hkv, page_bytes(d)), generator=g, dtype=torch.uint8).cuda() for _ in "kv"]
+    k, v = (r[:nb] for r in rooms)
+    ids = torch.randperm(nb, generator=g)[:n].to(torch.int32)
+    ids[-1] = nb - 1 if nb - 1 not in ids.tolist() else ids[-1]     # the last page is among them
+    host, behind = pinned(n, hkv, d)
+    kvt.copy_blocks(k, v, ids.cuda(), host, to_host=True, checked=True)
+    torch.cuda.synchronize()
+    at = ids.long()
+    assert torch.equal(host[:, 0], k.cpu()[at]) and torch.equal(host[:, 1], v.cpu()[at])
+    assert bool((behind == 0xA5).all())
+    # back, into each other's places
+    want = [r.cpu().clone() for r in rooms]
+    to = ids.roll(1)
+    for x, side in zip(want, (0, 1)):
+        x[to.long()] = host[:, side]
+    kvt.copy_blocks(k, v, to.cuda(), host, to_host=False, checked=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(r.cpu(), x) for r, x in zip(rooms, want))
+
+
+@pytest.mark.timeout(120)
+def test_ids_outside_the_pool_are_skipped():
+    k, v = (torch.randint(0, 256, (32, 2, page_bytes(64)), dtype=torch.uint8, device="cuda") for _ in "kv")
+    host, _ = pinned(4, 2, 64)
+    kvt.copy_blocks(k, v, torch.tensor([3, 32, -1, 1 << 30], dtype=torch.int32, device="cuda"), host, to_host=True)
+    torch.cuda.synchronize()
+    assert torch.equal(host[0, 0], k[3].cpu()) and torch.equal(host[0, 1], v[3].cpu())
+    assert bool((host[1:] == 0xA5).all())
+
+
+@pytest.mark.timeout(120)
+@pytest.mark.parametrize("dtype, d", [("bf16", 128), ("f32", 64)])
+def test_attention_over_pages_that_were_away(dtype, d):
+    """Pages leave, others' bytes take their place, and they come back elsewhere: the same bits."""
+    prefix = [700, 40]
+    c = Batch(prefix, [1, 1], 8, 2, d, dtype, 61, extra_pages=60)
+    want = kvt.mx_decode_attention(c.q, c.k_pool, c.v_pool, c.table, prefix, return_lse=True)
+    used = [-(-(p + 1) // PAGE) for p in prefix]
+    ids = torch.cat([c.table[b, :n] for b, n in enumerate(used)])
+    free = [x for x in range(c.k_pool.shape[0]) if x not in set(ids.tolist())]
+    host, _ = pinned(ids.numel(), 2, d)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    kvt.copy_blocks(c.k_pool, c.v_pool, ids, host, to_host=True, stream=s)
+    torch.cuda.synchronize()
+    c.k_pool[ids.long()] = 0x5A
+    c.v_pool[ids.long()] = 0x5A
+    to = torch.tensor(free[:ids.numel()], dtype=torch.int32, device="cuda")
+    assert to.numel() == ids.numel()
+    kvt.copy_blocks(c.k_pool, c.v_pool, to, host, to_host=False, checked=True)
+    table = c.table.clone()
+    at = 0
+    for b, n in enumerate(used):
+        table[b, :n] = to[at:at + n]
+        at += n
+    got = kvt.mx_decode_attention(c.q, c.k_pool, c.v_pool, table, prefix, return_lse=True)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
