@@ -1188,7 +1188,7 @@ struct MxDecodePlan {
   std::vector<int> order;          // sequences, longest key range first
   std::vector<int32_t> share;      // by launch: tiles of a slot, 0: slot x is sequence x
   std::vector<int32_t> parts;      // by place in `order`: slots that hold a part of the sequence
-  int chunks = 1;                  // workgroups that share the rows of a kv-head
+  std::vector<int32_t> chunks;     // by launch: workgroups that share the rows of a kv-head, of its largest message
   int64_t part_rows = 0;
   size_t ws_bytes = 0;
 };
@@ -1208,21 +1208,28 @@ size_t mx_part_o_bytes(const kvt_pool* pool, int64_t part_rows) {
 MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   MxDecodePlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
-  int64_t most = 0;
-  for (int b = 0; b < B; ++b) most = std::max(most, (int64_t)seqs->suffix_len[b] * G);
-  p.chunks = (int)((most + kvt::kMxChunkRows - 1) / kvt::kMxChunkRows);
   p.order = longest_first(seqs);
   p.parts.assign(B, 1);
-  const int64_t heads = (int64_t)pool->num_kv_heads * p.chunks;
+  const int64_t hkv = pool->num_kv_heads, cus = device_cus();
   for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
     const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
-    int64_t total = 0;
-    for (int i = 0; i < n; ++i) total += mx_tiles(seqs, p.order[c0 + i]);
+    // tiles; those that the chunks with rows go through (a chunk past a sequence's
+    // rows passes over it); chunks with rows
+    int64_t total = 0, work = 0, chunks = 0, most = 1;
+    for (int i = 0; i < n; ++i) {
+      const int b = p.order[c0 + i];
+      const int64_t of = ((int64_t)seqs->suffix_len[b] * G + kvt::kMxChunkRows - 1) / kvt::kMxChunkRows;
+      total += mx_tiles(seqs, b);
+      work += mx_tiles(seqs, b) * of;
+      chunks += of;
+      most = std::max(most, of);
+    }
+    p.chunks.push_back((int32_t)most);
     const int64_t longest = mx_tiles(seqs, p.order[c0]);
     // two workgroups to a CU, of at least 16 tiles (four for each wave).  One context
     // of 131072 keys and 64 of 1024..16384, 96/8 heads of 128, with one, two and
     // four: 41.0, 33.4 and 33.4 us, 107, 84 and 90
-    const int64_t slots = std::max<int64_t>(1, 2 * device_cus() / heads);
+    const int64_t slots = std::max<int64_t>(1, 2 * cus * total / (hkv * work));
     int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
     // a sequence lies in at most one slot more than its tiles fill
     share = std::max(share, (longest + kvt::kMxMaxParts - 2) / (kvt::kMxMaxParts - 1));
@@ -1235,10 +1242,11 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     // of 100..600 28.2, 38.8; 100 of 1024..16384 131.8, 121.7; 70 of 6000 109.1, 87.5
     // (4/4 heads 60.3, 47.3).
     const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
-    const double stream = (double)total * heads * tile_bytes / 5.5e6;
-    const int64_t first = device_cus() / heads;   // sequences that have a CU of their own
-    const double beside = n > slots ? longest : n > first ? mx_tiles(seqs, p.order[c0 + first]) : 0;
-    const double last = n > slots ? mx_tiles(seqs, p.order[c0 + n - 1]) : 0;
+    const double stream = (double)work * hkv * tile_bytes / 5.5e6;
+    const int64_t first = cus * n / (hkv * chunks);   // sequences that have a CU of their own ...
+    const int64_t start = std::max<int64_t>(1, 2 * cus * n / (hkv * chunks));   // ... and that start at once
+    const double beside = n > start ? longest : n > first ? mx_tiles(seqs, p.order[c0 + first]) : 0;
+    const double last = n > start ? mx_tiles(seqs, p.order[c0 + n - 1]) : 0;
     const double alone = std::max(0.18 * longest + 0.12 * beside, stream * (n > first ? 1.0 : 5.5 / 4.3) + 0.18 * last);
     if (alone <= 6.5 + std::max(0.18 * share, stream) + 1.5 * n * share / total) share = total;
     bool split = false;
@@ -1291,7 +1299,6 @@ kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void*
   a.num_q_heads = num_q_heads;
   a.num_kv_heads = pool->num_kv_heads;
   a.group = num_q_heads / pool->num_kv_heads;
-  a.chunks = plan.chunks;
   a.scale_log2 = scale * 1.4426950408889634f;
   if (plan.ws_bytes > 0) {
     a.part_o = reinterpret_cast<float*>(workspace);
@@ -1309,6 +1316,7 @@ kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void*
     const int n = std::min(kvt::kSeqsPerLaunch, seqs->num_seqs - c0);
     a.nseq = n;
     a.share = plan.share[launch];
+    a.chunks = plan.chunks[launch];
     join.nseq = 0;
     join.row_begin[0] = 0;
     int64_t tiles = 0;
@@ -1331,7 +1339,7 @@ kvt_status launch_mx_few(const kvt_pool* pool, const kvt_seqs* seqs, const void*
     if (tiles > INT32_MAX / 2) return KVT_ERR_INVALID_ARG;   // (the kernel adds a share to a tile)
     a.tile_begin[n] = (int32_t)tiles;
     const int64_t slots = a.share > 0 ? (tiles + a.share - 1) / a.share : n;
-    const int64_t grid = slots * pool->num_kv_heads * plan.chunks;
+    const int64_t grid = slots * pool->num_kv_heads * a.chunks;
     if (grid > INT32_MAX) return KVT_ERR_INVALID_ARG;
     hipError_t e = kvt::launch_mx_decode(a, pool->dtype, pool->head_dim, (int)grid, s);
     if (e == hipSuccess && join.nseq > 0) e = kvt::launch_mx_join(join, pool->dtype, pool->head_dim, s);

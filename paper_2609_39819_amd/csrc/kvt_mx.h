@@ -50,7 +50,7 @@ struct MxDecodeArgs {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t group;        // Hq / Hkv
-  int32_t chunks;       // workgroups that share the rows of a kv-head (S_b * group): of the longest
+  int32_t chunks;       // workgroups that share the rows of a kv-head (S_b * group), of the launch's largest
   float scale_log2;
   int32_t share;
   int32_t nseq;
