@@ -1205,6 +1205,20 @@ size_t mx_part_o_bytes(const kvt_pool* pool, int64_t part_rows) {
   return ((size_t)part_rows * pool->head_dim * sizeof(float) + 255) / 256 * 256;
 }
 
+// What the choice below goes by, in us and bytes per us: a tile of a workgroup, more
+// of it while another one runs on the CU; the stream of all workgroups, and of one to
+// a CU; the join; a merge where a share goes on.  Messages of more than 16 rows run
+// an instance with twice the products and exponentials.
+struct MxRates {
+  double tile, beside, stream, one, join, merge;
+};
+const MxRates& mx_rates(int head_dim, bool message) {
+  static constexpr MxRates kRates[2][2] = {
+      {{0.15, 0.12, 3.7e6, 2.9e6, 6.5, 1.5}, {0.30, 0.10, 2.3e6, 2.3e6, 10.0, 10.0}},
+      {{0.18, 0.12, 5.5e6, 4.3e6, 6.5, 1.5}, {0.30, 0.10, 3.0e6, 3.0e6, 10.0, 10.0}}};
+  return kRates[head_dim == 128 ? 1 : 0][message ? 1 : 0];
+}
+
 MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t num_q_heads) {
   MxDecodePlan p;
   const int B = seqs->num_seqs, G = num_q_heads / pool->num_kv_heads;
@@ -1215,7 +1229,7 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
     // tiles; those that the chunks with rows go through (a chunk past a sequence's
     // rows passes over it); chunks with rows
-    int64_t total = 0, work = 0, chunks = 0, most = 1;
+    int64_t total = 0, work = 0, chunks = 0, most = 1, rows = 0, longest_message = 0;
     for (int i = 0; i < n; ++i) {
       const int b = p.order[c0 + i];
       const int64_t of = ((int64_t)seqs->suffix_len[b] * G + kvt::kMxChunkRows - 1) / kvt::kMxChunkRows;
@@ -1223,6 +1237,8 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
       work += mx_tiles(seqs, b) * of;
       chunks += of;
       most = std::max(most, of);
+      rows = std::max(rows, (int64_t)seqs->suffix_len[b] * G);
+      longest_message = std::max<int64_t>(longest_message, seqs->suffix_len[b]);
     }
     p.chunks.push_back((int32_t)most);
     const int64_t longest = mx_tiles(seqs, p.order[c0]);
@@ -1233,22 +1249,28 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     int64_t share = std::max<int64_t>(16, (total + slots - 1) / slots);
     // a sequence lies in at most one slot more than its tiles fill
     share = std::max(share, (longest + kvt::kMxMaxParts - 2) / (kvt::kMxMaxParts - 1));
-    // A slot for each sequence needs no join (a launch, the workspace: 6.5 us) and no
-    // merge where a share goes on to the next sequence (1.5 us).  A workgroup takes
-    // 0.18 us a tile, 0.30 while another one runs on its CU; all of them read 5.5
-    // TB/s, one to a CU 4.3; and the shortest sequence starts last.  Steps of 32/8
-    // heads of 128 so and in shares: one context of 1000, 2000 and 3000 keys 11.1,
-    // 15.8 and 21.7 us, 16.5; 200 of 500..3000 62.9, 74.0 (16/2 heads 25.6, 31.5); 256
-    // of 100..600 28.2, 38.8; 100 of 1024..16384 131.8, 121.7; 70 of 6000 109.1, 87.5
-    // (4/4 heads 60.3, 47.3).
+    // A slot for each sequence needs no join (a launch, the workspace) and no merge
+    // where a share goes on to the next sequence.  A workgroup takes so long for a
+    // tile, longer while another one runs on its CU; all of them stream so much, less
+    // with one to a CU; and the shortest sequence starts last.  Steps of 32/8 heads of
+    // 128, bf16, so and in shares: one context of 1000, 2000 and 3000 keys 11.1, 15.8
+    // and 21.7 us, 16.5; 200 of 500..3000 62.9, 74.0 (16/2 heads 25.6, 31.5); 256 of
+    // 100..600 28.2, 38.8; 100 of 1024..16384 131.8, 121.7; 70 of 6000 109.1, 87.5
+    // (4/4 heads 60.3, 47.3); 100 of 500..3000 38.7, 47.1, heads of 64 28.3, 37.2, with
+    // fp32 queries 27.9, 43.4.  The rates were taken from 1464 calls timed both ways (heads of 64
+    // and 128, bf16 and fp32, single tokens and messages, 1 to 200 contexts of 300 to
+    // 131000 keys): the choice takes 0.2 to 0.8 % longer than the better way on
+    // average, with the rates of 128 for heads of 64 2.5 to 4.4 %.
     const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
-    const double stream = (double)work * hkv * tile_bytes / 5.5e6;
+    const MxRates& r = mx_rates(pool->head_dim, rows > 16 && longest_message > 1);
+    const double stream = (double)work * hkv * tile_bytes / r.stream;
     const int64_t first = cus * n / (hkv * chunks);   // sequences that have a CU of their own ...
     const int64_t start = std::max<int64_t>(1, 2 * cus * n / (hkv * chunks));   // ... and that start at once
     const double beside = n > start ? longest : n > first ? mx_tiles(seqs, p.order[c0 + first]) : 0;
     const double last = n > start ? mx_tiles(seqs, p.order[c0 + n - 1]) : 0;
-    const double alone = std::max(0.18 * longest + 0.12 * beside, stream * (n > first ? 1.0 : 5.5 / 4.3) + 0.18 * last);
-    if (alone <= 6.5 + std::max(0.18 * share, stream) + 1.5 * n * share / total) share = total;
+    const double alone = std::max(r.tile * longest + r.beside * beside,
+                                  stream * (n > first ? 1.0 : r.stream / r.one) + r.tile * last);
+    if (alone <= r.join + std::max(r.tile * share, stream) + r.merge * n * share / total) share = total;
     bool split = false;
     int64_t begin = 0;
     for (int i = 0; i < n; ++i) {

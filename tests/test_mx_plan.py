@@ -32,3 +32,16 @@ def test_a_launch_is_split_by_its_own_messages(message):
     S = [message] + [1] * 255
     assert partials(first + rest, S + [1] * 3) == partials(first, S) + partials(rest, [1] * 3)
     assert partials(rest, [1] * 3) > 3
+
+
+@pytest.mark.parametrize("d, contexts, message, whole", [
+    # measured both ways: heads of 64, 100 contexts 28 us in one launch, 37 in shares and a join ...
+    (64, [500 + 25 * i for i in range(100)], 1, True),
+    (64, [2000] * 48, 16, True),
+    # ... one of 30000 keys and 4 new tokens 135 and 16
+    (64, [30000], 1, False), (128, [30000], 1, False), (64, [30000], 16, False),
+    (128, [8000] * 32, 16, True)])
+def test_whole_sequences_or_shares_by_what_was_measured(d, contexts, message, whole):
+    p = pool(nb=1 << 24, hkv=HKV, d=d)
+    s = seqs(P=contexts, S=[message] + [1] * (len(contexts) - 1), max_blocks=1 << 20)
+    assert (need("kvt_mx_extend_workspace_bytes", p, s, HQ) == 0) == whole
