@@ -1616,6 +1616,14 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
     }
   }
 
+  const std::vector<int> order = longest_first(seqs);
+  for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {   // every launch, before the first one
+    int64_t pages = 0;
+    for (int i = c0; i < std::min(B, c0 + kvt::kSeqsPerLaunch); ++i)
+      pages += (kept[order[i]] + kvt::kBlock - 1) / kvt::kBlock;
+    if (pages * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
+  }
+
   kvt::EvictArgs a;
   std::memset(&a, 0, sizeof(a));
   a.k_pool = pool->k;
@@ -1634,7 +1642,6 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
   a.sinks = ev->sinks;
   a.recent = ev->recent;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const std::vector<int> order = longest_first(seqs);
   for (int c0 = 0; c0 < B; c0 += kvt::kSeqsPerLaunch) {
     const int n = std::min(kvt::kSeqsPerLaunch, B - c0);
     int64_t pages = 0;
@@ -1644,7 +1651,6 @@ kvt_status evict(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_eviction*
       a.seq[i] = kvt::EvictDesc{b, seqs->prefix_len[b] + seqs->suffix_len[b], kept[b]};
       a.unit_begin[i] = (int32_t)pages;
       pages += (kept[b] + kvt::kBlock - 1) / kvt::kBlock;
-      if (pages * pool->num_kv_heads > INT32_MAX) return KVT_ERR_INVALID_ARG;
     }
     a.unit_begin[n] = (int32_t)pages;
     hipError_t e = kvt::launch_evict_select(a, s);
