@@ -1472,6 +1472,11 @@ kvt_status attention_weights(const kvt_pool* pool, const kvt_seqs* seqs, const v
   a.num_q_heads = num_q_heads;
   a.num_kv_heads = pool->num_kv_heads;
   a.group = G;
+  // 2^(32 + s) / G rounded up, 2^s < G <= 2^(s + 1): at least 2^31, and off by less
+  // than 1, so that x * by_group is off by less than x and the quotient is exact while
+  // x * G < 2^(32 + s)
+  while ((int64_t)2 << a.group_shift < G) ++a.group_shift;
+  a.by_group = G == 1 ? 0u : (uint32_t)((((uint64_t)1 << (32 + a.group_shift)) + G - 1) / G);
   a.scale_log2 = scale * 1.4426950408889634f;
   const bool rounded = scores == KVT_WEIGHTS_ROUNDED && pool->dtype == KVT_DTYPE_F32;
   const int format = mx ? kvt::kMx : rounded ? kvt::kRounded : pool->dtype;

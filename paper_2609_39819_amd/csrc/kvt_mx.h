@@ -92,6 +92,8 @@ struct WeightsArgs {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t group;        // Hq / Hkv
+  uint32_t by_group;    // x / group = (x * by_group >> 32) >> group_shift for x < 2 * group + 256, group > 1
+  int32_t group_shift;
   float scale_log2;
   int32_t share;        // step kernel: tiles of a workgroup
   int32_t tiles;        // turn kernel: of a workgroup, if every sequence's rows are one stage; else 0

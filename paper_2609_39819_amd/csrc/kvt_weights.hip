@@ -25,7 +25,8 @@
 //     keys as operands in registers; the rows pass through LDS, 256 in bf16 or 64
 //     in fp32 at a time, two such stages in turn, for all waves of the workgroup.
 //     512 new tokens over 8192, 32/8 heads of 128: 54.5 us, of which a full round of
-//     wide workgroups is 39 (880 TFLOP/s); fp32 195, rounded 91.
+//     wide workgroups is 39 (880 TFLOP/s) and a narrow one 15; fp32 192, rounded 91.
+//     Vector instructions take 49 % of the SIMDs' cycles, products 28 %.
 #include <type_traits>
 
 #include "kvt_mx_device.h"
@@ -429,15 +430,13 @@ __global__ __launch_bounds__(512) void weights_turn_kernel(const WeightsArgs a) 
 
   // ---- rows in stages, from the first that sees one of the workgroup's keys.
   // Row r of a stage whose first row is head h0 of token t0 is head x - d * G of
-  // token t0 + d, d = x / G, x = h0 + r < G + ROWS: up to ROWS heads a product with
-  // 2^32 / G, rounded up (exact while x * G < 2^32), with more of them d is 0 or 1.
+  // token t0 + d, d = x / G, x = h0 + r < G + ROWS.
   const int first = !ONCE && start > P ? (int)((int64_t)(start - P) * G / ROWS) : 0;
   const int adv_t = ROWS / G, adv_h = ROWS - adv_t * G;
   int t0 = (int)((int64_t)first * ROWS / G), h0 = first * ROWS - t0 * G;    // of the stage that is loaded next
-  const unsigned magic = G == 1 ? 0u : 0xffffffffu / (unsigned)G + 1u;
   auto place = [&](int r, int& tok, int64_t& row) __attribute__((always_inline)) {
     const int x = h0 + r;
-    const int d = G == 1 ? x : G > ROWS ? (int)(x >= G) : (int)__umulhi((unsigned)x, magic);
+    const int d = G == 1 ? x : (int)(__umulhi((unsigned)x, a.by_group) >> a.group_shift);
     tok = t0 + d;
     const bool past = tok >= sd.suffix;          // past the last row: any row, it sees nothing
     row = (int64_t)(sd.row_off + (past ? 0 : tok)) * a.num_q_heads + g * G + (x - d * G);
