@@ -20,10 +20,12 @@
 //
 // Bound by the matrix products, with the exponentials and the conversion of the
 // probabilities beside them, as over bf16 pages.  32/8 heads of 128, bf16: 2048
-// new tokens over 131072, 3.95 ms (1120 TFLOP/s; over bf16 pages 3.90); 512 over
-// 8192, 82 us (89); 8 sequences with heads of 64, 32..128 over 1024..16384, 56 us
-// (57): the products of 64 columns take no longer than the exponentials, and the
-// rows of a short message do not fill their tile of 256.
+// new tokens over 131072, 3.95 ms (1120 TFLOP/s; over bf16 pages 3.90; products 49 %
+// of the SIMDs' cycles, vector instructions 46 %); 512 over 8192, 82 us (89), with
+// fp32 queries 170; 8 sequences with heads of 64, 32..128 over 1024..16384, 56 us (57;
+// 20 % and 38 %): the products of 64 columns take no longer than the exponentials, and
+// the rows of a short message do not fill their tile of 256.  fp32 queries over heads
+// of 128 spill 27 registers in the main loop.
 #include "kvt_mx_device.h"
 
 namespace kvt {
