@@ -576,7 +576,8 @@ kvt_status kvt_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const
                            int64_t num_ids, void* host, int32_t direction, void* stream);
 
 /* kvt_copy_blocks for 4-bit pages: host is a packed
- * [num_ids][2][Hkv][KVT_MX_PAGE_BYTES(head_dim)] array of bytes. */
+ * [num_ids][2][Hkv][KVT_MX_PAGE_BYTES(head_dim)] array of bytes, 16-byte aligned
+ * (else KVT_ERR_INVALID_ARG). */
 kvt_status kvt_mx_copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int32_t* block_ids_host,
                               int64_t num_ids, void* host, int32_t direction, void* stream);
 

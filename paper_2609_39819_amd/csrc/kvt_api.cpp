@@ -1678,6 +1678,7 @@ kvt_status copy_blocks(const kvt_pool* pool, const int32_t* block_ids, const int
   if (num_ids < 0 || (num_ids > 0 && (block_ids == nullptr || host == nullptr))) return KVT_ERR_INVALID_ARG;
   if (direction != KVT_COPY_TO_HOST && direction != KVT_COPY_TO_DEVICE) return KVT_ERR_INVALID_ARG;
   if (num_ids == 0) return KVT_OK;
+  if (mx && !aligned16(host)) return KVT_ERR_INVALID_ARG;   // (bytes can begin anywhere)
   const int64_t page_bytes = (int64_t)pool->num_kv_heads * page_bytes_of_head(pool, mx);
   if (num_ids > (INT64_MAX / 4) / (2 * page_bytes)) return KVT_ERR_INVALID_ARG;
   if (block_ids_host != nullptr) {

@@ -51,6 +51,17 @@ def test_offload_and_reload_are_bit_exact(hkv, d, n):
     assert all(torch.equal(r.cpu(), x) for r, x in zip(rooms, want))
 
 
+def test_a_host_buffer_that_is_not_aligned_is_refused():
+    k, v = (torch.zeros((4, 1, page_bytes(64)), dtype=torch.uint8, device="cuda") for _ in "kv")
+    room = torch.empty(2 * page_bytes(64) + 16, dtype=torch.uint8, pin_memory=True)
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for at in (1, 8):
+        with pytest.raises(kvt.KvtError):
+            kvt.copy_blocks(k, v, ids, room[at:at + 2 * page_bytes(64)].view(1, 2, 1, -1), to_host=True)
+    kvt.copy_blocks(k, v, ids, room[16:].view(1, 2, 1, -1), to_host=True)
+    torch.cuda.synchronize()
+
+
 @pytest.mark.timeout(120)
 def test_ids_outside_the_pool_are_skipped():
     k, v = (torch.randint(0, 256, (32, 2, page_bytes(64)), dtype=torch.uint8, device="cuda") for _ in "kv")

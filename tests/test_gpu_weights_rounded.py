@@ -102,6 +102,45 @@ def test_weights_with_the_lse_of_the_attention_call(kind, d):
         assert share <= LSE + 2 * off
 
 
+@pytest.mark.parametrize("suffix", [1, 70])
+def test_bf16_pages_have_nothing_to_round(suffix):
+    c = Batch([300], [suffix], 8, 2, 64, "bf16", 45, cache="bf16")
+    lse, w = exact_lse(c).cuda(), [torch.ones((1, 2, 400), device="cuda") for _ in range(2)]
+    for x, flag in zip(w, (False, True)):
+        kvt.attention_weights(c.q, c.k_pool, c.v_pool, c.table, [300], [suffix], lse, x, rounded=flag)
+    assert torch.equal(*w)
+
+
+@pytest.mark.timeout(300)
+def test_a_captured_call_replays():
+    """Step and turn over rounded fp32 pages from a graph, onto weights that change between the replays."""
+    for suffix in ([1, 1], [40, 9]):
+        c = Batch([700, 90], suffix, 8, 2, 128, "f32", 46, cache="f32")
+        lse, w = exact_lse(rounded(c)).cuda(), torch.zeros((2, 2, 800), device="cuda")
+
+        def call():
+            kvt.attention_weights(c.q, c.k_pool, c.v_pool, c.table, c.prefix, suffix, lse, w, rounded=True)
+
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            call()
+        torch.cuda.current_stream().wait_stream(s)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        for i in range(3):
+            w.fill_(i)
+            call()
+            torch.cuda.synchronize()
+            want = w.clone()
+            w.fill_(i)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(w, want), (suffix, i)
+            torch.randn(1000, device="cuda").sum().item()
+
+
 @pytest.mark.timeout(300)
 def test_turns_over_fp32_pages():
     """Chunks and single tokens, each with the attention's own log-sum-exp, add up to the weights of all of them."""

@@ -28,6 +28,7 @@ def test_bad_calls_are_rejected():
     pageable = np.zeros(4 * 2 * 544, dtype=np.uint8)
     assert copy(pool(), ids_host=[0, 1, 2, 3], host=pageable.ctypes.data) == E
     assert copy(pool(), n=1 << 60) == E                    # bytes past 64 bits
+    assert copy(pool(), host=FAKE_OUT + 8, ids_host=[0, 64, 1, 2]) == E      # not aligned, before the ids are looked at
 
 
 def test_the_binding_takes_records_alone():
