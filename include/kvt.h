@@ -443,7 +443,9 @@ kvt_status kvt_mx_read_kv(const kvt_pool* pool, const kvt_seqs* seqs, const kvt_
  * without splitting, otherwise at least kvt_mx_extend_workspace_bytes() for the
  * same arguments, 16-byte aligned and apart from q, out, lse and the pools (else
  * KVT_ERR_WORKSPACE, KVT_ERR_INVALID_ARG; any workspace will do where that is
- * 0).  Results are bit-reproducible for given arguments.
+ * 0; with more than 64 rows of a kv-head, new tokens x query heads, in a message a
+ * smaller one that holds the fewer splits of kvt_extend_attention, too).  Results
+ * are bit-reproducible for given arguments.
  */
 kvt_status kvt_mx_extend_attention(const kvt_pool* pool, const kvt_seqs* seqs,
                                    const void* q, int32_t num_q_heads, float scale,
