@@ -1257,10 +1257,10 @@ MxDecodePlan mx_decode_plan(const kvt_pool* pool, const kvt_seqs* seqs, int32_t 
     // and 21.7 us, 16.5; 200 of 500..3000 62.9, 74.0 (16/2 heads 25.6, 31.5); 256 of
     // 100..600 28.2, 38.8; 100 of 1024..16384 131.8, 121.7; 70 of 6000 109.1, 87.5
     // (4/4 heads 60.3, 47.3); 100 of 500..3000 38.7, 47.1, heads of 64 28.3, 37.2, with
-    // fp32 queries 27.9, 43.4.  The rates were taken from 1464 calls timed both ways (heads of 64
-    // and 128, bf16 and fp32, single tokens and messages, 1 to 200 contexts of 300 to
+    // fp32 queries 27.9, 43.4.  The rates are from 1464 calls timed both ways (heads of
+    // 64 and 128, bf16 and fp32, single tokens and messages, 1 to 200 contexts of 300 to
     // 131000 keys): the choice takes 0.2 to 0.8 % longer than the better way on
-    // average, with the rates of 128 for heads of 64 2.5 to 4.4 %.
+    // average; with the rates of 128 for heads of 64 it took 2.5 to 4.4 %.
     const double tile_bytes = 2.0 * kvt::mx_page_bytes(pool->head_dim) * kvt::kDecKeysPerTile / kvt::kBlock;
     const MxRates& r = mx_rates(pool->head_dim, rows > 16 && longest_message > 1);
     const double stream = (double)work * hkv * tile_bytes / r.stream;
